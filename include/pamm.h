@@ -70,7 +70,9 @@ typedef enum { PAMM_IDX_I32 = 0, PAMM_IDX_U16 = 1, PAMM_IDX_U8 = 2 } pamm_index_
 typedef enum {
     PAMM_WS_COMPRESS = 0,            /* sort products pamm_compress_fused leaves for the backward pass */
     PAMM_WS_CONTRACT = 1,            /* also covers pamm_contract_weight_grad */
-    PAMM_WS_STEP_HOST = 2            /* device arena of pamm_qkv_step_host    */
+    PAMM_WS_STEP_HOST = 2,           /* device arena of pamm_qkv_step_host    */
+    PAMM_WS_NORM_BACKWARD = 3,       /* pamm_norm_backward of b rows of n (m and k are not looked at; b may be 0) */
+    PAMM_WS_GRAD_NORM = 4            /* pamm_grad_norm, pamm_clip_grad_norm (no size is looked at) */
 } pamm_ws_kind;
 
 /* Human-readable name of a status code (static string, never NULL). */
@@ -358,6 +360,118 @@ pamm_status pamm_saved_bytes(int64_t b, int64_t n, int64_t k, pamm_dtype dt, pam
 pamm_status pamm_contract_no_alloc(const int32_t* f, const float* alpha, const void* dY, int64_t ldy,
                                    int64_t b, int64_t m, pamm_dtype dt, int64_t k,
                                    float* Btilde, int64_t ldb, void* stream);
+
+/*
+ * ---- Operators around the projection ------------------------------------------------
+ * What a training step runs directly before the fused Q|K|V projection (the norm whose
+ * output is X), directly after it (rotary positions on the heads of Z) and at its end (the
+ * gradients' norm and clipping).  The paper takes them as given; their formulas are below.
+ * They keep the conventions above, with these differences: rows need only the alignment
+ * of their element type (rows that are 16-byte aligned are faster), zero rows are a valid
+ * call, and outputs may take the place of inputs where the comment says so.
+ */
+typedef enum { PAMM_NORM_LAYER = 0, PAMM_NORM_RMS = 1 } pamm_norm_kind;
+
+/*
+ * Layer norm, or its root-mean-square form, of the rows of X, with the residual addition:
+ *   h = x (+ r);  mu = mean(h), 0 in the RMS form;  v = mean((h - mu)^2);
+ *   s = 1 / sqrt(v + eps);  y = (h - mu) s w (+ c)
+ * Sums are fp32 over rows held on chip (the variance is taken around the mean).  mu, s and y
+ * are those of h before it is rounded to dt.
+ *   R      b x n or NULL: no addition.      H   b x n or NULL: receives h, rounded to dt
+ *   w, c   n entries of w_dt, or NULL (1 and 0)
+ *   mean, rstd   b fp32 each, or NULL: mu and s for the backward pass (mean receives 0 in the RMS form)
+ * Y may be X or R, and H may be X or R (the same base and leading dimension); Y may not be H.
+ * A row with a NaN or infinity gives what the formulas give.  Limit: n <= 32768.
+ */
+pamm_status pamm_norm_forward(pamm_norm_kind kind, const void* X, int64_t ldx, const void* R, int64_t ldr, int64_t b, int64_t n,
+                              pamm_dtype dt, const void* w, const void* c, pamm_dtype w_dt, float eps, void* Y, int64_t ldy,
+                              void* H, int64_t ldh, float* mean, float* rstd, void* stream);
+
+/*
+ * Its backward pass.  X is the row that was normalised (h where there was an addition):
+ *   u = (x - mu) s;  g = dy w;  dx = s (g - mean(g) - u mean(g u)) (+ dh), without mean(g) in the RMS form
+ *   dw = sum over rows of dy u;  dc = sum over rows of dy
+ *   mean   b fp32 (not read in the RMS form, may be NULL);  rstd   b fp32
+ *   dH     b x n or NULL: the gradient that reached h past the norm, added to dx.  With an addition in
+ *          the forward pass dX is the gradient of both of its inputs.
+ *   dw, dc n entries of dw_dt, each may be NULL.  Summed in fp32 in a fixed order, rounded once.
+ *   workspace  pamm_workspace_bytes(PAMM_WS_NORM_BACKWARD, b, n, ...); may be NULL if dw and dc are
+ * dX may be dY, X or dH (the same base and leading dimension).  b = 0 gives dw = dc = 0.
+ * Limit: n <= 32768.
+ */
+pamm_status pamm_norm_backward(pamm_norm_kind kind, const void* dY, int64_t lddy, const void* X, int64_t ldx, const float* mean,
+                               const float* rstd, int64_t b, int64_t n, pamm_dtype dt, const void* w, pamm_dtype w_dt,
+                               const void* dH, int64_t lddh, void* dX, int64_t lddx, void* dw, void* dc, pamm_dtype dw_dt,
+                               void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Rotary positions.  Pair i of a head at position p is turned by p f_i:
+ *   (x1, x2) -> (x1 cos - x2 sin, x2 cos + x1 sin)
+ * with the pairs (i, i + rot_dim/2) (PAMM_PAIRS_HALF) or (2i, 2i+1) (PAMM_PAIRS_ADJACENT) of the head's
+ * first rot_dim elements; the others pass through.
+ *
+ * pamm_rotary_frequencies_host: f_i = base^(-2i/rot_dim) for i < rot_dim/2, in 64 bits, on the HOST, with
+ * one of the published scalings for contexts `factor` times longer than the trained one:
+ *   PAMM_ROTARY_LINEAR  f_i / factor (position interpolation, arXiv 2306.15595)
+ *   PAMM_ROTARY_BASE    the base times factor^(rot_dim/(rot_dim-2)): the fastest pair keeps its frequency,
+ *                       the slowest gets f / factor
+ *   PAMM_ROTARY_PARTS   by parts (arXiv 2309.00071): a pair that turns t = trained_length f_i / 2 pi times keeps
+ *                       the share min(1, max(0, (t - slow)/(fast - slow))) of f_i and takes the rest from
+ *                       f_i / factor; *amplitude = 0.1 ln(factor) + 1 (1 for the other kinds)
+ * pamm_rotary_table: rows of positions first .. first + length - 1, rot_dim fp32 each, on the device:
+ *   [amplitude cos(p f_0) .. | amplitude sin(p f_0) ..], computed in 64 bits and rounded once.  `freq` is the
+ *   HOST array of rot_dim/2; it is read before the call returns.
+ * Limit: rot_dim <= 512.
+ */
+typedef enum { PAMM_PAIRS_HALF = 0, PAMM_PAIRS_ADJACENT = 1 } pamm_rotary_pairs;
+typedef enum { PAMM_ROTARY_PLAIN = 0, PAMM_ROTARY_LINEAR = 1, PAMM_ROTARY_BASE = 2, PAMM_ROTARY_PARTS = 3 } pamm_rotary_scaling;
+typedef enum { PAMM_POS_I32 = 0, PAMM_POS_I64 = 1 } pamm_position_type;
+pamm_status pamm_rotary_frequencies_host(int64_t rot_dim, double base, pamm_rotary_scaling scaling, double factor,
+                                         int64_t trained_length, double slow, double fast, double* freq, double* amplitude);
+pamm_status pamm_rotary_table(const double* freq, int64_t rot_dim, double amplitude, int64_t first, int64_t length, float* table,
+                              void* stream);
+
+/*
+ * The rotation.  Element d of head h of token s of sequence b of X lies at
+ * X[b x_batch + s x_token + h x_head + d] (distances in elements, of any sign and order; 0 repeats), so the heads can
+ * be columns of the fused row [Q|K|V] or lie in any other order of batch, token and head.
+ *   rotated    the first `rotated` of the `heads` heads are turned, the others pass through
+ *   transposed 0, or 1 for the transposed turn (sin -> -sin): the gradient of X from that of Y
+ *   table      table_rows x rot_dim fp32 as pamm_rotary_table leaves it
+ *   positions  NULL: token s of every sequence has position first + s (which must fit the table: PAMM_ERR_INVALID_ARG);
+ *              else the device entries positions[b pos_batch + s pos_token].  A position outside
+ *              the table raises PAMM_ERR_BAD_INDEX in the device status and its token passes through unturned.
+ * Y may be X with the same distances: only what is turned is then read and written.  Products and sums are fp32,
+ * rounded once to dt.  A zero count of anything is a valid call that does nothing.
+ */
+pamm_status pamm_rotary(const void* X, int64_t x_batch, int64_t x_token, int64_t x_head, void* Y, int64_t y_batch, int64_t y_token,
+                        int64_t y_head, int64_t batch, int64_t seq, int64_t heads, int64_t rotated, int64_t head_dim,
+                        int64_t rot_dim, pamm_dtype dt, pamm_rotary_pairs pairs, int transposed, const float* table,
+                        int64_t table_rows, const void* positions, pamm_position_type pos_type, int64_t pos_batch,
+                        int64_t pos_token, int64_t first, void* stream);
+
+/*
+ * The global norm of a list of gradients and their clipping:
+ *   N = sqrt(sum over all elements of all tensors of g^2);  out = g min(1, max_norm / (N + 1e-6))
+ * The list is a HOST array, read before the call returns; its tensors are device matrices of any size (rows or
+ * columns may be 0), any mix of types, aligned to their element.  Squares are summed in 64 bits and in a fixed order.
+ *   norm       one fp32 on the device: N
+ *   out        NULL: the gradients are scaled in place, and where the factor is 1 nothing is written; else as many
+ *              tensors of the same rows and columns, of any type, that receive the result (rounded once; a tensor may
+ *              be its own output in the same type, other overlaps are not allowed)
+ *   max_norm   >= 0; infinity sets no limit.  If N is infinite or NaN the factor is what the formula gives (0 or
+ *              NaN): look at *norm before the step is taken.
+ *   workspace  pamm_workspace_bytes(PAMM_WS_GRAD_NORM, ...)
+ */
+typedef struct {
+    void* data;
+    int64_t rows, cols, ld;      /* ld is not looked at for fewer than two rows */
+    int64_t dt;                  /* a pamm_dtype */
+} pamm_tensor;
+pamm_status pamm_grad_norm(const pamm_tensor* grads, int64_t count, float* norm, void* workspace, size_t ws_bytes, void* stream);
+pamm_status pamm_clip_grad_norm(const pamm_tensor* grads, const pamm_tensor* out, int64_t count, double max_norm, float* norm,
+                                void* workspace, size_t ws_bytes, void* stream);
 
 /*
  * Reads and clears the current device's status word WITHOUT waiting for any of the

@@ -2,6 +2,7 @@
 // Every step of the path runs in the kernels included below; nothing here
 // computes on the host apart from pamm_draw_indices_host.
 #include <algorithm>
+#include <cmath>
 #include <cstdio>
 #include <cstring>
 #include <map>
@@ -25,6 +26,9 @@
 #include "linear_forward_pair.cuh"
 #include "small_k.cuh"
 #include "read_probe.cuh"
+#include "norm.cuh"
+#include "rotary.cuh"
+#include "grad_clip.cuh"
 
 using namespace pamm;
 
@@ -539,7 +543,301 @@ __global__ void selftest_bounded_wait_kernel(uint32_t polls) {
     if (!done && (threadIdx.x & 31) == 0) raise_status(DEV_TIMEOUT);
 }
 
+// ---- the operators around the projection ---------------------------------------------------
+namespace {
+
+// Row partition of the norm's column sums, and the scratch that holds their partial sums.
+inline int64_t norm_splits(int64_t b) { return std::max<int64_t>(1, std::min<int64_t>((b + 31) / 32, 2 * sm_count())); }
+inline size_t norm_backward_ws_bytes(int64_t b, int64_t n) { return (size_t)round_up(norm_splits(b) * 2 * n * 4, 256); }
+inline int grad_norm_blocks() { return sm_count() * GC_BLOCKS_PER_SM; }
+inline size_t grad_norm_ws_bytes() { return (size_t)round_up((int64_t)grad_norm_blocks() * 8, 256); }
+
+// An element-aligned row-major matrix of at least one row; leading dimension in elements.
+inline bool matrix_ok(const void* p, int64_t ld, int64_t cols, size_t es) { return p && aligned(p, es) && ld >= cols; }
+// Whether every row of the matrix starts on a 16-byte boundary (null: no matrix, no restriction).
+inline bool rows_aligned(const void* p, int64_t ld, size_t es) { return !p || (aligned(p, 16) && (ld * (int64_t)es) % 16 == 0); }
+
+template <typename T, int V>
+pamm_status launch_norm_forward(NormForwardArgs a, cudaStream_t st) {
+    const int ept = a.n <= 256 ? 8 : a.n <= 16384 ? 16 : 32;
+    a.warps = (int)((a.n + 32 * ept - 1) / (32 * ept));
+    const int threads = a.warps == 1 ? 256 : 32 * a.warps;
+    const int64_t rows_per_block = a.warps == 1 ? 8 : 1;
+    const dim3 grid((unsigned)((a.b + rows_per_block - 1) / rows_per_block));
+    if (ept == 8) launch(norm_forward_kernel<T, V, 8>, grid, dim3(threads), 0, st, true, a);
+    else if (ept == 16) launch(norm_forward_kernel<T, V, 16>, grid, dim3(threads), 0, st, true, a);
+    else launch(norm_forward_kernel<T, V, 32>, grid, dim3(threads), 0, st, true, a);
+    return launch_status();
+}
+
+template <typename T, int V>
+pamm_status launch_norm_backward(NormBackwardArgs a, cudaStream_t st) {
+    // the column sums first: dX may take the place of dY or X
+    if (a.dw || a.dc) {
+        const unsigned blocks = (unsigned)((a.n + NB_COL_THREADS - 1) / NB_COL_THREADS);
+        if (a.b) launch(norm_backward_columns_kernel<T>, dim3(blocks, (unsigned)a.splits), dim3(NB_COL_THREADS), 0, st, true, a);
+        launch(norm_backward_finish_kernel, dim3(blocks), dim3(NB_COL_THREADS), 0, st, true, a);
+    }
+    if (a.b) launch(norm_backward_row_kernel<T, V>, dim3((unsigned)a.b), dim3(NB_WIDE_THREADS), 0, st, true, a);
+    return launch_status();
+}
+
+template <typename T>
+pamm_status launch_rotary(const RotaryArgs& a, int64_t tokens, bool vec, cudaStream_t st) {
+    const dim3 grid((unsigned)tokens), block(ROTARY_THREADS);
+    if (vec) launch(rotary_kernel<T, Vec16<T>::N>, grid, block, 0, st, true, a);
+    else launch(rotary_kernel<T, 1>, grid, block, 0, st, true, a);
+    return launch_status();
+}
+
+// A launch whose parameters are too large to be copied from call to call.
+template <typename... A>
+void launch_in_place(const void* kern, unsigned grid, int block, cudaStream_t st, A*... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3((unsigned)block);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    void* pointers[] = {(void*)args...};
+    cudaLaunchKernelExC(&cfg, kern, pointers);
+    g_launches += 1;
+}
+
+pamm_status check_tensors(const pamm_tensor* t, int64_t count) {
+    if (count < 0 || (count > 0 && !t)) return PAMM_ERR_INVALID_ARG;
+    for (int64_t i = 0; i < count; ++i) {
+        if (t[i].dt != PAMM_F32 && t[i].dt != PAMM_BF16) return PAMM_ERR_UNSUPPORTED;
+        if (t[i].rows < 0 || t[i].cols < 0 || t[i].rows > (1ll << 40) || t[i].cols > (1ll << 40)) return PAMM_ERR_INVALID_ARG;
+        if (t[i].rows == 0 || t[i].cols == 0) continue;
+        if (!t[i].data || !aligned(t[i].data, esize((pamm_dtype)t[i].dt)) || (t[i].rows > 1 && t[i].ld < t[i].cols))
+            return PAMM_ERR_INVALID_ARG;
+        if (t[i].rows > (1ll << 40) / t[i].cols) return PAMM_ERR_INVALID_ARG;
+    }
+    return PAMM_OK;
+}
+
+// Fills the list with the tensors from `at` on that one launch holds; returns the first one left.
+template <int CAP>
+int64_t fill_grad_list(GradList<CAP>& list, const pamm_tensor* in, const pamm_tensor* out, int64_t at, int64_t count) {
+    list.count = 0;
+    list.chunks = 0;
+    for (; at < count && list.count < CAP; ++at) {
+        const pamm_tensor& t = in[at];
+        const pamm_tensor& o = out ? out[at] : t;
+        if (t.rows == 0 || t.cols == 0) continue;
+        GradEntry& e = list.e[list.count++];
+        e.in = t.data;
+        e.out = o.data;
+        e.in_bf16 = t.dt == PAMM_BF16;
+        e.out_bf16 = o.dt == PAMM_BF16;
+        const bool dense = t.rows == 1 || (t.ld == t.cols && o.ld == o.cols);       // one long row
+        e.rows = dense ? 1 : t.rows;
+        e.cols = dense ? t.rows * t.cols : t.cols;
+        e.ld_in = t.ld;
+        e.ld_out = o.ld;
+        e.first_chunk = list.chunks;
+        list.chunks += grad_chunks(e.rows, e.cols);
+    }
+    return at;
+}
+
+template <int CAP>
+pamm_status run_grad_clip(const pamm_tensor* in, const pamm_tensor* out, int64_t count, bool scale, double max_norm, float* norm,
+                          double* partial, cudaStream_t st) {
+    GradList<CAP> list;
+    int64_t most = 1, lists = 0;
+    for (int64_t at = 0; at < count; ++lists) {
+        at = fill_grad_list(list, in, nullptr, at, count);
+        most = std::max(most, list.chunks);
+    }
+    int parts = (int)std::min<int64_t>(most, grad_norm_blocks());
+    list.add = 0;
+    int64_t at = 0;
+    do {
+        if (lists != 1 || count == 0) at = fill_grad_list(list, in, nullptr, at, count);
+        else at = count;                                     // still filled
+        launch_in_place((const void*)grad_squares_kernel<CAP>, (unsigned)parts, GC_THREADS, st, &list, &partial);
+        list.add = 1;
+    } while (at < count);
+    if (!scale) {
+        const double* p = partial;
+        launch_in_place((const void*)grad_norm_finish_kernel, 1, GC_THREADS, st, &p, &parts, &norm);
+        return launch_status();
+    }
+    at = 0;
+    do {
+        at = fill_grad_list(list, in, out, at, count);
+        const double* p = partial;
+        launch_in_place((const void*)grad_scale_kernel<CAP>, (unsigned)std::max<int64_t>(1, std::min<int64_t>(list.chunks, grad_norm_blocks())),
+                        GC_THREADS, st, &list, &p, &parts, &max_norm, &norm);
+        norm = nullptr;
+    } while (at < count);
+    return launch_status();
+}
+
+pamm_status grad_clip(const pamm_tensor* in, const pamm_tensor* out, int64_t count, bool scale, double max_norm, float* norm,
+                      void* workspace, size_t ws_bytes, void* stream) {
+    pamm_status s = check_tensors(in, count);
+    if (s != PAMM_OK) return s;
+    if (out) {
+        s = check_tensors(out, count);
+        if (s != PAMM_OK) return s;
+        for (int64_t i = 0; i < count; ++i)
+            if (out[i].rows != in[i].rows || out[i].cols != in[i].cols) return PAMM_ERR_INVALID_ARG;
+    }
+    if (!norm || !aligned(norm, 4) || !(max_norm >= 0.0)) return PAMM_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 256) || ws_bytes < grad_norm_ws_bytes()) return PAMM_ERR_WORKSPACE;
+    cudaStream_t st = (cudaStream_t)stream;
+    return count <= GC_SMALL ? run_grad_clip<GC_SMALL>(in, out, count, scale, max_norm, norm, (double*)workspace, st)
+                             : run_grad_clip<GC_LARGE>(in, out, count, scale, max_norm, norm, (double*)workspace, st);
+}
+
+}  // namespace
+
 extern "C" {
+
+pamm_status pamm_norm_forward(pamm_norm_kind kind, const void* X, int64_t ldx, const void* R, int64_t ldr, int64_t b, int64_t n,
+                              pamm_dtype dt, const void* w, const void* c, pamm_dtype w_dt, float eps, void* Y, int64_t ldy,
+                              void* H, int64_t ldh, float* mean, float* rstd, void* stream) {
+    if (!dtype_ok(dt) || !dtype_ok(w_dt) || (kind != PAMM_NORM_LAYER && kind != PAMM_NORM_RMS)) return PAMM_ERR_UNSUPPORTED;
+    if (b < 0 || n < 1 || b > MAX_ROWS || !(eps >= 0.f)) return PAMM_ERR_INVALID_ARG;
+    if (n > NORM_MAX_N) return PAMM_ERR_UNSUPPORTED;
+    if (b == 0) return PAMM_OK;
+    const size_t es = esize(dt), ws = esize(w_dt);
+    if (!matrix_ok(X, ldx, n, es) || !matrix_ok(Y, ldy, n, es) || (R && !matrix_ok(R, ldr, n, es)) || (H && !matrix_ok(H, ldh, n, es)))
+        return PAMM_ERR_INVALID_ARG;
+    if (!aligned(w, ws) || !aligned(c, ws) || !aligned(mean, 4) || !aligned(rstd, 4) || H == Y) return PAMM_ERR_INVALID_ARG;
+    NormForwardArgs a;
+    a.x = X; a.r = R; a.w = w; a.c = c; a.y = Y; a.h = H; a.mean = mean; a.rstd = rstd;
+    a.ldx = ldx; a.ldr = ldr; a.ldy = ldy; a.ldh = ldh; a.b = b;
+    a.n = (int)n; a.warps = 0; a.eps = eps;
+    a.rms = kind == PAMM_NORM_RMS; a.w_bf16 = w_dt == PAMM_BF16; a.w_vec = aligned(w, 16) && aligned(c, 16);
+    const bool vec = rows_aligned(X, ldx, es) && rows_aligned(R, ldr, es) && rows_aligned(Y, ldy, es) && rows_aligned(H, ldh, es);
+    cudaStream_t st = (cudaStream_t)stream;
+    if (dt == PAMM_F32) return vec ? launch_norm_forward<float, 4>(a, st) : launch_norm_forward<float, 1>(a, st);
+    return vec ? launch_norm_forward<__nv_bfloat16, 8>(a, st) : launch_norm_forward<__nv_bfloat16, 1>(a, st);
+}
+
+pamm_status pamm_norm_backward(pamm_norm_kind kind, const void* dY, int64_t lddy, const void* X, int64_t ldx, const float* mean,
+                               const float* rstd, int64_t b, int64_t n, pamm_dtype dt, const void* w, pamm_dtype w_dt,
+                               const void* dH, int64_t lddh, void* dX, int64_t lddx, void* dw, void* dc, pamm_dtype dw_dt,
+                               void* workspace, size_t ws_bytes, void* stream) {
+    if (!dtype_ok(dt) || !dtype_ok(w_dt) || !dtype_ok(dw_dt) || (kind != PAMM_NORM_LAYER && kind != PAMM_NORM_RMS))
+        return PAMM_ERR_UNSUPPORTED;
+    if (b < 0 || n < 1 || b > MAX_ROWS) return PAMM_ERR_INVALID_ARG;
+    if (n > NORM_MAX_N) return PAMM_ERR_UNSUPPORTED;
+    const size_t es = esize(dt);
+    const bool rms = kind == PAMM_NORM_RMS;
+    if (!aligned(w, esize(w_dt)) || !aligned(dw, esize(dw_dt)) || !aligned(dc, esize(dw_dt)) || (dw && dw == dc))
+        return PAMM_ERR_INVALID_ARG;
+    if (b > 0) {
+        if (!matrix_ok(dY, lddy, n, es) || !matrix_ok(X, ldx, n, es) || !matrix_ok(dX, lddx, n, es) || (dH && !matrix_ok(dH, lddh, n, es)))
+            return PAMM_ERR_INVALID_ARG;
+        if (!rstd || !aligned(rstd, 4) || (!rms && !mean) || !aligned(mean, 4)) return PAMM_ERR_INVALID_ARG;
+    }
+    if ((dw || dc) && (!workspace || !aligned(workspace, 256) || ws_bytes < norm_backward_ws_bytes(b, n))) return PAMM_ERR_WORKSPACE;
+    if (b == 0 && !dw && !dc) return PAMM_OK;
+    NormBackwardArgs a;
+    a.dy = dY; a.x = X; a.w = w; a.dh = dH; a.mean = mean; a.rstd = rstd; a.dx = dX; a.dw = dw; a.dc = dc;
+    a.part = (float*)workspace;
+    a.lddy = lddy; a.ldx = ldx; a.lddh = lddh; a.lddx = lddx; a.b = b;
+    a.n = (int)n;
+    a.rows_per_split = b ? (b + norm_splits(b) - 1) / norm_splits(b) : 1;
+    a.splits = (int)((b + a.rows_per_split - 1) / a.rows_per_split);
+    a.rms = rms; a.w_bf16 = w_dt == PAMM_BF16; a.w_vec = aligned(w, 16); a.dw_bf16 = dw_dt == PAMM_BF16;
+    const bool vec = rows_aligned(dY, lddy, es) && rows_aligned(X, ldx, es) && rows_aligned(dH, lddh, es) && rows_aligned(dX, lddx, es);
+    cudaStream_t st = (cudaStream_t)stream;
+    if (dt == PAMM_F32) return vec ? launch_norm_backward<float, 4>(a, st) : launch_norm_backward<float, 1>(a, st);
+    return vec ? launch_norm_backward<__nv_bfloat16, 8>(a, st) : launch_norm_backward<__nv_bfloat16, 1>(a, st);
+}
+
+pamm_status pamm_rotary_frequencies_host(int64_t rot_dim, double base, pamm_rotary_scaling scaling, double factor,
+                                         int64_t trained_length, double slow, double fast, double* freq, double* amplitude) {
+    if (!freq || !amplitude || rot_dim < 2 || rot_dim % 2 || !(base > 0.0) || std::isinf(base)) return PAMM_ERR_INVALID_ARG;
+    if (rot_dim > ROTARY_MAX_ROT) return PAMM_ERR_UNSUPPORTED;
+    if (scaling < PAMM_ROTARY_PLAIN || scaling > PAMM_ROTARY_PARTS) return PAMM_ERR_UNSUPPORTED;
+    if (scaling != PAMM_ROTARY_PLAIN && (!(factor >= 1.0) || std::isinf(factor))) return PAMM_ERR_INVALID_ARG;
+    if (scaling == PAMM_ROTARY_PARTS && (trained_length < 1 || !(slow >= 0.0) || !(fast > slow))) return PAMM_ERR_INVALID_ARG;
+    if (scaling == PAMM_ROTARY_BASE && rot_dim > 2) base *= pow(factor, (double)rot_dim / (double)(rot_dim - 2));
+    *amplitude = scaling == PAMM_ROTARY_PARTS ? 0.1 * log(factor) + 1.0 : 1.0;
+    for (int64_t i = 0; i < rot_dim / 2; ++i) {
+        const double f = pow(base, -2.0 * (double)i / (double)rot_dim);
+        double keep = 1.0;                        // share of the unscaled frequency
+        if (scaling == PAMM_ROTARY_LINEAR) keep = 0.0;
+        if (scaling == PAMM_ROTARY_PARTS) {
+            const double turns = (double)trained_length * f / 6.283185307179586476925;
+            keep = std::min(1.0, std::max(0.0, (turns - slow) / (fast - slow)));
+        }
+        freq[i] = keep == 1.0 ? f : f / factor + keep * (f - f / factor);
+    }
+    return PAMM_OK;
+}
+
+pamm_status pamm_rotary_table(const double* freq, int64_t rot_dim, double amplitude, int64_t first, int64_t length, float* table,
+                              void* stream) {
+    if (!freq || rot_dim < 2 || rot_dim % 2 || length < 0 || first < 0 || first > (1ll << 50) || length > (1ll << 40))
+        return PAMM_ERR_INVALID_ARG;
+    if (rot_dim > ROTARY_MAX_ROT) return PAMM_ERR_UNSUPPORTED;
+    if (length == 0) return PAMM_OK;
+    if (!table || !aligned(table, 4)) return PAMM_ERR_INVALID_ARG;
+    RotaryFrequencies f = {};
+    std::copy(freq, freq + rot_dim / 2, f.f);
+    const int64_t want = (length * (rot_dim / 2) + ROTARY_THREADS - 1) / ROTARY_THREADS;
+    launch(rotary_table_kernel, dim3((unsigned)std::min<int64_t>(want, 8 * sm_count())), dim3(ROTARY_THREADS), 0, (cudaStream_t)stream,
+           true, f, (int)(rot_dim / 2), amplitude, first, length, table);
+    return launch_status();
+}
+
+pamm_status pamm_rotary(const void* X, int64_t x_batch, int64_t x_token, int64_t x_head, void* Y, int64_t y_batch, int64_t y_token,
+                        int64_t y_head, int64_t batch, int64_t seq, int64_t heads, int64_t rotated, int64_t head_dim,
+                        int64_t rot_dim, pamm_dtype dt, pamm_rotary_pairs pairs, int transposed, const float* table,
+                        int64_t table_rows, const void* positions, pamm_position_type pos_type, int64_t pos_batch,
+                        int64_t pos_token, int64_t first, void* stream) {
+    if (!dtype_ok(dt) || (pairs != PAMM_PAIRS_HALF && pairs != PAMM_PAIRS_ADJACENT)) return PAMM_ERR_UNSUPPORTED;
+    if (positions && pos_type != PAMM_POS_I32 && pos_type != PAMM_POS_I64) return PAMM_ERR_UNSUPPORTED;
+    if (batch < 0 || seq < 0 || heads < 0 || rotated < 0 || rotated > heads || head_dim < 1 || rot_dim < 2 || rot_dim % 2 ||
+        rot_dim > head_dim)
+        return PAMM_ERR_INVALID_ARG;
+    if (rot_dim > ROTARY_MAX_ROT || seq > MAX_ROWS || heads * head_dim > (1ll << 30) || heads > (1ll << 30) || head_dim > (1ll << 20) ||
+        (seq > 0 && batch > MAX_ROWS / seq))
+        return PAMM_ERR_UNSUPPORTED;
+    if (batch == 0 || seq == 0 || heads == 0) return PAMM_OK;
+    const size_t es = esize(dt);
+    if (!X || !Y || !table || !aligned(X, es) || !aligned(Y, es) || !aligned(table, 4) || table_rows < 1) return PAMM_ERR_INVALID_ARG;
+    if (positions ? !aligned(positions, pos_type == PAMM_POS_I64 ? 8 : 4)
+                  : first < 0 || first > table_rows || seq > table_rows - first)
+        return PAMM_ERR_INVALID_ARG;
+    // the same matrix in and out is turned in place; other overlaps are the caller's error
+    const bool in_place = X == (const void*)Y;
+    if (in_place && (x_batch != y_batch || x_token != y_token || x_head != y_head)) return PAMM_ERR_INVALID_ARG;
+    RotaryArgs a;
+    a.x = X; a.y = Y; a.table = table; a.positions = positions;
+    a.xb = x_batch; a.xs = x_token; a.xh = x_head; a.yb = y_batch; a.ys = y_token; a.yh = y_head;
+    a.pb = pos_batch; a.ps = pos_token; a.table_rows = table_rows; a.first = first;
+    a.seq = (int)seq; a.heads = (int)heads; a.rotated = (int)rotated; a.head_dim = (int)head_dim; a.rot = (int)rot_dim;
+    a.adjacent = pairs == PAMM_PAIRS_ADJACENT; a.transposed = transposed != 0; a.pos64 = pos_type == PAMM_POS_I64;
+    a.in_place = in_place;
+    const int64_t v = 16 / (int64_t)es;
+    const bool vec = aligned(X, 16) && aligned(Y, 16) && aligned(table, 16) && head_dim % v == 0 &&
+                     (a.adjacent ? rot_dim % v == 0 : rot_dim % (2 * v) == 0) && x_batch % v == 0 && x_token % v == 0 &&
+                     x_head % v == 0 && y_batch % v == 0 && y_token % v == 0 && y_head % v == 0;
+    cudaStream_t st = (cudaStream_t)stream;
+    return dt == PAMM_F32 ? launch_rotary<float>(a, batch * seq, vec, st) : launch_rotary<__nv_bfloat16>(a, batch * seq, vec, st);
+}
+
+pamm_status pamm_grad_norm(const pamm_tensor* grads, int64_t count, float* norm, void* workspace, size_t ws_bytes, void* stream) {
+    return grad_clip(grads, nullptr, count, false, 0.0, norm, workspace, ws_bytes, stream);
+}
+
+pamm_status pamm_clip_grad_norm(const pamm_tensor* grads, const pamm_tensor* out, int64_t count, double max_norm, float* norm,
+                                void* workspace, size_t ws_bytes, void* stream) {
+    return grad_clip(grads, out, count, true, max_norm, norm, workspace, ws_bytes, stream);
+}
+
 
 pamm_status pamm_selftest_bounded_wait(void* stream) {
     launch(selftest_bounded_wait_kernel, dim3(1), dim3(64), 0, (cudaStream_t)stream, false, (uint32_t)2048);
@@ -601,6 +899,11 @@ pamm_status pamm_set_profile_events(pamm_prof_kind kind, void* start_event, void
 }
 
 size_t pamm_workspace_bytes(pamm_ws_kind kind, int64_t b, int64_t n, int64_t m, int64_t k, pamm_dtype dt) {
+    if (kind == PAMM_WS_NORM_BACKWARD) {
+        if (!dtype_ok(dt) || b < 0 || b > MAX_ROWS || n < 1 || n > NORM_MAX_N) return (size_t)-1;
+        return norm_backward_ws_bytes(b, n);
+    }
+    if (kind == PAMM_WS_GRAD_NORM) return grad_norm_ws_bytes();
     if (!dtype_ok(dt) || b < 1 || k < 1 || k > b || b > MAX_ROWS) return (size_t)-1;
     switch (kind) {
         case PAMM_WS_COMPRESS:
@@ -612,6 +915,7 @@ size_t pamm_workspace_bytes(pamm_ws_kind kind, int64_t b, int64_t n, int64_t m, 
         case PAMM_WS_STEP_HOST:
             if (n < 1 || m < 1) return (size_t)-1;
             return step_arena_layout(nullptr, b, n, m, k, dt).bytes;
+        default: break;
     }
     return (size_t)-1;
 }
