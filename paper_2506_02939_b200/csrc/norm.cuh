@@ -6,9 +6,16 @@
 //   u = (h - mu) s;  g = dy w;  dx = s (g - mean(g) - u mean(g u)) (+ dh), without mean(g) in the RMS form
 //   dw = sum over rows of dy u;  dc = sum over rows of dy
 //
-// All of it is bound by memory: about 10 operations an element against 4 to 8 bytes.  The forward pass
-// holds its row in registers, so that x is read once and the variance is taken around the true mean.
+// All of it is bound by memory: about 10 operations an element against 4 to 8 bytes.  A row stays in
+// registers between its one reading and its one writing, and the variance is taken around the true mean.
 // mu and s are those of h before it is rounded to its storage type: y then carries one rounding.
+//
+// A thread holds EPT elements of its row in EPT / V pieces; V is a 16-byte vector or one element:
+//   vectors, whole   every row 16-byte aligned, n a multiple of V
+//   vectors, RAGGED  any n and any alignment that all matrices of the call share row by row: the row's whole vectors
+//                    on the 16-byte grid of memory, and its up to V - 1 elements before and behind them, which the
+//                    row's first 16 threads take one each
+//   elements         matrices whose rows are aligned differently
 #pragma once
 #include "pamm_common.cuh"
 #include "row_io.cuh"
@@ -17,14 +24,40 @@ namespace pamm {
 
 constexpr int64_t NORM_MAX_N = 32768;
 
-// Sum over the block (warps = blockDim.x / 32); `part` has 32 floats and is not used again by the
-// caller before another barrier.  Fixed order: the same sum in every thread, every time.
-__device__ __forceinline__ float block_sum(float x, float* part, int warps) {
-    x = warp_sum(x);
-    if (warps == 1) return x;
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = x;
-    __syncthreads();
-    return warp_sum((threadIdx.x & 31) < warps ? part[threadIdx.x & 31] : 0.f);
+// A row's whole vectors and this thread's element outside them.
+struct RowShape {
+    int lead, whole;        // elements before the first whole vector, and in the whole ones
+    int extra;              // this thread's element outside them (-1: none)
+};
+template <typename T, int V, bool RAGGED>
+__device__ __forceinline__ RowShape row_shape(const T* row, int n, int t) {
+    if constexpr (!RAGGED) {
+        return {0, n, -1};
+    } else {
+        const int lead = min(n, (int)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / (int)sizeof(T));
+        const int whole = (n - lead) / V * V, behind = lead + whole + t - 8;
+        return {lead, whole, t < lead ? t : t >= 8 && t < 16 && behind < n ? behind : -1};
+    }
+}
+
+// The row's pieces: PIECES vectors (or elements) at distance `step` from `at`; zero at and beyond `end`.
+template <typename T, int V, int PIECES>
+__device__ __forceinline__ void load_row(const T* p, int at, int step, int end, typename Piece<T, V>::Raw (&raw)[PIECES]) {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        if (at + i * step < end) raw[i] = Piece<T, V>::load(p + at + i * step);
+        else raw[i] = Piece<T, V>::zero();
+    }
+}
+// V weights from `w` on, which the row's offset may have moved off the 16-byte grid (`vec`: not).
+template <typename W, int V, bool RAGGED>
+__device__ __forceinline__ void load_row_weights(const W* w, bool vec, float* out) {
+    if (!RAGGED || vec) {
+        load_weights<W, V>(w, out);
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) out[e] = to_float(w[e]);
+    }
 }
 
 struct NormForwardArgs {
@@ -32,73 +65,135 @@ struct NormForwardArgs {
     void *y, *h;
     float *mean, *rstd;
     int64_t ldx, ldr, ldy, ldh, b;
-    int n, warps;           // warps of the block that share a row; 1: every warp of the block has a row
+    int n, warps;           // warps of the block that share a row; 1: LANES lanes have a row
     float eps;
-    bool rms, w_bf16, w_vec;
+    bool rms;
 };
 
-// EPT elements of a row per thread, in EPT / V pieces of V that lie 32 * warps * V apart.
-template <typename T, int V, int EPT>
+// Sum over the warps of a row (all of the block's); every thread gets it.  `part`: 32 floats that the caller
+// does not use again before another barrier.
+template <int LANES>
+__device__ __forceinline__ float row_sum(float x, float* part, int warps) {
+    x = warp_sum<LANES>(x);
+    if (LANES < 32 || warps == 1) return x;
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = x;
+    __syncthreads();
+    return warp_sum((threadIdx.x & 31) < warps ? part[threadIdx.x & 31] : 0.f);
+}
+
+// Measured on 65536 x 2048 bf16 (268 MB a matrix): the 16-byte copy of the same streams in one-shot blocks runs at 6.5 to
+// 6.7 TB/s, in persistent ones at 6.0, hence one block (or a part of one) per row and no loop over rows.  With 32
+// elements a thread the issue slots are a third used; 8 elements a thread repeat the row's overhead in four times the
+// threads and are for calls with few rows only, where the time is one row's latency.
+template <typename T, typename W, int V, int EPT, int LANES, bool RAGGED>
 __global__ void __launch_bounds__(1024)
-norm_forward_kernel(const NormForwardArgs a) {
+norm_forward_kernel(const __grid_constant__ NormForwardArgs a) {
+    using P = Piece<T, V>;
+    constexpr int PIECES = EPT / V;
     __shared__ float s_sum[32], s_sq[32];
     grid_dependency_wait();
     grid_launch_dependents();
-    constexpr int P = EPT / V;
-    const int lane_threads = 32 * a.warps;
-    const int t = a.warps == 1 ? threadIdx.x & 31 : threadIdx.x;
-    const int64_t row = a.warps == 1 ? (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : blockIdx.x;
-    if (row >= a.b) return;          // whole warps, and whole blocks where a row has more than one warp
-    const T* x = static_cast<const T*>(a.x) + row * a.ldx;
-    const T* r = a.r ? static_cast<const T*>(a.r) + row * a.ldr : nullptr;
-    float h[P][V];
+    const bool one = a.warps == 1;
+    const int step = (LANES < 32 ? LANES : 32 * a.warps) * V;
+    const int at = (LANES < 32 ? threadIdx.x & (LANES - 1) : one ? threadIdx.x & 31 : threadIdx.x) * V;
+    const int64_t row = one ? (int64_t)blockIdx.x * (blockDim.x / LANES) + threadIdx.x / LANES : blockIdx.x;
+    // the lanes behind the last row go along with it, so that shuffles have all of their warp, and write nothing
+    const bool mine = row < a.b;
+    const int64_t i = mine ? row : a.b - 1;
+    const T* x = static_cast<const T*>(a.x) + i * a.ldx;
+    const RowShape shape = row_shape<T, V, RAGGED>(x, a.n, at / V);
+    const int lead = shape.lead, end = shape.whole, extra = shape.extra;
+    typename P::Raw xr[PIECES];
+    load_row<T, V, PIECES>(x + lead, at, step, end, xr);
+    float h[EPT], hx = 0.f;
+    if (RAGGED && extra >= 0) hx = to_float(x[extra]);
+    if (a.r) {
+        const T* r = static_cast<const T*>(a.r) + i * a.ldr;
+        typename P::Raw rr[PIECES];
+        load_row<T, V, PIECES>(r + lead, at, step, end, rr);
+        if (RAGGED && extra >= 0) hx += to_float(r[extra]);
 #pragma unroll
-    for (int p = 0; p < P; ++p) RowIo<T, V>::load(x, (t + p * lane_threads) * V, a.n, h[p]);
-    if (r) {
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
+        for (int p = 0; p < PIECES; ++p) {
             float q[V];
-            RowIo<T, V>::load(r, (t + p * lane_threads) * V, a.n, q);
+            P::unpack(xr[p], h + p * V);
+            P::unpack(rr[p], q);
 #pragma unroll
-            for (int e = 0; e < V; ++e) h[p][e] += q[e];
+            for (int e = 0; e < V; ++e) h[p * V + e] += q[e];
         }
+    } else {
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) P::unpack(xr[p], h + p * V);
+    }
+    if (a.h && mine) {
+        T* ho = static_cast<T*>(a.h) + i * a.ldh;
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p)
+            if (at + p * step < end) P::store(ho + lead + at + p * step, h + p * V);
+        if (RAGGED && extra >= 0) ho[extra] = from_float<T>(hx);
     }
     const float inv_n = 1.f / (float)a.n;
     float mean = 0.f;
     if (!a.rms) {
-        float sum = 0.f;
+        float2 sum = make_float2(hx, 0.f);
 #pragma unroll
-        for (int p = 0; p < P; ++p)
+        for (int e = 0; e < EPT; e += 2) sum = add2(sum, make_float2(h[e], h[e + 1]));
+        mean = row_sum<LANES>(sum.x + sum.y, s_sum, a.warps) * inv_n;
+        const float2 minus = twice(-mean);
 #pragma unroll
-            for (int e = 0; e < V; ++e) sum += h[p][e];
-        mean = block_sum(sum, s_sum, a.warps) * inv_n;
-    }
-    float sq = 0.f;
+        for (int p = 0; p < PIECES; ++p) {
+            if (at + p * step < end) {          // what lies outside the row stays 0
+                if constexpr (V == 1) {
+                    h[p] -= mean;
+                } else {
 #pragma unroll
-    for (int p = 0; p < P; ++p)
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            const float d = (t + p * lane_threads) * V + e < a.n ? h[p][e] - mean : 0.f;
-            sq = fmaf(d, d, sq);
+                    for (int e = p * V; e < p * V + V; e += 2) {
+                        const float2 d = add2(make_float2(h[e], h[e + 1]), minus);
+                        h[e] = d.x; h[e + 1] = d.y;
+                    }
+                }
+            }
         }
-    const float rstd = 1.f / sqrtf(block_sum(sq, s_sq, a.warps) * inv_n + a.eps);
-    if (t == 0) {
-        if (a.mean) a.mean[row] = mean;
-        if (a.rstd) a.rstd[row] = rstd;
+        if (extra >= 0) hx -= mean;
     }
-    T* y = static_cast<T*>(a.y) + row * a.ldy;
-    T* ho = a.h ? static_cast<T*>(a.h) + row * a.ldh : nullptr;
+    float2 sq = make_float2(hx * hx, 0.f);
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-        const int col = (t + p * lane_threads) * V;
-        if (col >= a.n) continue;
-        if (ho) RowIo<T, V>::store(ho, col, a.n, h[p]);
-        float w[V], c[V];
-        load_weights<V>(a.w, a.w_bf16, a.w_vec, col, a.n, 1.f, w);
-        load_weights<V>(a.c, a.w_bf16, a.w_vec, col, a.n, 0.f, c);
+    for (int e = 0; e < EPT; e += 2) sq = fma2(make_float2(h[e], h[e + 1]), make_float2(h[e], h[e + 1]), sq);
+    const float rstd = rsqrtf(row_sum<LANES>(sq.x + sq.y, s_sq, a.warps) * inv_n + a.eps);
+    if (!mine) return;
+    if (at == 0) {
+        if (a.mean) a.mean[i] = mean;
+        if (a.rstd) a.rstd[i] = rstd;
+    }
+    T* y = static_cast<T*>(a.y) + i * a.ldy;
+    const W *w = static_cast<const W*>(a.w), *c = static_cast<const W*>(a.c);
+    if (RAGGED && extra >= 0)
+        y[extra] = from_float<T>(fmaf(hx * rstd, w ? to_float(w[extra]) : 1.f, c ? to_float(c[extra]) : 0.f));
+    const bool w_vec = (reinterpret_cast<uintptr_t>(w + lead) & 15) == 0, c_vec = (reinterpret_cast<uintptr_t>(c + lead) & 15) == 0;
 #pragma unroll
-        for (int e = 0; e < V; ++e) w[e] = fmaf((h[p][e] - mean) * rstd, w[e], c[e]);
-        RowIo<T, V>::store(y, col, a.n, w);
+    for (int p = 0; p < PIECES; ++p) {
+        const int col = lead + at + p * step;
+        if (at + p * step >= end) continue;
+        float q[V], k[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) q[e] = 1.f;
+        if (w) load_row_weights<W, V, RAGGED>(w + col, w_vec, q);
+        if (c) {
+            load_row_weights<W, V, RAGGED>(c + col, c_vec, k);
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) k[e] = 0.f;
+        }
+        if constexpr (V == 1) {
+            q[0] = fmaf(h[p] * rstd, q[0], k[0]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; e += 2) {
+                const float2 u = mul2(make_float2(h[p * V + e], h[p * V + e + 1]), twice(rstd));
+                const float2 v = fma2(u, make_float2(q[e], q[e + 1]), make_float2(k[e], k[e + 1]));
+                q[e] = v.x; q[e + 1] = v.y;
+            }
+        }
+        P::store(y + col, q);
     }
 }
 
@@ -108,16 +203,277 @@ struct NormBackwardArgs {
     void *dx, *dw, *dc;
     float *part;            // [splits][2][n]: partial sums of dw and dc
     int64_t lddy, ldx, lddh, lddx, b, rows_per_split;
-    int n, splits;
-    bool rms, w_bf16, w_vec, dw_bf16;
+    int n, splits, warps, groups, period;
+    bool rms, w_bf16, dw_bf16;
 };
+
+// V weights (1 where there are none) of either type.
+template <int V, bool RAGGED>
+__device__ __forceinline__ void load_any_weights(const void* w, bool is_bf16, int col, float* out) {
+    if (!w) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) out[e] = 1.f;
+    } else if (is_bf16) {
+        const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(w) + col;
+        load_row_weights<__nv_bfloat16, V, RAGGED>(p, (reinterpret_cast<uintptr_t>(p) & 15) == 0, out);
+    } else {
+        const float* p = static_cast<const float*>(w) + col;
+        load_row_weights<float, V, RAGGED>(p, (reinterpret_cast<uintptr_t>(p) & 15) == 0, out);
+    }
+}
+
+__device__ __forceinline__ void copy16_async(uint32_t smem, const void* p) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(p) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ uint4 load_shared16(uint32_t smem) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(smem) : "memory");
+    return v;
+}
+
+constexpr int NB_MAX_GROUPS = 8;
+// Rows in shared memory: four of at most 32 bytes a thread and matrix (98 KB for three matrices and 256 threads, two blocks an
+// SM), two where the rows are wider.
+template <typename T, int EPT> __host__ __device__ constexpr int norm_stages() { return EPT * (int)sizeof(T) > 32 ? 2 : 4; }
+
+// dx and the partial sums of dw (and, SHIFT, of dc) in one pass.  A block has `groups` groups of `warps` warps; a group takes
+// row after row, so that a thread's columns stay the same and their sums stay in its registers.  The rows that follow are
+// copied ahead into shared memory, STAGES - 1 of them: every thread fetches what it will read itself, so that no barrier is
+// needed for it (elements, V = 1, are loaded when they are needed).  Rows whose offset into the 16-byte grid differs go to
+// different blocks (`period` of them: the row distance's phase repeats after so many rows), which keeps the columns of
+// a thread fixed there too.
+// SHIFT: layer norm, or a bias in the RMS form; otherwise there is neither a mean nor dc.
+template <typename T, int V, int EPT, bool SHIFT, bool RAGGED>
+__global__ void __launch_bounds__(512)
+norm_backward_kernel(const __grid_constant__ NormBackwardArgs a) {
+    using P = Piece<T, V>;
+    constexpr int PIECES = EPT / V, STAGES = norm_stages<T, EPT>();
+    __shared__ float2 s_part[2][NB_MAX_GROUPS][16];
+    extern __shared__ __align__(16) unsigned char s_ring[];       // [stage][array][piece][thread] 16 bytes; in the end [2][n] sums
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int group = threadIdx.x / (32 * a.warps), t = threadIdx.x - group * 32 * a.warps;
+    const int step = 32 * a.warps * V, at = t * V, lane = threadIdx.x & 31, warp = t >> 5;
+    const int64_t cls = blockIdx.x % a.period;
+    const int64_t stride = (int64_t)a.period * a.groups * (gridDim.x / a.period);
+    const int64_t first = cls + a.period * ((int64_t)(blockIdx.x / a.period) * a.groups);      // of the block
+    const T *X = static_cast<const T*>(a.x), *DY = static_cast<const T*>(a.dy), *DH = static_cast<const T*>(a.dh);
+    const RowShape shape = row_shape<T, V, RAGGED>(X + cls * a.ldx, a.n, t);
+    const int lead = shape.lead, end = shape.whole, extra = shape.extra;
+    const float inv_n = 1.f / (float)a.n;
+    float w[EPT], dw[EPT], dc[SHIFT ? EPT : 1];
+    float wx = 0.f, dwx = 0.f, dcx = 0.f;
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) w[p * V + e] = 0.f;
+        if (at + p * step < end) load_any_weights<V, RAGGED>(a.w, a.w_bf16, lead + at + p * step, w + p * V);
+    }
+    if (RAGGED && extra >= 0) load_any_weights<1, false>(a.w, a.w_bf16, extra, &wx);
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) dw[e] = 0.f;
+#pragma unroll
+    for (int e = 0; e < (SHIFT ? EPT : 1); ++e) dc[e] = 0.f;
+
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_ring) + threadIdx.x * 16;
+    const uint32_t piece_bytes = blockDim.x * 16, array_bytes = PIECES * piece_bytes, stage_bytes = (DH ? 3 : 2) * array_bytes;
+    auto fetch = [&](int64_t r, int stage) {
+        if constexpr (V > 1) {
+            if (r < a.b) {
+                const uint32_t to = ring + stage * stage_bytes;
+                const T *x = X + r * a.ldx + lead + at, *dy = DY + r * a.lddy + lead + at, *dh = DH + r * a.lddh + lead + at;
+#pragma unroll
+                for (int p = 0; p < PIECES; ++p) {
+                    if (at + p * step < end) {
+                        copy16_async(to + p * piece_bytes, x + p * step);
+                        copy16_async(to + array_bytes + p * piece_bytes, dy + p * step);
+                        if (DH) copy16_async(to + 2 * array_bytes + p * piece_bytes, dh + p * step);
+                    }
+                }
+            }
+            copy_commit();
+        }
+    };
+    auto taken = [&](int stage, int array, int p) {
+        typename P::Raw r = P::zero();
+        if constexpr (V > 1) {
+            if (at + p * step < end) {
+                const uint4 v = load_shared16(ring + stage * stage_bytes + array * array_bytes + p * piece_bytes);
+                r.w[0] = v.x; r.w[1] = v.y; r.w[2] = v.z; r.w[3] = v.w;
+            }
+        }
+        return r;
+    };
+    // statistics and the element outside the vectors: one row ahead, in registers
+    float next_mean = 0.f, next_rstd = 0.f, next_x = 0.f, next_y = 0.f, next_h = 0.f;
+    auto fetch_scalars = [&](int64_t r) {
+        if (r >= a.b) return;
+        next_rstd = a.rstd[r];
+        if (SHIFT && !a.rms) next_mean = a.mean[r];
+        if (RAGGED && extra >= 0) {
+            next_x = to_float(X[r * a.ldx + extra]);
+            next_y = to_float(DY[r * a.lddy + extra]);
+            if (DH) next_h = to_float(DH[r * a.lddh + extra]);
+        }
+    };
+    int64_t row = first + a.period * group;
+#pragma unroll
+    for (int k = 0; k < STAGES - 1; ++k) fetch(row + k * stride, k);
+    fetch_scalars(row);
+    int stage = 0, parity = 0;
+    for (; row < a.b; row += stride, parity ^= 1) {        // a group's threads go the same rounds
+        const float s = next_rstd, m = next_mean, yx = next_y, hx = next_h;
+        float ux = next_x;
+        float u[EPT], g[EPT];
+        if constexpr (V > 1) {
+            copy_wait<STAGES - 2>();
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) {
+                P::unpack(taken(stage, 0, p), u + p * V);
+                P::unpack(taken(stage, 1, p), g + p * V);
+            }
+        } else {
+            typename P::Raw raw[PIECES];
+            load_row<T, V, PIECES>(X + row * a.ldx, at, step, end, raw);
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) P::unpack(raw[p], u + p);
+            load_row<T, V, PIECES>(DY + row * a.lddy, at, step, end, raw);
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) P::unpack(raw[p], g + p);
+        }
+        // the stage that the last round read is free
+        fetch(row + (STAGES - 1) * stride, stage == 0 ? STAGES - 1 : stage - 1);
+        fetch_scalars(row + stride);
+        float2 gu2 = twice(0.f), g2 = twice(0.f);
+#pragma unroll
+        for (int e = 0; e < EPT; e += 2) {
+            float2 uu = make_float2(u[e], u[e + 1]);
+            const float2 dd = make_float2(g[e], g[e + 1]);
+            if (SHIFT) uu = add2(uu, twice(-m));
+            uu = mul2(uu, twice(s));
+            const float2 ww = fma2(dd, uu, make_float2(dw[e], dw[e + 1]));
+            dw[e] = ww.x; dw[e + 1] = ww.y;
+            if (SHIFT) {
+                const float2 cc = add2(dd, make_float2(dc[e], dc[e + 1]));
+                dc[e] = cc.x; dc[e + 1] = cc.y;
+            }
+            const float2 gg = mul2(dd, make_float2(w[e], w[e + 1]));
+            gu2 = fma2(gg, uu, gu2);
+            if (SHIFT) g2 = add2(g2, gg);
+            u[e] = uu.x; u[e + 1] = uu.y; g[e] = gg.x; g[e + 1] = gg.y;
+        }
+        float gu = gu2.x + gu2.y, gs = g2.x + g2.y, gx = 0.f;
+        if (RAGGED && extra >= 0) {
+            ux = (ux - m) * s;
+            dwx = fmaf(yx, ux, dwx);
+            dcx += yx;
+            gx = yx * wx;
+            gu = fmaf(gx, ux, gu);
+            gs += gx;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            gu += __shfl_xor_sync(0xffffffffu, gu, o);
+            if (SHIFT) gs += __shfl_xor_sync(0xffffffffu, gs, o);
+        }
+        if (a.warps > 1) {          // at most 16; two buffers, so that one barrier a row is enough
+            if (lane == 0) s_part[parity][group][warp] = make_float2(gu, gs);
+            asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(32 * a.warps) : "memory");
+            const float2 v = (lane & 15) < a.warps ? s_part[parity][group][lane & 15] : twice(0.f);
+            gu = v.x; gs = v.y;
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) {
+                gu += __shfl_xor_sync(0xffffffffu, gu, o);
+                if (SHIFT) gs += __shfl_xor_sync(0xffffffffu, gs, o);
+            }
+        }
+        const float mu = -gu * inv_n, mg = SHIFT && !a.rms ? -gs * inv_n : 0.f;
+        T* dx = static_cast<T*>(a.dx) + row * a.lddx;
+        typename P::Raw hr[PIECES];
+        if constexpr (V == 1) {
+            if (DH) load_row<T, V, PIECES>(DH + row * a.lddh, at, step, end, hr);
+        }
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) {
+            if (at + p * step >= end) continue;
+            float q[V], hv[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) hv[e] = 0.f;
+            if (DH) {
+                if constexpr (V > 1) P::unpack(taken(stage, 2, p), hv);
+                else P::unpack(hr[p], hv);
+            }
+            if constexpr (V == 1) {
+                q[0] = fmaf(fmaf(u[p], mu, g[p] + mg), s, hv[0]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < V; e += 2) {
+                    const int j = p * V + e;
+                    float2 gg = make_float2(g[j], g[j + 1]);
+                    if (SHIFT) gg = add2(gg, twice(mg));
+                    const float2 d = fma2(fma2(make_float2(u[j], u[j + 1]), twice(mu), gg), twice(s), make_float2(hv[e], hv[e + 1]));
+                    q[e] = d.x; q[e + 1] = d.y;
+                }
+            }
+            P::store(dx + lead + at + p * step, q);
+        }
+        if (RAGGED && extra >= 0) dx[extra] = from_float<T>(fmaf(fmaf(ux, mu, gx + mg), s, hx));
+        stage = stage == STAGES - 1 ? 0 : stage + 1;
+    }
+    if (!a.part) return;
+    float* part = a.part + (int64_t)blockIdx.x * 2 * a.n;
+    if (a.groups == 1) {
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) {
+            if (at + p * step >= end) continue;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const int col = lead + at + p * step + e;
+                part[col] = dw[p * V + e];
+                if (SHIFT) part[a.n + col] = dc[p * V + e];
+            }
+        }
+        if (RAGGED && extra >= 0) {
+            part[extra] = dwx;
+            if (SHIFT) part[a.n + extra] = dcx;
+        }
+        return;
+    }
+    // the groups' sums one after the other, in the place of the ring, whose last copies (of no row) are through
+    float* cols = reinterpret_cast<float*>(s_ring);
+    copy_wait<0>();
+    __syncthreads();
+    for (int k = 0; k < a.groups; ++k) {
+        if (k == group) {
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) {
+                if (at + p * step >= end) continue;
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const int col = lead + at + p * step + e;
+                    cols[col] = dw[p * V + e] + (k ? cols[col] : 0.f);
+                    if (SHIFT) cols[a.n + col] = dc[p * V + e] + (k ? cols[a.n + col] : 0.f);
+                }
+            }
+            if (RAGGED && extra >= 0) {
+                cols[extra] = dwx + (k ? cols[extra] : 0.f);
+                if (SHIFT) cols[a.n + extra] = dcx + (k ? cols[a.n + extra] : 0.f);
+            }
+        }
+        __syncthreads();
+    }
+    for (int i = threadIdx.x; i < (SHIFT ? 2 : 1) * a.n; i += blockDim.x) part[i] = cols[i];
+}
 
 constexpr int NB_WIDE_THREADS = 256;
 
 // One row per block, read twice (the second time from the caches): the two sums, then dx.
 template <typename T, int V>
 __global__ void __launch_bounds__(NB_WIDE_THREADS)
-norm_backward_row_kernel(const NormBackwardArgs a) {
+norm_backward_row_kernel(const __grid_constant__ NormBackwardArgs a) {
+    using P = Piece<T, V>;
     __shared__ float s_gu[32], s_g[32];
     grid_dependency_wait();
     grid_launch_dependents();
@@ -128,9 +484,9 @@ norm_backward_row_kernel(const NormBackwardArgs a) {
     float gu = 0.f, g = 0.f;
     for (int col = threadIdx.x * V; col < a.n; col += NB_WIDE_THREADS * V) {
         float xv[V], dv[V], w[V];
-        RowIo<T, V>::load(x, col, a.n, xv);
-        RowIo<T, V>::load(dy, col, a.n, dv);
-        load_weights<V>(a.w, a.w_bf16, a.w_vec, col, a.n, 1.f, w);
+        P::unpack(P::load(x + col), xv);
+        P::unpack(P::load(dy + col), dv);
+        load_any_weights<V, false>(a.w, a.w_bf16, col, w);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             const float q = dv[e] * w[e];
@@ -139,20 +495,20 @@ norm_backward_row_kernel(const NormBackwardArgs a) {
         }
     }
     const float inv_n = 1.f / (float)a.n;
-    gu = block_sum(gu, s_gu, NB_WIDE_THREADS / 32) * inv_n;
-    g = a.rms ? 0.f : block_sum(g, s_g, NB_WIDE_THREADS / 32) * inv_n;
+    gu = row_sum<32>(gu, s_gu, NB_WIDE_THREADS / 32) * inv_n;
+    g = a.rms ? 0.f : row_sum<32>(g, s_g, NB_WIDE_THREADS / 32) * inv_n;
     T* dx = static_cast<T*>(a.dx) + row * a.lddx;
     const T* dh = a.dh ? static_cast<const T*>(a.dh) + row * a.lddh : nullptr;
     for (int col = threadIdx.x * V; col < a.n; col += NB_WIDE_THREADS * V) {
         float xv[V], dv[V], w[V], hv[V] = {};
-        RowIo<T, V>::load(x, col, a.n, xv);
-        RowIo<T, V>::load(dy, col, a.n, dv);
-        load_weights<V>(a.w, a.w_bf16, a.w_vec, col, a.n, 1.f, w);
-        if (dh) RowIo<T, V>::load(dh, col, a.n, hv);
+        P::unpack(P::load(x + col), xv);
+        P::unpack(P::load(dy + col), dv);
+        load_any_weights<V, false>(a.w, a.w_bf16, col, w);
+        if (dh) P::unpack(P::load(dh + col), hv);
 #pragma unroll
         for (int e = 0; e < V; ++e)
             dv[e] = fmaf(rstd, dv[e] * w[e] - g - (xv[e] - mean) * rstd * gu, hv[e]);
-        RowIo<T, V>::store(dx, col, a.n, dv);
+        P::store(dx + col, dv);
     }
 }
 
@@ -160,7 +516,7 @@ norm_backward_row_kernel(const NormBackwardArgs a) {
 constexpr int NB_COL_THREADS = 128;
 template <typename T>
 __global__ void __launch_bounds__(NB_COL_THREADS)
-norm_backward_columns_kernel(const NormBackwardArgs a) {
+norm_backward_columns_kernel(const __grid_constant__ NormBackwardArgs a) {
     grid_dependency_wait();
     grid_launch_dependents();
     const int col = blockIdx.x * NB_COL_THREADS + threadIdx.x;
@@ -180,27 +536,33 @@ norm_backward_columns_kernel(const NormBackwardArgs a) {
     part[a.n] = dc;
 }
 
-// The partial sums of all ranges, added in their order.
-__global__ void __launch_bounds__(NB_COL_THREADS)
-norm_backward_finish_kernel(const NormBackwardArgs a) {
+// The partial sums of all ranges, added in a fixed order: 32 columns a block, 32 strands of the ranges.
+__global__ void __launch_bounds__(1024)
+norm_backward_finish_kernel(const __grid_constant__ NormBackwardArgs a) {
+    __shared__ float s_part[2][32][33];
     grid_dependency_wait();
     grid_launch_dependents();
-    const int col = blockIdx.x * NB_COL_THREADS + threadIdx.x;
-    if (col >= a.n) return;
+    const int lane = threadIdx.x & 31, strand = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
     float dw = 0.f, dc = 0.f;
-    for (int s = 0; s < a.splits; ++s) {
-        const float* part = a.part + (int64_t)s * 2 * a.n + col;
-        dw += part[0];
-        dc += part[a.n];
+    if (col < a.n) {
+        for (int s = strand; s < a.splits; s += 32) {
+            const float* part = a.part + (int64_t)s * 2 * a.n + col;
+            dw += part[0];
+            if (a.dc) dc += part[a.n];
+        }
     }
-    if (a.dw) {
-        if (a.dw_bf16) static_cast<__nv_bfloat16*>(a.dw)[col] = __float2bfloat16_rn(dw);
-        else static_cast<float*>(a.dw)[col] = dw;
-    }
-    if (a.dc) {
-        if (a.dw_bf16) static_cast<__nv_bfloat16*>(a.dc)[col] = __float2bfloat16_rn(dc);
-        else static_cast<float*>(a.dc)[col] = dc;
-    }
+    s_part[0][strand][lane] = dw;
+    s_part[1][strand][lane] = dc;
+    __syncthreads();
+    if (strand > 1) return;
+    // the first warp finishes dw, the second dc
+    void* out = strand == 0 ? a.dw : a.dc;
+    if (!out || col >= a.n) return;
+    float sum = 0.f;
+#pragma unroll
+    for (int s = 0; s < 32; ++s) sum += s_part[strand][s][lane];
+    if (a.dw_bf16) static_cast<__nv_bfloat16*>(out)[col] = __float2bfloat16_rn(sum);
+    else static_cast<float*>(out)[col] = sum;
 }
 
 }  // namespace pamm

@@ -548,37 +548,102 @@ namespace {
 
 // Row partition of the norm's column sums, and the scratch that holds their partial sums.
 inline int64_t norm_splits(int64_t b) { return std::max<int64_t>(1, std::min<int64_t>((b + 31) / 32, 2 * sm_count())); }
-inline size_t norm_backward_ws_bytes(int64_t b, int64_t n) { return (size_t)round_up(norm_splits(b) * 2 * n * 4, 256); }
+inline size_t norm_backward_ws_bytes(int64_t b, int64_t n) {
+    return (size_t)round_up(std::min<int64_t>(b + 8, 2 * sm_count()) * 2 * n * 4, 256);
+}
 inline int grad_norm_blocks() { return sm_count() * GC_BLOCKS_PER_SM; }
 inline size_t grad_norm_ws_bytes() { return (size_t)round_up((int64_t)grad_norm_blocks() * 8, 256); }
 
 // An element-aligned row-major matrix of at least one row; leading dimension in elements.
 inline bool matrix_ok(const void* p, int64_t ld, int64_t cols, size_t es) { return p && aligned(p, es) && ld >= cols; }
-// Whether every row of the matrix starts on a 16-byte boundary (null: no matrix, no restriction).
-inline bool rows_aligned(const void* p, int64_t ld, size_t es) { return !p || (aligned(p, 16) && (ld * (int64_t)es) % 16 == 0); }
 
-template <typename T, int V>
+// How the matrices of a call can be accessed (the three ways are described in norm.cuh).
+enum class RowAccess { whole, ragged, elements };
+struct RowMatrix { const void* p; int64_t ld; };
+template <int N>
+RowAccess row_access(const RowMatrix (&m)[N], int64_t n, size_t es, bool weights_aligned) {
+    const auto phase = [&](int i) { return reinterpret_cast<uintptr_t>(m[i].p) % 16; };
+    const auto turn = [&](int i) { return (m[i].ld * (int64_t)es) % 16; };
+    bool same = true, zero = phase(0) == 0 && turn(0) == 0;
+    for (int i = 1; i < N; ++i) same = same && (!m[i].p || (phase(i) == phase(0) && turn(i) == turn(0)));
+    if (same && zero && (n * es) % 16 == 0 && weights_aligned) return RowAccess::whole;
+    return same ? RowAccess::ragged : RowAccess::elements;
+}
+
+// Elements a thread: few while the rows do not fill the device (a row's latency is what counts), else 32.  Both sides
+// measured: 65536 x 2048 bf16 takes 83 us with 32 and 110 us with 8.
+template <typename T, typename W, int V, bool RAGGED>
 pamm_status launch_norm_forward(NormForwardArgs a, cudaStream_t st) {
-    const int ept = a.n <= 256 ? 8 : a.n <= 16384 ? 16 : 32;
-    a.warps = (int)((a.n + 32 * ept - 1) / (32 * ept));
-    const int threads = a.warps == 1 ? 256 : 32 * a.warps;
-    const int64_t rows_per_block = a.warps == 1 ? 8 : 1;
+    const int n = a.n;
+    const int64_t thin_warps = (n + 255) / 256;               // of a row at 8 elements a thread
+    const int ept = thin_warps <= 32 && (thin_warps == 1 || a.b * thin_warps <= 8 * sm_count()) ? 8 : n <= 512 || (V == 1 && n <= 16384) ? 16 : 32;
+    a.warps = (n + 32 * ept - 1) / (32 * ept);
+    const int lanes = ept > 8 || n > 128 ? 32 : n > 64 || RAGGED ? 16 : 8;      // a ragged row needs 16 for its ends
+    const int threads = a.warps > 1 ? 32 * a.warps : a.b * lanes >= 256 ? 256 : (int)round_up(a.b * lanes, 32);
+    const int64_t rows_per_block = a.warps > 1 ? 1 : threads / lanes;
     const dim3 grid((unsigned)((a.b + rows_per_block - 1) / rows_per_block));
-    if (ept == 8) launch(norm_forward_kernel<T, V, 8>, grid, dim3(threads), 0, st, true, a);
-    else if (ept == 16) launch(norm_forward_kernel<T, V, 16>, grid, dim3(threads), 0, st, true, a);
-    else launch(norm_forward_kernel<T, V, 32>, grid, dim3(threads), 0, st, true, a);
+    if (lanes == 8) launch(norm_forward_kernel<T, W, V, 8, RAGGED ? 16 : 8, RAGGED>, grid, dim3(threads), 0, st, true, a);
+    else if (lanes == 16) launch(norm_forward_kernel<T, W, V, 8, 16, RAGGED>, grid, dim3(threads), 0, st, true, a);
+    else if (ept == 8) launch(norm_forward_kernel<T, W, V, 8, 32, RAGGED>, grid, dim3(threads), 0, st, true, a);
+    else if (ept == 16) launch(norm_forward_kernel<T, W, V, 16, 32, RAGGED>, grid, dim3(threads), 0, st, true, a);
+    else launch(norm_forward_kernel<T, W, V, 32, 32, RAGGED>, grid, dim3(threads), 0, st, true, a);
+    return launch_status();
+}
+template <typename T, typename W>
+pamm_status launch_norm_forward(const NormForwardArgs& a, RowAccess access, cudaStream_t st) {
+    if (access == RowAccess::whole) return launch_norm_forward<T, W, Vec16<T>::N, false>(a, st);
+    if (access == RowAccess::ragged) return launch_norm_forward<T, W, Vec16<T>::N, true>(a, st);
+    return launch_norm_forward<T, W, 1, false>(a, st);
+}
+
+template <typename T, int V, int EPT, bool RAGGED>
+pamm_status launch_norm_backward_fused(NormBackwardArgs& a, cudaStream_t st) {
+    a.warps = (a.n + 32 * EPT - 1) / (32 * EPT);
+    a.groups = std::max(1, NB_MAX_GROUPS / a.warps);
+    const int64_t turn = (a.ldx * (int64_t)sizeof(T)) % 16;
+    a.period = 1;
+    while (RAGGED && (a.period * turn) % 16 != 0) a.period *= 2;
+    const int threads = 32 * a.warps * a.groups;
+    const size_t ring = V > 1 ? (size_t)norm_stages<T, EPT>() * (a.dh ? 3 : 2) * (EPT / V) * threads * 16 : 0;
+    const size_t smem = std::max(ring, a.groups > 1 ? (size_t)2 * a.n * 4 : 0);
+    const auto kernel = !a.rms || a.dc ? norm_backward_kernel<T, V, EPT, true, RAGGED> : norm_backward_kernel<T, V, EPT, false, RAGGED>;
+    if (!ensure_dynamic_smem((const void*)kernel, smem)) return PAMM_ERR_CUDA;
+    const int64_t want = ((a.b + a.period - 1) / a.period + a.groups - 1) / a.groups;      // blocks of each phase
+    a.splits = (int)(a.period * std::min<int64_t>(want, std::max(1, sm_count() * (threads <= 256 ? 2 : 1) / a.period)));
+    launch(kernel, dim3((unsigned)a.splits), dim3(threads), smem, st, true, a);
     return launch_status();
 }
 
-template <typename T, int V>
-pamm_status launch_norm_backward(NormBackwardArgs a, cudaStream_t st) {
-    // the column sums first: dX may take the place of dY or X
-    if (a.dw || a.dc) {
-        const unsigned blocks = (unsigned)((a.n + NB_COL_THREADS - 1) / NB_COL_THREADS);
-        if (a.b) launch(norm_backward_columns_kernel<T>, dim3(blocks, (unsigned)a.splits), dim3(NB_COL_THREADS), 0, st, true, a);
-        launch(norm_backward_finish_kernel, dim3(blocks), dim3(NB_COL_THREADS), 0, st, true, a);
+template <typename T>
+pamm_status launch_norm_backward(NormBackwardArgs a, RowAccess access, cudaStream_t st) {
+    constexpr int V = Vec16<T>::N;
+    const bool sums = a.dw || a.dc;
+    const dim3 finish_grid((unsigned)((a.n + 31) / 32));
+    // 32 bytes of each matrix a thread, twice that where the row is wider than 16 such warps
+    constexpr int E = 2 * V;
+    const bool fused = access == RowAccess::elements ? a.n <= 512 * E : a.n <= 1024 * E;
+    a.splits = 0;
+    if (fused && a.b) {
+        pamm_status s;
+        if (access == RowAccess::whole)
+            s = a.n <= 512 * E ? launch_norm_backward_fused<T, V, E, false>(a, st) : launch_norm_backward_fused<T, V, 2 * E, false>(a, st);
+        else if (access == RowAccess::ragged)
+            s = a.n <= 512 * E ? launch_norm_backward_fused<T, V, E, true>(a, st) : launch_norm_backward_fused<T, V, 2 * E, true>(a, st);
+        else
+            s = launch_norm_backward_fused<T, 1, E, false>(a, st);
+        if (s != PAMM_OK) return s;
+    } else if (a.b && sums) {
+        // rows too wide for registers: the column sums by themselves, before dX may take the place of dY or X
+        a.rows_per_split = (a.b + norm_splits(a.b) - 1) / norm_splits(a.b);
+        a.splits = (int)((a.b + a.rows_per_split - 1) / a.rows_per_split);
+        launch(norm_backward_columns_kernel<T>, dim3((unsigned)((a.n + NB_COL_THREADS - 1) / NB_COL_THREADS), (unsigned)a.splits),
+               dim3(NB_COL_THREADS), 0, st, true, a);
     }
-    if (a.b) launch(norm_backward_row_kernel<T, V>, dim3((unsigned)a.b), dim3(NB_WIDE_THREADS), 0, st, true, a);
+    if (sums) launch(norm_backward_finish_kernel, finish_grid, dim3(1024), 0, st, true, a);
+    if (a.b && !fused) {
+        if (access == RowAccess::whole) launch(norm_backward_row_kernel<T, V>, dim3((unsigned)a.b), dim3(NB_WIDE_THREADS), 0, st, true, a);
+        else launch(norm_backward_row_kernel<T, 1>, dim3((unsigned)a.b), dim3(NB_WIDE_THREADS), 0, st, true, a);
+    }
     return launch_status();
 }
 
@@ -715,11 +780,13 @@ pamm_status pamm_norm_forward(pamm_norm_kind kind, const void* X, int64_t ldx, c
     a.x = X; a.r = R; a.w = w; a.c = c; a.y = Y; a.h = H; a.mean = mean; a.rstd = rstd;
     a.ldx = ldx; a.ldr = ldr; a.ldy = ldy; a.ldh = ldh; a.b = b;
     a.n = (int)n; a.warps = 0; a.eps = eps;
-    a.rms = kind == PAMM_NORM_RMS; a.w_bf16 = w_dt == PAMM_BF16; a.w_vec = aligned(w, 16) && aligned(c, 16);
-    const bool vec = rows_aligned(X, ldx, es) && rows_aligned(R, ldr, es) && rows_aligned(Y, ldy, es) && rows_aligned(H, ldh, es);
+    a.rms = kind == PAMM_NORM_RMS;
+    const RowMatrix all[] = {{X, ldx}, {R, ldr}, {Y, ldy}, {H, ldh}};
+    const RowAccess access = row_access(all, n, es, aligned(w, 16) && aligned(c, 16));
     cudaStream_t st = (cudaStream_t)stream;
-    if (dt == PAMM_F32) return vec ? launch_norm_forward<float, 4>(a, st) : launch_norm_forward<float, 1>(a, st);
-    return vec ? launch_norm_forward<__nv_bfloat16, 8>(a, st) : launch_norm_forward<__nv_bfloat16, 1>(a, st);
+    using bf16 = __nv_bfloat16;
+    if (dt == PAMM_F32) return w_dt == PAMM_F32 ? launch_norm_forward<float, float>(a, access, st) : launch_norm_forward<float, bf16>(a, access, st);
+    return w_dt == PAMM_F32 ? launch_norm_forward<bf16, float>(a, access, st) : launch_norm_forward<bf16, bf16>(a, access, st);
 }
 
 pamm_status pamm_norm_backward(pamm_norm_kind kind, const void* dY, int64_t lddy, const void* X, int64_t ldx, const float* mean,
@@ -743,16 +810,14 @@ pamm_status pamm_norm_backward(pamm_norm_kind kind, const void* dY, int64_t lddy
     if (b == 0 && !dw && !dc) return PAMM_OK;
     NormBackwardArgs a;
     a.dy = dY; a.x = X; a.w = w; a.dh = dH; a.mean = mean; a.rstd = rstd; a.dx = dX; a.dw = dw; a.dc = dc;
-    a.part = (float*)workspace;
-    a.lddy = lddy; a.ldx = ldx; a.lddh = lddh; a.lddx = lddx; a.b = b;
-    a.n = (int)n;
-    a.rows_per_split = b ? (b + norm_splits(b) - 1) / norm_splits(b) : 1;
-    a.splits = (int)((b + a.rows_per_split - 1) / a.rows_per_split);
-    a.rms = rms; a.w_bf16 = w_dt == PAMM_BF16; a.w_vec = aligned(w, 16); a.dw_bf16 = dw_dt == PAMM_BF16;
-    const bool vec = rows_aligned(dY, lddy, es) && rows_aligned(X, ldx, es) && rows_aligned(dH, lddh, es) && rows_aligned(dX, lddx, es);
+    a.part = dw || dc ? (float*)workspace : nullptr;
+    a.lddy = lddy; a.ldx = ldx; a.lddh = lddh; a.lddx = lddx; a.b = b; a.rows_per_split = 0;
+    a.n = (int)n; a.splits = a.warps = a.groups = a.period = 0;
+    a.rms = rms; a.w_bf16 = w_dt == PAMM_BF16; a.dw_bf16 = dw_dt == PAMM_BF16;
+    const RowMatrix all[] = {{X, ldx}, {dY, lddy}, {dH, lddh}, {dX, lddx}};
+    const RowAccess access = row_access(all, n, es, aligned(w, 16));
     cudaStream_t st = (cudaStream_t)stream;
-    if (dt == PAMM_F32) return vec ? launch_norm_backward<float, 4>(a, st) : launch_norm_backward<float, 1>(a, st);
-    return vec ? launch_norm_backward<__nv_bfloat16, 8>(a, st) : launch_norm_backward<__nv_bfloat16, 1>(a, st);
+    return dt == PAMM_F32 ? launch_norm_backward<float>(a, access, st) : launch_norm_backward<__nv_bfloat16>(a, access, st);
 }
 
 pamm_status pamm_rotary_frequencies_host(int64_t rot_dim, double base, pamm_rotary_scaling scaling, double factor,

@@ -26,6 +26,11 @@ struct RotaryArgs {
     bool adjacent, transposed, pos64, in_place;
 };
 
+template <typename T, int V>
+__device__ __forceinline__ void load_unit(const T* p, float* out) {
+    Piece<T, V>::unpack(Piece<T, V>::load(p), out);
+}
+
 // One pair.  The products' order is written out, so that every access width gives the same bits.
 __device__ __forceinline__ void turn_pair(float& x1, float& x2, float c, float s) {
     const float y1 = fmaf(x1, c, -__fmul_rn(x2, s));
@@ -78,8 +83,8 @@ rotary_kernel(const RotaryArgs a) {
         T* yr = y + (int64_t)head * a.yh;
         if (!turn) {
             float v[V];
-            RowIo<T, V>::load(xr, col, a.head_dim, v);
-            RowIo<T, V>::store(yr, col, a.head_dim, v);
+            load_unit<T, V>(xr + col, v);
+            Piece<T, V>::store(yr + col, v);
             continue;
         }
         if (a.adjacent) {
@@ -89,7 +94,7 @@ rotary_kernel(const RotaryArgs a) {
                 v[0] = to_float(xr[2 * col]);
                 v[1] = to_float(xr[2 * col + 1]);
             } else {
-                RowIo<T, V>::load(xr, col * V, a.rot, v);
+                load_unit<T, V>(xr + col * V, v);
             }
             if (known) {
 #pragma unroll
@@ -103,12 +108,12 @@ rotary_kernel(const RotaryArgs a) {
                 yr[2 * col] = from_float<T>(v[0]);
                 yr[2 * col + 1] = from_float<T>(v[1]);
             } else {
-                RowIo<T, V>::store(yr, col * V, a.rot, v);
+                Piece<T, V>::store(yr + col * V, v);
             }
         } else {
             float v1[V], v2[V];
-            RowIo<T, V>::load(xr, col * V, half, v1);
-            RowIo<T, V>::load(xr + half, col * V, half, v2);
+            load_unit<T, V>(xr + col * V, v1);
+            load_unit<T, V>(xr + half + col * V, v2);
             if (known) {
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
@@ -117,8 +122,8 @@ rotary_kernel(const RotaryArgs a) {
                     turn_pair(v1[e], v2[e], c, sn);
                 }
             }
-            RowIo<T, V>::store(yr, col * V, half, v1);
-            RowIo<T, V>::store(yr + half, col * V, half, v2);
+            Piece<T, V>::store(yr + col * V, v1);
+            Piece<T, V>::store(yr + half + col * V, v2);
         }
     }
 }

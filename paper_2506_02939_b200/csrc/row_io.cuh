@@ -39,81 +39,105 @@ __device__ __forceinline__ uint4 round_vec<__nv_bfloat16>(const float (&x)[8]) {
     return make_uint4(round_bf16x2(x[0], x[1]), round_bf16x2(x[2], x[3]), round_bf16x2(x[4], x[5]), round_bf16x2(x[6], x[7]));
 }
 
-// V consecutive elements of a row of `n`, V = one 16-byte vector (row 16-byte aligned, col a
-// multiple of V) or one element (any alignment of the type).  Elements at or beyond n read as zero
-// and are not written.
+// V consecutive elements of a row as they lie in memory: one 16-byte vector (V = Vec16<T>::N, 16-byte aligned) or one
+// element (V = 1, any alignment of the type).  Loading and unpacking are apart, so that all of a
+// thread's loads are in flight before the first is waited for.
 template <typename T, int V>
-struct RowIo {
+struct Piece {
     static_assert(V == 1 || V == Vec16<T>::N, "one element or 16 bytes");
-    static __device__ __forceinline__ void load(const T* row, int64_t col, int64_t n, float (&out)[V]) {
-        if constexpr (V == 1) {
-            out[0] = col < n ? to_float(row[col]) : 0.f;
-        } else {
-            if (col + V <= n) {
-                unpack_vec<T>(ld16(row + col), out);
-            } else {
+    static constexpr int WORDS = V == 1 ? 1 : 4;
+    struct Raw { uint32_t w[WORDS]; };
+
+    static __device__ __forceinline__ Raw zero() {
+        Raw r;
 #pragma unroll
-                for (int e = 0; e < V; ++e) out[e] = col + e < n ? to_float(row[col + e]) : 0.f;
+        for (int i = 0; i < WORDS; ++i) r.w[i] = 0;
+        return r;
+    }
+    static __device__ __forceinline__ Raw load(const T* p) {
+        Raw r;
+        if constexpr (V == 1) {
+            if constexpr (sizeof(T) == 4) r.w[0] = *reinterpret_cast<const uint32_t*>(p);
+            else r.w[0] = *reinterpret_cast<const unsigned short*>(p);
+        } else {
+            const uint4 v = ld16(p);
+            r.w[0] = v.x; r.w[1] = v.y; r.w[2] = v.z; r.w[3] = v.w;
+        }
+        return r;
+    }
+    static __device__ __forceinline__ void unpack(const Raw& r, float* out) {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) out[e] = __uint_as_float(r.w[e]);
+        } else if constexpr (V == 1) {
+            out[0] = bf16_lo(r.w[0]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                out[2 * i] = bf16_lo(r.w[i]);
+                out[2 * i + 1] = bf16_hi(r.w[i]);
             }
         }
     }
-    static __device__ __forceinline__ void store(T* row, int64_t col, int64_t n, const float (&x)[V]) {
+    static __device__ __forceinline__ void store(T* p, const float* x) {       // rounded to nearest even
         if constexpr (V == 1) {
-            if (col < n) row[col] = from_float<T>(x[0]);
+            *p = from_float<T>(x[0]);
+        } else if constexpr (sizeof(T) == 4) {
+            st16(p, make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])));
         } else {
-            if (col + V <= n) {
-                st16(row + col, round_vec<T>(x));
-            } else {
-#pragma unroll
-                for (int e = 0; e < V; ++e)
-                    if (col + e < n) row[col + e] = from_float<T>(x[e]);
-            }
+            st16(p, make_uint4(round_bf16x2(x[0], x[1]), round_bf16x2(x[2], x[3]), round_bf16x2(x[4], x[5]), round_bf16x2(x[6], x[7])));
         }
     }
 };
 
-// V consecutive entries of a vector of weights (fp32 or bf16, a runtime choice), zero at and beyond
-// n.  A null vector stands for `missing` in every place.  Vector access where the base is 16-byte
-// aligned (`vec`); col is a multiple of V and V at most 8.
-template <int V>
-__device__ __forceinline__ void load_weights(const void* w, bool is_bf16, bool vec, int col, int n, float missing, float (&out)[V]) {
-    if (!w) {
+// V consecutive entries of a vector of weights (V > 1: 16-byte aligned base, col a multiple of V).
+template <typename W, int V>
+__device__ __forceinline__ void load_weights(const W* w, float* out) {
+    if constexpr (V == 1) {
+        out[0] = to_float(*w);
+    } else if constexpr (sizeof(W) == 4) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) out[e] = missing;
-        return;
-    }
-    if (V > 1 && vec && col + V <= n) {
-        if constexpr (V == 8) {
-            if (is_bf16) {
-                unpack_vec<__nv_bfloat16>(__ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(w) + col)), out);
-            } else {
-                const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(w) + col);
-                const float4 a = __ldg(p), b = __ldg(p + 1);
-                out[0] = a.x; out[1] = a.y; out[2] = a.z; out[3] = a.w;
-                out[4] = b.x; out[5] = b.y; out[6] = b.z; out[7] = b.w;
-            }
-        } else if constexpr (V == 4) {
-            if (is_bf16) {
-                const uint2 t = __ldg(reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(w) + col));
-                out[0] = bf16_lo(t.x); out[1] = bf16_hi(t.x); out[2] = bf16_lo(t.y); out[3] = bf16_hi(t.y);
-            } else {
-                const float4 a = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(w) + col));
-                out[0] = a.x; out[1] = a.y; out[2] = a.z; out[3] = a.w;
-            }
+        for (int e = 0; e < V; e += 4) {
+            const float4 t = __ldg(reinterpret_cast<const float4*>(w + e));
+            out[e] = t.x; out[e + 1] = t.y; out[e + 2] = t.z; out[e + 3] = t.w;
         }
-        return;
-    }
+    } else {
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-        const int i = col + e;
-        out[e] = i >= n ? 0.f : is_bf16 ? to_float(static_cast<const __nv_bfloat16*>(w)[i]) : static_cast<const float*>(w)[i];
+        for (int e = 0; e < V; e += 4) {
+            const uint2 t = __ldg(reinterpret_cast<const uint2*>(w + e));
+            out[e] = bf16_lo(t.x); out[e + 1] = bf16_hi(t.x); out[e + 2] = bf16_lo(t.y); out[e + 3] = bf16_hi(t.y);
+        }
     }
 }
 
-__device__ __forceinline__ float warp_sum(float x) {
+// Two fp32 operations in one instruction (each rounded as the single one).
+__device__ __forceinline__ float2 fma2(const float2 a, const float2 b, const float2 c) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+        "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(const float2 a, const float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+        "mul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(const float2 a, const float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+        "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+template <int LANES = 32>
+__device__ __forceinline__ float warp_sum(float x) {       // over LANES neighbouring lanes, the same sum in each
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
+    for (int off = LANES / 2; off > 0; off >>= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
     return x;
 }
+__device__ __forceinline__ float2 twice(float x) { return make_float2(x, x); }
 
 }  // namespace pamm
