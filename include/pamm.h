@@ -444,6 +444,7 @@ pamm_status pamm_rotary_table(const double* freq, int64_t rot_dim, double amplit
  *              the table raises PAMM_ERR_BAD_INDEX in the device status and its token passes through unturned.
  * Y may be X with the same distances: only what is turned is then read and written.  Products and sums are fp32,
  * rounded once to dt.  A zero count of anything is a valid call that does nothing.
+ * Limits: rot_dim <= 512, heads x head_dim <= 2^24, batch x seq < 2^31.
  */
 pamm_status pamm_rotary(const void* X, int64_t x_batch, int64_t x_token, int64_t x_head, void* Y, int64_t y_batch, int64_t y_token,
                         int64_t y_head, int64_t batch, int64_t seq, int64_t heads, int64_t rotated, int64_t head_dim,

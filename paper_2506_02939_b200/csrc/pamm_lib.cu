@@ -647,12 +647,43 @@ pamm_status launch_norm_backward(NormBackwardArgs a, RowAccess access, cudaStrea
     return launch_status();
 }
 
-template <typename T>
-pamm_status launch_rotary(const RotaryArgs& a, int64_t tokens, bool vec, cudaStream_t st) {
-    const dim3 grid((unsigned)tokens), block(ROTARY_THREADS);
-    if (vec) launch(rotary_kernel<T, Vec16<T>::N>, grid, block, 0, st, true, a);
-    else launch(rotary_kernel<T, 1>, grid, block, 0, st, true, a);
+struct RotaryShape { int64_t batch, seq, heads, rotated, head_dim; bool adjacent, in_place; };
+
+template <typename T, int V, bool ADJACENT, int HEADS>
+pamm_status launch_rotary(RotaryArgs a, const RotaryShape& g, cudaStream_t st) {
+    const int per_turn = ADJACENT ? (V == 1 ? 2 : V) : 2 * V;             // elements of a turned unit
+    a.turns = a.rot / per_turn;
+    const int64_t rest = g.in_place ? 0 : (g.head_dim - a.rot) / V, whole = g.in_place ? 0 : g.head_dim / V;
+    a.turned_step = (int)((g.rotated + HEADS - 1) / HEADS);
+    a.whole_step = (int)((g.heads - g.rotated + HEADS - 1) / HEADS);
+    a.turned_units = (int)(a.turned_step * (a.turns + rest));
+    const int64_t units = a.turned_units + a.whole_step * whole;
+    if (units == 0) return PAMM_OK;
+    a.tokens = g.batch * g.seq;
+    a.heads = (int)g.heads; a.rotated = (int)g.rotated;
+    a.seq = make_divisor((uint32_t)g.seq);
+    a.units = make_divisor((uint32_t)units);
+    a.per_turned = make_divisor((uint32_t)(a.turns + rest));
+    a.per_whole = make_divisor((uint32_t)std::max<int64_t>(1, whole));
+    // 128 threads a block or a little less where several tokens of few units share one, at most 256 of a token of many
+    a.tokens_per_block = (int)std::max<int64_t>(1, std::min<int64_t>(128 / units, a.tokens));
+    const int64_t work = a.tokens_per_block * units, parts = (work + 255) / 256;
+    const int threads = (int)round_up((work + parts - 1) / parts, 32);
+    const dim3 grid((unsigned)((a.tokens + a.tokens_per_block - 1) / a.tokens_per_block), (unsigned)parts);
+    launch(rotary_kernel<T, V, ADJACENT, HEADS>, grid, dim3(threads), 0, st, true, a);
     return launch_status();
+}
+template <typename T, int V>
+pamm_status launch_rotary(const RotaryArgs& a, const RotaryShape& g, cudaStream_t st) {
+    return g.adjacent ? launch_rotary<T, V, true, 8>(a, g, st) : launch_rotary<T, V, false, 4>(a, g, st);
+}
+// `width`: the elements, a power of two, that everything the call touches is a multiple of and aligned to
+template <typename T>
+pamm_status launch_rotary(const RotaryArgs& a, const RotaryShape& g, int width, cudaStream_t st) {
+    if constexpr (sizeof(T) == 2)
+        if (width >= 8) return launch_rotary<T, 8>(a, g, st);
+    if (width >= 4) return launch_rotary<T, 4>(a, g, st);
+    return width >= 2 ? launch_rotary<T, 2>(a, g, st) : launch_rotary<T, 1>(a, g, st);
 }
 
 // A launch whose parameters are too large to be copied from call to call.
@@ -867,7 +898,7 @@ pamm_status pamm_rotary(const void* X, int64_t x_batch, int64_t x_token, int64_t
     if (batch < 0 || seq < 0 || heads < 0 || rotated < 0 || rotated > heads || head_dim < 1 || rot_dim < 2 || rot_dim % 2 ||
         rot_dim > head_dim)
         return PAMM_ERR_INVALID_ARG;
-    if (rot_dim > ROTARY_MAX_ROT || seq > MAX_ROWS || heads * head_dim > (1ll << 30) || heads > (1ll << 30) || head_dim > (1ll << 20) ||
+    if (rot_dim > ROTARY_MAX_ROT || seq > MAX_ROWS || heads > ROTARY_MAX_ROW || head_dim > ROTARY_MAX_ROW || heads * head_dim > ROTARY_MAX_ROW ||
         (seq > 0 && batch > MAX_ROWS / seq))
         return PAMM_ERR_UNSUPPORTED;
     if (batch == 0 || seq == 0 || heads == 0) return PAMM_OK;
@@ -879,19 +910,19 @@ pamm_status pamm_rotary(const void* X, int64_t x_batch, int64_t x_token, int64_t
     // the same matrix in and out is turned in place; other overlaps are the caller's error
     const bool in_place = X == (const void*)Y;
     if (in_place && (x_batch != y_batch || x_token != y_token || x_head != y_head)) return PAMM_ERR_INVALID_ARG;
-    RotaryArgs a;
+    RotaryArgs a = {};
     a.x = X; a.y = Y; a.table = table; a.positions = positions;
     a.xb = x_batch; a.xs = x_token; a.xh = x_head; a.yb = y_batch; a.ys = y_token; a.yh = y_head;
     a.pb = pos_batch; a.ps = pos_token; a.table_rows = table_rows; a.first = first;
-    a.seq = (int)seq; a.heads = (int)heads; a.rotated = (int)rotated; a.head_dim = (int)head_dim; a.rot = (int)rot_dim;
-    a.adjacent = pairs == PAMM_PAIRS_ADJACENT; a.transposed = transposed != 0; a.pos64 = pos_type == PAMM_POS_I64;
-    a.in_place = in_place;
-    const int64_t v = 16 / (int64_t)es;
-    const bool vec = aligned(X, 16) && aligned(Y, 16) && aligned(table, 16) && head_dim % v == 0 &&
-                     (a.adjacent ? rot_dim % v == 0 : rot_dim % (2 * v) == 0) && x_batch % v == 0 && x_token % v == 0 &&
-                     x_head % v == 0 && y_batch % v == 0 && y_token % v == 0 && y_head % v == 0;
+    a.rot = (int)rot_dim; a.transposed = transposed != 0; a.pos64 = pos_type == PAMM_POS_I64;
+    const RotaryShape g = {batch, seq, heads, rotated, head_dim, pairs == PAMM_PAIRS_ADJACENT, in_place};
+    // the lowest bit of all sizes, distances and addresses (in elements): the widest access that fits everything
+    uint64_t bits = (uint64_t)(16 / es) | (uint64_t)head_dim | (uint64_t)(g.adjacent ? rot_dim : rot_dim / 2) |
+                    reinterpret_cast<uintptr_t>(X) / es | reinterpret_cast<uintptr_t>(Y) / es | (uint64_t)x_batch | (uint64_t)x_token |
+                    (uint64_t)x_head | (uint64_t)y_batch | (uint64_t)y_token | (uint64_t)y_head;
+    const int width = aligned(table, 16) ? (int)(bits & (~bits + 1)) : 1;
     cudaStream_t st = (cudaStream_t)stream;
-    return dt == PAMM_F32 ? launch_rotary<float>(a, batch * seq, vec, st) : launch_rotary<__nv_bfloat16>(a, batch * seq, vec, st);
+    return dt == PAMM_F32 ? launch_rotary<float>(a, g, width, st) : launch_rotary<__nv_bfloat16>(a, g, width, st);
 }
 
 pamm_status pamm_grad_norm(const pamm_tensor* grads, int64_t count, float* norm, void* workspace, size_t ws_bytes, void* stream) {

@@ -39,13 +39,12 @@ __device__ __forceinline__ uint4 round_vec<__nv_bfloat16>(const float (&x)[8]) {
     return make_uint4(round_bf16x2(x[0], x[1]), round_bf16x2(x[2], x[3]), round_bf16x2(x[4], x[5]), round_bf16x2(x[6], x[7]));
 }
 
-// V consecutive elements of a row as they lie in memory: one 16-byte vector (V = Vec16<T>::N, 16-byte aligned) or one
-// element (V = 1, any alignment of the type).  Loading and unpacking are apart, so that all of a
-// thread's loads are in flight before the first is waited for.
+// V consecutive elements of a row as they lie in memory, aligned to their size of 2, 4, 8 or 16 bytes.  Loading and unpacking
+// are apart, so that all of a thread's loads are in flight before the first is waited for.
 template <typename T, int V>
 struct Piece {
-    static_assert(V == 1 || V == Vec16<T>::N, "one element or 16 bytes");
-    static constexpr int WORDS = V == 1 ? 1 : 4;
+    static constexpr int BYTES = V * (int)sizeof(T), WORDS = BYTES < 4 ? 1 : BYTES / 4;
+    static_assert(BYTES == 2 || BYTES == 4 || BYTES == 8 || BYTES == 16, "a power of two up to 16 bytes");
     struct Raw { uint32_t w[WORDS]; };
 
     static __device__ __forceinline__ Raw zero() {
@@ -56,9 +55,13 @@ struct Piece {
     }
     static __device__ __forceinline__ Raw load(const T* p) {
         Raw r;
-        if constexpr (V == 1) {
-            if constexpr (sizeof(T) == 4) r.w[0] = *reinterpret_cast<const uint32_t*>(p);
-            else r.w[0] = *reinterpret_cast<const unsigned short*>(p);
+        if constexpr (BYTES == 2) {
+            r.w[0] = *reinterpret_cast<const unsigned short*>(p);
+        } else if constexpr (BYTES == 4) {
+            r.w[0] = *reinterpret_cast<const uint32_t*>(p);
+        } else if constexpr (BYTES == 8) {
+            const uint2 v = *reinterpret_cast<const uint2*>(p);
+            r.w[0] = v.x; r.w[1] = v.y;
         } else {
             const uint4 v = ld16(p);
             r.w[0] = v.x; r.w[1] = v.y; r.w[2] = v.z; r.w[3] = v.w;
@@ -73,20 +76,27 @@ struct Piece {
             out[0] = bf16_lo(r.w[0]);
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < WORDS; ++i) {
                 out[2 * i] = bf16_lo(r.w[i]);
                 out[2 * i + 1] = bf16_hi(r.w[i]);
             }
         }
     }
     static __device__ __forceinline__ void store(T* p, const float* x) {       // rounded to nearest even
-        if constexpr (V == 1) {
+        uint32_t w[WORDS];
+        if constexpr (BYTES == 2) {
             *p = from_float<T>(x[0]);
+            return;
         } else if constexpr (sizeof(T) == 4) {
-            st16(p, make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])));
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) w[i] = __float_as_uint(x[i]);
         } else {
-            st16(p, make_uint4(round_bf16x2(x[0], x[1]), round_bf16x2(x[2], x[3]), round_bf16x2(x[4], x[5]), round_bf16x2(x[6], x[7])));
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) w[i] = round_bf16x2(x[2 * i], x[2 * i + 1]);
         }
+        if constexpr (BYTES == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
+        else if constexpr (BYTES == 8) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+        else if constexpr (BYTES == 16) st16(p, make_uint4(w[0], w[1], w[2], w[3]));
     }
 };
 
