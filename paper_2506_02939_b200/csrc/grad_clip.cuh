@@ -1,12 +1,13 @@
 // The global norm of a list of gradients, and their clipping:
 //   N = sqrt(sum over all elements of g^2);  g <- g min(1, max_norm / (N + 1e-6))
 //
-// Two passes, both bound by memory: the squares' sum reads every element once, the scaling reads and
-// writes it once more (or, in place and below the limit, does nothing).  The list travels in the
-// kernels' parameters, so that a call needs no copy and no allocation and can be captured; lists
-// longer than one launch holds take several.  The work is cut into chunks of about 8192 elements that
-// every block takes a consecutive range of; squares are summed in 64 bits, whose range no bf16 or fp32
-// gradient leaves, and joined in a fixed order.
+// Three launches, the first and the last bound by memory: every block sums the squares of its share; one block
+// joins the sums in a fixed order; and the scaling reads and writes every element once more (or, in place and below the
+// limit, returns at once).  The list travels in the kernels' parameters, so that a call needs no copy and no allocation
+// and can be captured; lists longer than one launch holds take several.  The work is cut into chunks of 4096 to 65536
+// elements, block after block; the scaling goes through them backwards, and so finds in L2 what the sum read last.
+// Squares are summed in 64 bits, whose range no bf16 or fp32 gradient leaves (B200 has half as many 64-bit as 32-bit
+// lanes; the sum stays bound by memory).
 #pragma once
 #include "pamm_common.cuh"
 #include "row_io.cuh"
@@ -14,87 +15,106 @@
 namespace pamm {
 
 constexpr int GC_THREADS = 256;
-constexpr int GC_CHUNK = 8192;          // elements
-constexpr int GC_BLOCKS_PER_SM = 8;
-constexpr int GC_SMALL = 24, GC_LARGE = 448;      // list entries per launch: parameters of 1.5 and 28 KB
+constexpr int GC_UNROLL = 4;            // vectors in flight per thread
+constexpr int GC_BLOCKS_PER_SM = 8;     // of the sum: one wave
+// elements of a chunk: of the sum, by the size of the list; of the scaling
+constexpr int GC_MIN_CHUNK = 4096, GC_MAX_CHUNK = 65536, GC_SCALE_CHUNK = 16384;
+constexpr int GC_SMALL = 24, GC_LARGE = 448;      // list entries per launch: parameters of 1.6 and 29 KB
 
 struct GradEntry {
     const void* in;
     void* out;
     int64_t rows, cols, ld_in, ld_out;
-    int64_t first_chunk;
+    int64_t first_chunk, pieces;          // chunks before this entry; of a wide row
     int in_bf16, out_bf16;
 };
 template <int CAP>
 struct GradList {
-    int count, add;                     // add: the partial sums continue those of an earlier launch
+    int count;
+    int add;                            // the partial sums continue those of an earlier launch
+    int in_place;                       // every output is its input
+    int chunk;                          // elements
     int64_t chunks;
     GradEntry e[CAP];
 };
 
-// Rows of at most GC_CHUNK columns are put together until a chunk is full, wider rows are cut.
-__host__ __device__ inline int64_t grad_rows_per_chunk(int64_t cols) { return cols < GC_CHUNK ? GC_CHUNK / cols : 1; }
-__host__ __device__ inline int64_t grad_pieces(int64_t cols) { return (cols + GC_CHUNK - 1) / GC_CHUNK; }
-__host__ __device__ inline int64_t grad_chunks(int64_t rows, int64_t cols) {
+// Rows of fewer columns than a chunk has elements are put together until it is full, wider rows are cut.
+inline int64_t grad_chunks(int64_t rows, int64_t cols, int64_t chunk) {
     if (rows == 0 || cols == 0) return 0;
-    const int64_t rpc = grad_rows_per_chunk(cols);
-    return cols < GC_CHUNK ? (rows + rpc - 1) / rpc : rows * grad_pieces(cols);
+    return rows > 1 && cols < chunk ? (rows + chunk / cols - 1) / (chunk / cols) : rows * ((cols + chunk - 1) / chunk);
 }
 
-// Squares of `len` consecutive elements, by `step` threads of which this is number t.
+// Elements before the first 16-byte boundary at or after p, at most len.
 template <typename T>
-__device__ __forceinline__ double span_squares(const T* p, int len, int t, int step) {
-    constexpr int V = Vec16<T>::N;
-    double acc = 0.0;
-    const int lead = min(len, (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / (int)sizeof(T));
-    const int vecs = (len - lead) / V;
-    for (int i = t; i < vecs; i += step) {
-        float v[V];
-        unpack_vec<T>(ld16(p + lead + i * V), v);
-#pragma unroll
-        for (int e = 0; e < V; ++e) acc += (double)v[e] * (double)v[e];
-    }
-    if (t < lead) {
-        const double v = to_float(p[t]);
-        acc += v * v;
-    }
-    const int done = lead + vecs * V;
-    if (t < len - done) {
-        const double v = to_float(p[done + t]);
-        acc += v * v;
-    }
-    return acc;
+__device__ __forceinline__ int lead_elements(const T* p, int len) {
+    return min(len, (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / (int)sizeof(T));
 }
 
-// The factor as a product of two, so that one below fp32's normal range keeps its digits.
+// A square in 64 bits.  Conversions and products keep up with memory (bf16 from HBM: 6.0 TB/s with them, 6.5 without).
+__device__ __forceinline__ void add_square(double& acc, float x) { acc = fma((double)x, (double)x, acc); }
+
+// Calls one(i) for the elements of a span of `len` before its first and behind its last whole vector, and many(first element, k)
+// for its groups of G elements, k = 0 .. U - 1 of them at a time and then one at a time; by STEP threads, this being number t.
+template <int G, int U, int STEP, typename Load, typename Use, typename One>
+__device__ __forceinline__ void walk_span(int lead, int len, int t, Load load, Use use, One one) {
+    const int groups = (len - lead) / G, done = lead + groups * G;
+    int i = t;
+    for (; i + (U - 1) * STEP < groups; i += U * STEP) {
+#pragma unroll
+        for (int k = 0; k < U; ++k) load(k, lead + (i + k * STEP) * G);
+#pragma unroll
+        for (int k = 0; k < U; ++k) use(k, lead + (i + k * STEP) * G);
+    }
+    for (; i < groups; i += STEP) {
+        load(0, lead + i * G);
+        use(0, lead + i * G);
+    }
+    if (t < lead) one(t);
+    if (t < len - done) one(done + t);
+}
+
+template <typename T, int STEP>
+__device__ __forceinline__ void add_squares(const T* p, int len, int t, double& sum) {
+    constexpr int V = Vec16<T>::N, U = STEP > 32 ? GC_UNROLL : 1;
+    using P = Piece<T, V>;
+    typename P::Raw r[U];
+    walk_span<V, U, STEP>(lead_elements(p, len), len, t, [&](int k, int at) { r[k] = P::load(p + at); },
+                          [&](int k, int) {
+                              float v[V];
+                              P::unpack(r[k], v);
+#pragma unroll
+                              for (int e = 0; e < V; ++e) add_square(sum, v[e]);
+                          },
+                          [&](int at) { add_square(sum, to_float(p[at])); });
+}
+
+// The factor as a product of two, so that one below fp32's normal range keeps its digits; and whether it is 1.
 struct GradFactor {
     float first, second;
+    int keep;
     __device__ __forceinline__ float operator()(float g) const { return g * first * second; }
 };
 
-template <typename TI, typename TO>
-__device__ __forceinline__ void span_scale(const TI* p, TO* q, int len, GradFactor f, int t, int step) {
-    constexpr int V = Vec16<TI>::N, W = Vec16<TO>::N;
-    const int lead = min(len, (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / (int)sizeof(TI));
-    // vector access where both sides reach a 16-byte boundary (of 16-bit and 32-bit elements alike) together
-    constexpr int G = V > W ? V : W;
-    if ((reinterpret_cast<uintptr_t>(q + lead) & 15) != 0) {
-        for (int i = t; i < len; i += step) q[i] = from_float<TO>(f(to_float(p[i])));
+template <typename TI, typename TO, int STEP>
+__device__ __forceinline__ void scale_span(const TI* p, TO* q, int len, const GradFactor& f, int t) {
+    // G elements at a time: 16 bytes on the side of the wider type, so that a warp's accesses have no gaps on either
+    constexpr int G = Vec16<TI>::N < Vec16<TO>::N ? Vec16<TI>::N : Vec16<TO>::N, U = STEP > 32 ? GC_UNROLL : 1;
+    const int lead = lead_elements(p, len);
+    if ((reinterpret_cast<uintptr_t>(q + lead) & 15) != 0) {        // the output is not on a 16-byte boundary there
+        for (int i = t; i < len; i += STEP) q[i] = from_float<TO>(f(to_float(p[i])));
         return;
     }
-    const int groups = (len - lead) / G;
-    for (int i = t; i < groups; i += step) {
-        float v[G];
+    const uint64_t policy = evict_first_policy();       // what is yet to be read stays in L2
+    typename Piece<TI, G>::Raw r[U];
+    walk_span<G, U, STEP>(lead, len, t, [&](int k, int at) { r[k] = Piece<TI, G>::load(p + at); },
+                          [&](int k, int at) {
+                              float v[G];
+                              Piece<TI, G>::unpack(r[k], v);
 #pragma unroll
-        for (int k = 0; k < G; k += V) unpack_vec<TI>(ld16(p + lead + i * G + k), *reinterpret_cast<float(*)[V]>(v + k));
-#pragma unroll
-        for (int e = 0; e < G; ++e) v[e] = f(v[e]);
-#pragma unroll
-        for (int k = 0; k < G; k += W) st16(q + lead + i * G + k, round_vec<TO>(*reinterpret_cast<float(*)[W]>(v + k)));
-    }
-    if (t < lead) q[t] = from_float<TO>(f(to_float(p[t])));
-    const int done = lead + groups * G;
-    if (t < len - done) q[done + t] = from_float<TO>(f(to_float(p[done + t])));
+                              for (int e = 0; e < G; ++e) v[e] = f(v[e]);
+                              Piece<TO, G>::store(q + at, v, policy);
+                          },
+                          [&](int at) { q[at] = from_float<TO>(f(to_float(p[at]))); });
 }
 
 __device__ __forceinline__ double block_sum_double(double x, double* part) {
@@ -108,98 +128,100 @@ __device__ __forceinline__ double block_sum_double(double x, double* part) {
     return x;
 }
 
-// Calls body(entry, row, column, length, thread, threads) for every span of the block's chunks.
-template <int CAP, typename F>
-__device__ __forceinline__ void for_each_span(const GradList<CAP>& list, F body) {
-    const int64_t per = (list.chunks + gridDim.x - 1) / gridDim.x;
-    const int64_t begin = (int64_t)blockIdx.x * per;
-    const int64_t end = begin + per < list.chunks ? begin + per : list.chunks;
-    if (begin >= end) return;
-    int lo = 0, hi = list.count - 1;            // the last entry that starts at or before `begin`
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (list.e[mid].first_chunk <= begin) lo = mid;
-        else hi = mid - 1;
-    }
-    int k = lo;
-    for (int64_t chunk = begin; chunk < end; ++chunk) {
-        while (k + 1 < list.count && list.e[k + 1].first_chunk <= chunk) ++k;
-        const GradEntry& g = list.e[k];
-        const int64_t local = chunk - g.first_chunk;
-        if (g.cols >= GC_CHUNK) {
-            const int64_t pieces = grad_pieces(g.cols), row = local / pieces, col = (local - row * pieces) * GC_CHUNK;
-            body(g, row, col, (int)(g.cols - col < GC_CHUNK ? g.cols - col : GC_CHUNK), (int)threadIdx.x, GC_THREADS);
-        } else {
-            const int64_t rpc = grad_rows_per_chunk(g.cols), first = local * rpc;
-            const int64_t last = first + rpc < g.rows ? first + rpc : g.rows;
-            if (last - first == 1) {
-                body(g, first, 0, (int)g.cols, (int)threadIdx.x, GC_THREADS);
-            } else {
-                for (int64_t row = first + (threadIdx.x >> 5); row < last; row += GC_THREADS / 32)
-                    body(g, row, 0, (int)g.cols, (int)(threadIdx.x & 31), 32);
-            }
+template <int N> struct Threads { static constexpr int value = N; };
+
+// Calls wide(entry, row, column, length) for every span of the block's chunks (which lie gridDim.x apart) that the whole block
+// takes, narrow(entry, row, 0, length) for those that a warp takes.
+template <int CAP, typename F, typename G>
+__device__ __forceinline__ void for_each_span(const GradList<CAP>& list, bool backwards, F wide, G narrow) {
+    for (int64_t n = blockIdx.x; n < list.chunks; n += gridDim.x) {
+        const int64_t at = backwards ? list.chunks - 1 - n : n;
+        int lo = 0, hi = list.count - 1;            // the last entry that starts at or before the chunk
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if (list.e[mid].first_chunk <= at) lo = mid;
+            else hi = mid - 1;
+        }
+        const GradEntry& g = list.e[lo];
+        const int64_t local = at - g.first_chunk;
+        if (g.rows == 1) {
+            const int64_t col = local * list.chunk;
+            wide(g, (int64_t)0, col, (int)(g.cols - col < list.chunk ? g.cols - col : list.chunk));
+        } else if (g.cols >= list.chunk) {
+            const int64_t row = local / g.pieces, col = (local - row * g.pieces) * list.chunk;
+            wide(g, row, col, (int)(g.cols - col < list.chunk ? g.cols - col : list.chunk));
+        } else {                                    // whole rows
+            const int64_t rows = list.chunk / (int)g.cols, first = local * rows;
+            const int64_t last = first + rows < g.rows ? first + rows : g.rows;
+            for (int64_t row = first + (threadIdx.x >> 5); row < last; row += GC_THREADS / 32) narrow(g, row, (int64_t)0, (int)g.cols);
         }
     }
 }
 
 template <int CAP>
-__global__ void __launch_bounds__(GC_THREADS)
+__global__ void __launch_bounds__(GC_THREADS, GC_BLOCKS_PER_SM)
 grad_squares_kernel(const __grid_constant__ GradList<CAP> list, double* partial) {
     __shared__ double s_part[GC_THREADS / 32];
     grid_dependency_wait();
     grid_launch_dependents();
-    double acc = 0.0;
-    for_each_span(list, [&](const GradEntry& g, int64_t row, int64_t col, int len, int t, int step) {
+    double sum = 0.0;
+    const auto span = [&](auto step, int t, const GradEntry& g, int64_t row, int64_t col, int len) {
         const int64_t at = row * g.ld_in + col;
-        acc += g.in_bf16 ? span_squares(static_cast<const __nv_bfloat16*>(g.in) + at, len, t, step)
-                         : span_squares(static_cast<const float*>(g.in) + at, len, t, step);
-    });
-    acc = block_sum_double(acc, s_part);
+        if (g.in_bf16) add_squares<__nv_bfloat16, decltype(step)::value>(static_cast<const __nv_bfloat16*>(g.in) + at, len, t, sum);
+        else add_squares<float, decltype(step)::value>(static_cast<const float*>(g.in) + at, len, t, sum);
+    };
+    for_each_span(list, false,
+                  [&](const GradEntry& g, int64_t row, int64_t col, int len) { span(Threads<GC_THREADS>(), threadIdx.x, g, row, col, len); },
+                  [&](const GradEntry& g, int64_t row, int64_t col, int len) { span(Threads<32>(), threadIdx.x & 31, g, row, col, len); });
+    const double acc = block_sum_double(sum, s_part);
     if (threadIdx.x == 0) partial[blockIdx.x] = (list.add ? partial[blockIdx.x] : 0.0) + acc;
 }
 
-// The norm from the partial sums, in every block alike.
-__device__ __forceinline__ double norm_of(const double* partial, int parts, double* s_part) {
+// The norm and the factor, by one block.
+__global__ void __launch_bounds__(GC_THREADS)
+grad_norm_finish_kernel(const double* partial, int parts, double max_norm, float* norm, GradFactor* factor) {
+    __shared__ double s_part[GC_THREADS / 32];
+    grid_dependency_wait();
+    grid_launch_dependents();
     double acc = 0.0;
     for (int i = threadIdx.x; i < parts; i += GC_THREADS) acc += partial[i];
-    return sqrt(block_sum_double(acc, s_part));
-}
-
-__global__ void __launch_bounds__(GC_THREADS)
-grad_norm_finish_kernel(const double* partial, int parts, float* norm) {
-    __shared__ double s_part[GC_THREADS / 32];
-    grid_dependency_wait();
-    grid_launch_dependents();
-    const double total = norm_of(partial, parts, s_part);
-    if (threadIdx.x == 0) *norm = (float)total;
-}
-
-template <int CAP>
-__global__ void __launch_bounds__(GC_THREADS)
-grad_scale_kernel(const __grid_constant__ GradList<CAP> list, const double* partial, int parts, double max_norm, float* norm) {
-    __shared__ double s_part[GC_THREADS / 32];
-    grid_dependency_wait();
-    grid_launch_dependents();
-    const double total = norm_of(partial, parts, s_part);
-    if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)total;
+    const double total = sqrt(block_sum_double(acc, s_part));
+    if (threadIdx.x != 0) return;
+    *norm = (float)total;
     const double limited = max_norm / (total + 1e-6);
     // no limit at all, or one that is kept: 1; a NaN norm gives NaN, as in the formula
     const bool keep = isinf(max_norm) || limited >= 1.0;
-    GradFactor f = {1.f, keep ? 1.f : (float)limited};
-    if (!keep && limited < 0x1p-100) f = {0x1p-64f, (float)(limited * 0x1p64)};
-    for_each_span(list, [&](const GradEntry& g, int64_t row, int64_t col, int len, int t, int step) {
-        if (keep && g.in == g.out && g.in_bf16 == g.out_bf16) return;     // g * 1 is there already
+    GradFactor f = {1.f, keep ? 1.f : (float)limited, keep ? 1 : 0};
+    if (!keep && limited < 0x1p-100) {
+        f.first = 0x1p-64f;
+        f.second = (float)(limited * 0x1p64);
+    }
+    *factor = f;
+}
+
+template <int CAP>
+__global__ void __launch_bounds__(GC_THREADS, 6)
+grad_scale_kernel(const __grid_constant__ GradList<CAP> list, const GradFactor* factor) {
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const GradFactor f = *factor;
+    if (f.keep && list.in_place) return;            // g * 1 is there already
+    const auto span = [&](auto step, int t, const GradEntry& g, int64_t row, int64_t col, int len) {
+        constexpr int STEP = decltype(step)::value;
         const int64_t i = row * g.ld_in + col, o = row * g.ld_out + col;
         if (g.in_bf16) {
             const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(g.in) + i;
-            if (g.out_bf16) span_scale(p, static_cast<__nv_bfloat16*>(g.out) + o, len, f, t, step);
-            else span_scale(p, static_cast<float*>(g.out) + o, len, f, t, step);
+            if (g.out_bf16) scale_span<__nv_bfloat16, __nv_bfloat16, STEP>(p, static_cast<__nv_bfloat16*>(g.out) + o, len, f, t);
+            else scale_span<__nv_bfloat16, float, STEP>(p, static_cast<float*>(g.out) + o, len, f, t);
         } else {
             const float* p = static_cast<const float*>(g.in) + i;
-            if (g.out_bf16) span_scale(p, static_cast<__nv_bfloat16*>(g.out) + o, len, f, t, step);
-            else span_scale(p, static_cast<float*>(g.out) + o, len, f, t, step);
+            if (g.out_bf16) scale_span<float, __nv_bfloat16, STEP>(p, static_cast<__nv_bfloat16*>(g.out) + o, len, f, t);
+            else scale_span<float, float, STEP>(p, static_cast<float*>(g.out) + o, len, f, t);
         }
-    });
+    };
+    for_each_span(list, true,
+                  [&](const GradEntry& g, int64_t row, int64_t col, int len) { span(Threads<GC_THREADS>(), threadIdx.x, g, row, col, len); },
+                  [&](const GradEntry& g, int64_t row, int64_t col, int len) { span(Threads<32>(), threadIdx.x & 31, g, row, col, len); });
 }
 
 }  // namespace pamm

@@ -17,6 +17,17 @@ __device__ __forceinline__ void st16(void* p, const uint4& v) {
     asm volatile("st.global.v4.u32 [%0], {%1,%2,%3,%4};" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 
+// A store whose lines leave L2 first (a policy of evict_first_policy).
+__device__ __forceinline__ uint64_t evict_first_policy() {
+    uint64_t p;
+    asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+    return p;
+}
+__device__ __forceinline__ void st16(void* p, const uint4& v, uint64_t policy) {
+    asm volatile("st.global.L2::cache_hint.v4.u32 [%0], {%1,%2,%3,%4}, %5;" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w), "l"(policy)
+                 : "memory");
+}
+
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 template <typename T> __device__ __forceinline__ T from_float(float x);
@@ -82,11 +93,9 @@ struct Piece {
             }
         }
     }
-    static __device__ __forceinline__ void store(T* p, const float* x) {       // rounded to nearest even
-        uint32_t w[WORDS];
+    static __device__ __forceinline__ void pack(const float* x, uint32_t (&w)[WORDS]) {       // rounded to nearest even
         if constexpr (BYTES == 2) {
-            *p = from_float<T>(x[0]);
-            return;
+            w[0] = round_bf16x2(x[0], 0.f);
         } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
             for (int i = 0; i < WORDS; ++i) w[i] = __float_as_uint(x[i]);
@@ -94,9 +103,23 @@ struct Piece {
 #pragma unroll
             for (int i = 0; i < WORDS; ++i) w[i] = round_bf16x2(x[2 * i], x[2 * i + 1]);
         }
-        if constexpr (BYTES == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
+    }
+    static __device__ __forceinline__ void store(T* p, const float* x) {
+        uint32_t w[WORDS];
+        pack(x, w);
+        if constexpr (BYTES == 2) *reinterpret_cast<unsigned short*>(p) = (unsigned short)w[0];
+        else if constexpr (BYTES == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
         else if constexpr (BYTES == 8) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
-        else if constexpr (BYTES == 16) st16(p, make_uint4(w[0], w[1], w[2], w[3]));
+        else st16(p, make_uint4(w[0], w[1], w[2], w[3]));
+    }
+    static __device__ __forceinline__ void store(T* p, const float* x, uint64_t policy) {     // the policy is for 16 bytes only
+        if constexpr (BYTES == 16) {
+            uint32_t w[WORDS];
+            pack(x, w);
+            st16(p, make_uint4(w[0], w[1], w[2], w[3]), policy);
+        } else {
+            store(p, x);
+        }
     }
 };
 
