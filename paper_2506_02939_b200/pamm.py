@@ -6,10 +6,8 @@ loudly when the library has not been built; there is no CPU fallback.
 """
 from __future__ import annotations
 
-import array
 import contextlib
 import ctypes
-import functools
 from pathlib import Path
 
 import torch
@@ -20,6 +18,7 @@ if not _LIB_PATH.exists():
         f"{_LIB_PATH} is missing: build it with `python -m paper_2506_02939_b200.build` "
         "(nvcc, sm_100a). The PAMM path has no fallback.")
 _lib = ctypes.CDLL(str(_LIB_PATH))
+from . import _binding  # noqa: E402  (linked against the library; built next to it)
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT, ERR_BAD_INDEX = range(7)
 F32, BF16 = 0, 1
@@ -77,7 +76,6 @@ for _name, (_args, _res) in _SIGNATURES.items():
     _fn.argtypes, _fn.restype = _args, _res
 
 EXPORTED = tuple(_SIGNATURES)
-_SIZES = _lib                             # for sizes that are asked for while another call is being prepared
 
 
 class PammError(RuntimeError):
@@ -85,6 +83,9 @@ class PammError(RuntimeError):
         self.code = code
         detail = _lib.pamm_last_error_detail().decode() if code == ERR_CUDA else ""
         super().__init__(f"{where}: {status_string(code)} (status {code})" + (f": {detail}" if detail else ""))
+
+
+_binding.set_error(PammError)
 
 
 def status_string(code: int) -> str:
@@ -121,10 +122,6 @@ def _ld(t: torch.Tensor) -> int:
 def _stream(stream) -> ctypes.c_void_p:
     s = torch.cuda.current_stream() if stream is None else stream
     return ctypes.c_void_p(s.cuda_stream)
-
-
-def _raw_stream(stream) -> int:
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
 
 
 _prep_keep = None      # while a call is being prepared: the tensors it allocates, kept alive with the prepared call
@@ -389,13 +386,16 @@ def prepared(call, *args, **kwargs):
     Python-side marshalling -- for loops where a step is only a few microseconds of GPU work.  Outputs the call
     allocates itself stay alive with the callable but are not handed out: pass in the ones you want to read."""
     global _lib, _prep_keep
-    real, rec = _lib, _RecordingLib(_lib)
+    real, rec, direct = _lib, _RecordingLib(_lib), []
     _lib, _prep_keep = rec, []
+    _binding.set_record(direct)
     try:
         call(*args, **kwargs)
-        keep = (args, kwargs, _prep_keep)          # the tensors behind the pointers, the call's own allocations included
+        keep = (args, kwargs, _prep_keep, direct)  # the tensors behind the pointers, the call's own allocations included
     finally:
         _lib, _prep_keep = real, None
+        _binding.set_record(None)
+    rec.calls += [(name, getattr(real, name), cargs) for name, cargs, _ in direct]
     if len(rec.calls) != 1:
         raise ValueError("prepared() takes a binding function that makes exactly one library call")
     name, fn, cargs = rec.calls[0]
@@ -408,46 +408,14 @@ def prepared(call, *args, **kwargs):
 
 
 # ---- the operators around the projection: norm, rotary positions, gradient clipping ----------------
-# Inputs may lie on any stream's memory; what a call allocates belongs to the stream it runs on.
+# Checks, allocation and the C call are in the compiled binding (csrc/binding.cpp).  A call runs on the current
+# stream of its tensors' device, or on `stream`; what it allocates belongs to that stream.
 
-_NO_CONTEXT = contextlib.nullcontext()
-_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
-
-
-def _on(stream):
-    """A context in which tensors are allocated for `stream` (None: the current stream, nothing to do)."""
-    return _NO_CONTEXT if stream is None else torch.cuda.stream(stream)
-
-
-def _type(t: torch.Tensor, what: str) -> int:
-    code = _DTYPES.get(t.dtype)
-    if code is None:
-        raise TypeError(f"{what} is float32 or bfloat16, got {t.dtype}")
-    if not t.is_cuda:
-        raise ValueError(f"{what} is a CUDA tensor")
-    return code
-
-
-def _matrix(t: torch.Tensor, what: str, b: int, n: int, dtype) -> int:
-    """Leading dimension of a b x n matrix of the given type with contiguous rows."""
-    if t.dim() != 2 or t.shape[0] != b or t.shape[1] != n:
-        raise ValueError(f"{what} is {b} x {n}, got {tuple(t.shape)}")
-    if t.dtype != dtype or not t.is_cuda:
-        raise TypeError(f"{what} is a CUDA tensor of {dtype}, got {t.dtype} on {t.device}")
-    ld, unit = t.stride()
-    if unit != 1 and n > 1:
-        raise ValueError(f"{what} needs contiguous rows (a row stride is allowed)")
-    return n if b < 2 else ld
-
-
-def _vector(t, what: str, n: int, dtype=None) -> int | None:
-    """Address of a contiguous CUDA vector of n entries (None: none)."""
-    if t is None:
-        return None
-    if t.shape != (n,) or not t.is_contiguous() or not t.is_cuda or (dtype is not None and t.dtype != dtype):
-        raise ValueError(f"{what} is a contiguous CUDA vector of {n}{'' if dtype is None else f' of {dtype}'}, "
-                         f"got {tuple(t.shape)} of {t.dtype} on {t.device}")
-    return t.data_ptr()
+def _binding_on(stream, function, *args):
+    if stream is None:
+        return function(*args)
+    with torch.cuda.stream(stream):
+        return function(*args)
 
 
 def norm_forward(X, weight=None, bias=None, residual=None, eps: float = 1e-5, rms: bool = False, Y=None, H=None, mean=None,
@@ -455,66 +423,16 @@ def norm_forward(X, weight=None, bias=None, residual=None, eps: float = 1e-5, rm
     """Layer norm of the rows of ``X`` (``rms``: its root-mean-square form) after adding ``residual``; see
     pamm_norm_forward.  Returns Y, h = X + residual (``X`` itself without a residual), and mean and rstd (fp32) for
     ``norm_backward``; mean is None in the RMS form.  ``Y`` and ``H`` may be ``X`` or ``residual`` to save memory."""
-    b, n = X.shape
-    dt, dtype = _type(X, "X"), X.dtype
-    ldx = _matrix(X, "X", b, n, dtype)
-    w_type = None if weight is None else weight.dtype
-    w_dt = dt if weight is None else _type(weight, "weight")
-    if weight is None and bias is not None:
-        w_dt, w_type = _type(bias, "bias"), bias.dtype
-    w, c = _vector(weight, "weight", n), _vector(bias, "bias", n, w_type)
-    ldr = 0 if residual is None else _matrix(residual, "residual", b, n, dtype)
-    with _on(stream):
-        Y = _empty((b, n), dtype=dtype, device=X.device) if Y is None else Y
-        if H is None and residual is not None:
-            H = _empty((b, n), dtype=dtype, device=X.device)
-        if mean is None and not rms:
-            mean = _empty(b, dtype=torch.float32, device=X.device)
-        rstd = _empty(b, dtype=torch.float32, device=X.device) if rstd is None else rstd
-    _check(_lib.pamm_norm_forward(
-        NORM_RMS if rms else NORM_LAYER, X.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ldr, b, n, dt,
-        w, c, w_dt, eps, Y.data_ptr(), _matrix(Y, "Y", b, n, dtype), None if H is None else H.data_ptr(),
-        0 if H is None else _matrix(H, "H", b, n, dtype), _vector(mean, "mean", b, torch.float32),
-        _vector(rstd, "rstd", b, torch.float32), _raw_stream(stream)), "pamm_norm_forward")
-    return Y, X if H is None else H, None if rms else mean, rstd
+    return _binding_on(stream, _binding.norm_forward, X, weight, bias, residual, eps, rms, Y, H, mean, rstd)
 
 
 def norm_backward(dY, X, mean, rstd, weight=None, bias: bool = False, dH=None, dX=None, dw=None, dc=None, need_dw: bool = True,
                   dw_dtype=None, workspace=None, stream=None):
     """Gradients of ``norm_forward``: dX, dw and (``bias``) dc.  ``X`` is the row that was normalised (h after a residual
     addition), ``mean`` None for the RMS form, ``dH`` the gradient that reached h past the norm.  ``dw_dtype`` is
-    the weight's type by default; ``need_dw=False`` (a frozen norm) leaves dw and dc out.  ``dX`` may be ``dY``, ``X`` or
-    ``dH``."""
-    b, n = X.shape
-    dt, dtype = _type(X, "X"), X.dtype
-    ldx, lddy = _matrix(X, "X", b, n, dtype), _matrix(dY, "dY", b, n, dtype)
-    w_dt = dt if weight is None else _type(weight, "weight")
-    if dw_dtype is None:
-        dw_dtype = dw.dtype if dw is not None else dc.dtype if dc is not None else dtype if weight is None else weight.dtype
-    lddh = 0 if dH is None else _matrix(dH, "dH", b, n, dtype)
-    with _on(stream):
-        dX = _empty((b, n), dtype=dtype, device=X.device) if dX is None else dX
-        if need_dw:
-            dw = _empty(n, dtype=dw_dtype, device=X.device) if dw is None else dw
-            if bias and dc is None:
-                dc = _empty(n, dtype=dw_dtype, device=X.device)
-        if workspace is None and (dw is not None or dc is not None):
-            workspace = _empty(_norm_backward_bytes(b, n), dtype=torch.uint8, device=X.device)
-    if dw_dtype not in _DTYPES:
-        raise TypeError(f"dw is float32 or bfloat16, got {dw_dtype}")
-    _check(_lib.pamm_norm_backward(
-        NORM_RMS if mean is None else NORM_LAYER, dY.data_ptr(), lddy, X.data_ptr(), ldx, _vector(mean, "mean", b, torch.float32),
-        _vector(rstd, "rstd", b, torch.float32), b, n, dt, _vector(weight, "weight", n), w_dt,
-        None if dH is None else dH.data_ptr(), lddh, dX.data_ptr(), _matrix(dX, "dX", b, n, dtype),
-        _vector(dw, "dw", n, dw_dtype), _vector(dc, "dc", n, dw_dtype), _DTYPES[dw_dtype],
-        None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(),
-        _raw_stream(stream)), "pamm_norm_backward")
-    return dX, dw, dc
-
-
-@functools.lru_cache(maxsize=256)
-def _norm_backward_bytes(b: int, n: int) -> int:
-    return _SIZES.pamm_workspace_bytes(WS_NORM_BACKWARD, b, n, 1, 1, F32)
+    the weight's type by default; ``need_dw=False`` (a frozen norm) leaves dw and dc out unless they are given.  ``dX`` may
+    be ``dY``, ``X`` or ``dH``."""
+    return _binding_on(stream, _binding.norm_backward, dY, X, mean, rstd, weight, bias, dH, dX, dw, dc, need_dw, dw_dtype, workspace)
 
 
 def rotary_frequencies(rot_dim: int, base: float = 10000.0, scaling: int = ROTARY_PLAIN, factor: float = 1.0,
@@ -523,7 +441,7 @@ def rotary_frequencies(rot_dim: int, base: float = 10000.0, scaling: int = ROTAR
     context ``factor`` times as long as the trained one; see pamm_rotary_frequencies_host."""
     freq, amplitude = _empty(max(0, rot_dim) // 2, dtype=torch.float64), _kept(ctypes.c_double())
     _check(_lib.pamm_rotary_frequencies_host(rot_dim, base, scaling, factor, trained_length, slow, fast,
-                                             freq.data_ptr() or None, ctypes.addressof(amplitude)), "pamm_rotary_frequencies_host")
+                                             _ptr(freq), ctypes.addressof(amplitude)), "pamm_rotary_frequencies_host")
     return freq, amplitude.value
 
 
@@ -531,147 +449,34 @@ def rotary_table(length: int, frequencies, amplitude: float = 1.0, first: int = 
     """fp32 rows [amplitude cos | amplitude sin] of positions ``first`` .. ``first + length - 1``, made once and kept."""
     freq = _kept(frequencies.to(device="cpu", dtype=torch.float64).contiguous())
     rot = 2 * freq.numel()
-    with _on(stream):
-        table = _empty((length, rot), dtype=torch.float32, device=device) if out is None else out
-    if table.shape != (length, rot) or table.dtype != torch.float32 or not table.is_contiguous() or not table.is_cuda:
+    if out is None:
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+            out = _empty((length, rot), dtype=torch.float32, device=device)
+    if out.shape != (length, rot) or out.dtype != torch.float32 or not out.is_contiguous() or not out.is_cuda:
         raise ValueError(f"the table is a contiguous CUDA float32 matrix of {length} x {rot}")
-    _check(_lib.pamm_rotary_table(freq.data_ptr(), rot, amplitude, first, length, table.data_ptr(), _raw_stream(stream)),
-           "pamm_rotary_table")
-    return table
+    _check(_lib.pamm_rotary_table(_ptr(freq), rot, amplitude, first, length, _ptr(out), _stream(stream)), "pamm_rotary_table")
+    return out
 
 
 def rotary(X, table, positions=None, rotated: int | None = None, rot_dim: int | None = None, interleaved: bool = False,
            transposed: bool = False, first: int = 0, out=None, stream=None):
     """Rotary positions on the heads of ``X``, of shape (tokens, heads, head_dim) or (batch, tokens, heads, head_dim), any
     strides with contiguous heads -- for instance ``Z.view(batch, seq, heads, head_dim)`` of the fused row [Q|K|V].
-    The first ``rotated`` heads (None: all) are turned, the others copied; ``table`` is ``rotary_table``'s, whose width is
-    the default ``rot_dim``.  ``positions``: int32 or int64 of shape (tokens,) or (batch, tokens); None: ``first`` + the
-    token's index.  ``transposed`` gives the gradient's turn.  ``out=X`` turns in place."""
-    shape = X.shape
-    if len(shape) == 4:
-        batch, seq, heads, d = shape
-        xb, xs, xh, xd = X.stride()
-    elif len(shape) == 3:
-        batch, (seq, heads, d) = 1, shape
-        xb, (xs, xh, xd) = 0, X.stride()
-    else:
-        raise ValueError(f"X is (tokens, heads, head_dim) or (batch, tokens, heads, head_dim), got {tuple(shape)}")
-    dt = _type(X, "X")
-    if table.dim() != 2 or table.dtype != torch.float32 or not table.is_cuda or not table.is_contiguous():
-        raise ValueError("the table is a contiguous CUDA float32 matrix")
-    rows, width = table.shape
-    if rot_dim is not None and rot_dim != width:
-        raise ValueError(f"the table holds rotations of {width} elements, not {rot_dim}")
-    if xd != 1 and d > 1:
-        raise ValueError("X needs contiguous heads")
-    if out is None:
-        with _on(stream):
-            out = _empty(shape, dtype=X.dtype, device=X.device)
-    elif out.shape != shape or out.dtype != X.dtype or not out.is_cuda:
-        raise ValueError(f"out is a CUDA tensor of X's shape and type, got {tuple(out.shape)} of {out.dtype}")
-    yb, ys, yh, yd = out.stride() if len(shape) == 4 else (0, *out.stride())
-    if (yd != 1 and d > 1) or (yb == 0 and batch > 1) or (ys == 0 and seq > 1) or (yh == 0 and heads > 1):
-        raise ValueError("out needs contiguous heads that do not overlap")
-    pos, pos_dt, pb, ps = None, POS_I64, 0, 0
-    if positions is not None:
-        pos_dt = {torch.int32: POS_I32, torch.int64: POS_I64}.get(positions.dtype)
-        if pos_dt is None or not positions.is_cuda:
-            raise TypeError("positions are a CUDA tensor of int32 or int64")
-        if positions.shape == (batch, seq):
-            pb, ps = positions.stride()
-        elif positions.shape == (seq,):
-            ps = positions.stride(0)
-        else:
-            raise ValueError(f"positions are of shape ({seq},) or ({batch}, {seq}), got {tuple(positions.shape)}")
-        pos = positions.data_ptr()
-    _check(_lib.pamm_rotary(X.data_ptr(), xb, xs, xh, out.data_ptr(), yb, ys, yh, batch, seq, heads,
-                            heads if rotated is None else rotated, d, width, dt, PAIRS_ADJACENT if interleaved else PAIRS_HALF,
-                            1 if transposed else 0, table.data_ptr(), rows, pos, pos_dt, pb, ps, first, _raw_stream(stream)),
-           "pamm_rotary")
-    return out
-
-
-def _tensor_list(tensors, what: str):
-    """pamm_tensor entries of a list of tensors.  Memory without gaps is one row whatever its shape and order."""
-    flat = _kept(array.array("q"))
-    for t in tensors:
-        dt = _DTYPES.get(t.dtype)
-        if dt is None or not t.is_cuda:
-            raise TypeError(f"{what} are CUDA tensors of float32 or bfloat16, got {t.dtype} on {t.device}")
-        if t.is_contiguous():
-            size = t.numel()
-            flat.extend((t.data_ptr(), 1, size, size, dt))
-        elif t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= t.shape[1]:
-            flat.extend((t.data_ptr(), t.shape[0], t.shape[1], t.stride(0), dt))
-        elif t.dim() == 2 and t.stride(0) == 1 and t.stride(1) >= t.shape[0]:
-            flat.extend((t.data_ptr(), t.shape[1], t.shape[0], t.stride(1), dt))
-        else:
-            raise ValueError(f"{what} are contiguous, or matrices with contiguous rows or columns; got strides {t.stride()}")
-    return flat
-
-
-def _clip_workspace(workspace, device):
-    return _empty(_grad_norm_bytes(), dtype=torch.uint8, device=device) if workspace is None else workspace
-
-
-@functools.lru_cache(maxsize=1)
-def _grad_norm_bytes() -> int:
-    return _SIZES.pamm_workspace_bytes(WS_GRAD_NORM, 1, 1, 1, 1, F32)
+    The first ``rotated`` heads (None: all) are turned, the others copied; ``table`` is ``rotary_table``'s, whose width
+    ``rot_dim`` has to be where it is given.  ``positions``: int32 or int64 of shape (tokens,) or (batch, tokens); None: ``first`` +
+    the token's index.  ``transposed`` gives the gradient's turn.  ``out=X`` turns in place."""
+    return _binding_on(stream, _binding.rotary, X, table, positions, rotated, rot_dim, interleaved, transposed, first, out)
 
 
 def grad_norm(grads, norm=None, workspace=None, stream=None):
     """The global 2-norm of a list of gradients (fp32 or bf16, mixed), as one fp32 on the device."""
-    grads = _kept(list(grads))
-    flat = _tensor_list(grads, "gradients")
-    device = grads[0].device if grads else torch.device("cuda")
-    with _on(stream):
-        norm = _empty((), dtype=torch.float32, device=device) if norm is None else norm
-        workspace = _clip_workspace(workspace, device)
-    _check(_lib.pamm_grad_norm(flat.buffer_info()[0], len(grads), norm.data_ptr(), workspace.data_ptr(), workspace.numel(),
-                               _raw_stream(stream)), "pamm_grad_norm")
-    return norm
+    return _binding_on(stream, _binding.clip, grads, None, None, norm, workspace)
 
 
 def clip_grad_norm(grads, max_norm: float, out=None, norm=None, workspace=None, stream=None):
     """Scale the gradients by min(1, max_norm / (N + 1e-6)), N their global 2-norm, in place or into the tensors ``out``
     (for instance an optimizer's fp32 buffers); returns N (fp32 on the device) without waiting for it."""
-    grads = _kept(list(grads))
-    flat = _tensor_list(grads, "gradients")
-    flat_out = None
-    if out is not None:
-        out = _kept(list(out))
-        if len(out) != len(grads):
-            raise ValueError(f"{len(grads)} gradients and {len(out)} outputs")
-        flat_out = _tensor_list(out, "outputs")
-        for g, t in zip(grads, out):
-            if g.shape != t.shape or (g.stride() != t.stride() and not (g.is_contiguous() and t.is_contiguous())):
-                flat, flat_out = _same_order(grads, out)
-                break
-    device = grads[0].device if grads else torch.device("cuda")
-    with _on(stream):
-        norm = _empty((), dtype=torch.float32, device=device) if norm is None else norm
-        workspace = _clip_workspace(workspace, device)
-    _check(_lib.pamm_clip_grad_norm(flat.buffer_info()[0], None if flat_out is None else flat_out.buffer_info()[0], len(grads),
-                                    max_norm, norm.data_ptr(), workspace.data_ptr(), workspace.numel(), _raw_stream(stream)),
-           "pamm_clip_grad_norm")
-    return norm
-
-
-def _same_order(grads, out):
-    """The two lists for pairs of tensors that lie in memory differently (a matrix with a row stride and one without)."""
-    flat, flat_out = _kept(array.array("q")), _kept(array.array("q"))
-    for g, t in zip(grads, out):
-        if g.shape != t.shape:
-            raise ValueError(f"a gradient of {tuple(g.shape)} has an output of {tuple(t.shape)}")
-        if g.is_contiguous() and t.is_contiguous():
-            g, t = g.reshape(1, -1), t.reshape(1, -1)
-        elif g.dim() != 2 or g.stride(1) != 1 or t.stride(1) != 1:
-            if g.dim() != 2 or g.stride(0) != 1 or t.stride(0) != 1:
-                raise ValueError("a gradient and its output need the same order of elements in memory")
-            g, t = g.t(), t.t()
-        for row, flat_list in ((g, flat), (t, flat_out)):
-            flat_list.extend((row.data_ptr(), row.shape[0], row.shape[1], row.stride(0), _DTYPES[row.dtype]))
-    return flat, flat_out
+    return _binding_on(stream, _binding.clip, grads, out, float(max_norm), norm, workspace)
 
 
 PROBE_SUM, PROBE_ROWS = 0, 1
