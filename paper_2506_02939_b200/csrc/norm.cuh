@@ -70,104 +70,143 @@ struct NormForwardArgs {
     bool rms;
 };
 
-// Sum over the warps of a row (all of the block's); every thread gets it.  `part`: 32 floats that the caller
-// does not use again before another barrier.
-template <int LANES>
-__device__ __forceinline__ float row_sum(float x, float* part, int warps) {
-    x = warp_sum<LANES>(x);
-    if (LANES < 32 || warps == 1) return x;
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = x;
+// Sums over the warps of a block's rows (all of the block's); every thread gets them.  `part`: [ROWS][32] floats that the
+// caller does not use again before another barrier.
+template <int LANES, int ROWS>
+__device__ __forceinline__ void row_sums(float (&x)[ROWS], float (*part)[32], int warps) {
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) x[r] = warp_sum<LANES>(x[r]);
+    if (LANES < 32 || warps == 1) return;
+    const int lane = threadIdx.x & 31;
+    if (lane == 0) {
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) part[r][threadIdx.x >> 5] = x[r];
+    }
     __syncthreads();
-    return warp_sum((threadIdx.x & 31) < warps ? part[threadIdx.x & 31] : 0.f);
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) x[r] = warp_sum(lane < warps ? part[r][lane] : 0.f);
 }
 
 // Measured on 65536 x 2048 bf16 (268 MB a matrix): the 16-byte copy of the same streams in one-shot blocks runs at 6.5 to
-// 6.7 TB/s, in persistent ones at 6.0, hence one block (or a part of one) per row and no loop over rows.  With 32
-// elements a thread the issue slots are a third used; 8 elements a thread repeat the row's overhead in four times the
-// threads and are for calls with few rows only, where the time is one row's latency.
-template <typename T, typename W, int V, int EPT, int LANES, bool RAGGED>
+// 6.7 TB/s, in persistent ones at 6.0, hence a block (or a part of one) for its rows and no loop over rows.
+// 158 us with the residual addition (6.8 TB/s), 84 without.  A thread may have ROWS = 2 rows, which share its weights (the launch says when).  8 elements a thread repeat the row's
+// overhead in more threads and are for calls with few rows, where the time is one row's latency.
+template <typename T, typename W, int V, int EPT, int LANES, int ROWS, bool RAGGED>
 __global__ void __launch_bounds__(1024)
 norm_forward_kernel(const __grid_constant__ NormForwardArgs a) {
+    static_assert(ROWS == 1 || !RAGGED, "rows of one thread share their offset");
     using P = Piece<T, V>;
     constexpr int PIECES = EPT / V;
-    __shared__ float s_sum[32], s_sq[32];
+    __shared__ float s_sum[ROWS][32], s_sq[ROWS][32];
     grid_dependency_wait();
     grid_launch_dependents();
     const bool one = a.warps == 1;
     const int step = (LANES < 32 ? LANES : 32 * a.warps) * V;
     const int at = (LANES < 32 ? threadIdx.x & (LANES - 1) : one ? threadIdx.x & 31 : threadIdx.x) * V;
-    const int64_t row = one ? (int64_t)blockIdx.x * (blockDim.x / LANES) + threadIdx.x / LANES : blockIdx.x;
+    const int64_t row0 = (one ? (int64_t)blockIdx.x * (blockDim.x / LANES) + threadIdx.x / LANES : blockIdx.x) * ROWS;
     // the lanes behind the last row go along with it, so that shuffles have all of their warp, and write nothing
-    const bool mine = row < a.b;
-    const int64_t i = mine ? row : a.b - 1;
-    const T* x = static_cast<const T*>(a.x) + i * a.ldx;
-    const RowShape shape = row_shape<T, V, RAGGED>(x, a.n, at / V);
+    int64_t row[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) row[r] = row0 + r < a.b ? row0 + r : a.b - 1;
+    const T* x0 = static_cast<const T*>(a.x) + row[0] * a.ldx;
+    const RowShape shape = row_shape<T, V, RAGGED>(x0, a.n, at / V);
     const int lead = shape.lead, end = shape.whole, extra = shape.extra;
-    typename P::Raw xr[PIECES];
-    load_row<T, V, PIECES>(x + lead, at, step, end, xr);
-    float h[EPT], hx = 0.f;
-    if (RAGGED && extra >= 0) hx = to_float(x[extra]);
-    if (a.r) {
-        const T* r = static_cast<const T*>(a.r) + i * a.ldr;
-        typename P::Raw rr[PIECES];
-        load_row<T, V, PIECES>(r + lead, at, step, end, rr);
-        if (RAGGED && extra >= 0) hx += to_float(r[extra]);
+    float h[ROWS][EPT], hx = 0.f;
+    {
+        typename P::Raw xr[ROWS][PIECES];
 #pragma unroll
-        for (int p = 0; p < PIECES; ++p) {
-            float q[V];
-            P::unpack(xr[p], h + p * V);
-            P::unpack(rr[p], q);
+        for (int r = 0; r < ROWS; ++r) load_row<T, V, PIECES>(static_cast<const T*>(a.x) + row[r] * a.ldx + lead, at, step, end, xr[r]);
+        if (RAGGED && extra >= 0) hx = to_float(x0[extra]);
+        if (a.r) {
+            typename P::Raw rr[ROWS][PIECES];
+            const T* r0 = static_cast<const T*>(a.r) + row[0] * a.ldr;
 #pragma unroll
-            for (int e = 0; e < V; ++e) h[p * V + e] += q[e];
+            for (int r = 0; r < ROWS; ++r) load_row<T, V, PIECES>(static_cast<const T*>(a.r) + row[r] * a.ldr + lead, at, step, end, rr[r]);
+            if (RAGGED && extra >= 0) hx += to_float(r0[extra]);
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+#pragma unroll
+                for (int p = 0; p < PIECES; ++p) {
+                    float q[V];
+                    P::unpack(xr[r][p], h[r] + p * V);
+                    P::unpack(rr[r][p], q);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) h[r][p * V + e] += q[e];
+                }
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+                for (int p = 0; p < PIECES; ++p) P::unpack(xr[r][p], h[r] + p * V);
         }
-    } else {
-#pragma unroll
-        for (int p = 0; p < PIECES; ++p) P::unpack(xr[p], h + p * V);
     }
-    if (a.h && mine) {
-        T* ho = static_cast<T*>(a.h) + i * a.ldh;
+    if (a.h) {
 #pragma unroll
-        for (int p = 0; p < PIECES; ++p)
-            if (at + p * step < end) P::store(ho + lead + at + p * step, h + p * V);
-        if (RAGGED && extra >= 0) ho[extra] = from_float<T>(hx);
+        for (int r = 0; r < ROWS; ++r) {
+            if (row0 + r >= a.b) continue;
+            T* ho = static_cast<T*>(a.h) + row[r] * a.ldh;
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p)
+                if (at + p * step < end) P::store(ho + lead + at + p * step, h[r] + p * V);
+            if (RAGGED && extra >= 0) ho[extra] = from_float<T>(hx);
+        }
     }
     const float inv_n = 1.f / (float)a.n;
-    float mean = 0.f;
+    float mean[ROWS], rstd[ROWS];
     if (!a.rms) {
-        float2 sum = make_float2(hx, 0.f);
 #pragma unroll
-        for (int e = 0; e < EPT; e += 2) sum = add2(sum, make_float2(h[e], h[e + 1]));
-        mean = row_sum<LANES>(sum.x + sum.y, s_sum, a.warps) * inv_n;
-        const float2 minus = twice(-mean);
+        for (int r = 0; r < ROWS; ++r) {
+            float2 sum = make_float2(RAGGED ? hx : 0.f, 0.f);
 #pragma unroll
-        for (int p = 0; p < PIECES; ++p) {
-            if (at + p * step < end) {          // what lies outside the row stays 0
-                if constexpr (V == 1) {
-                    h[p] -= mean;
-                } else {
+            for (int e = 0; e < EPT; e += 2) sum = add2(sum, make_float2(h[r][e], h[r][e + 1]));
+            mean[r] = sum.x + sum.y;
+        }
+        row_sums<LANES>(mean, s_sum, a.warps);
 #pragma unroll
-                    for (int e = p * V; e < p * V + V; e += 2) {
-                        const float2 d = add2(make_float2(h[e], h[e + 1]), minus);
-                        h[e] = d.x; h[e + 1] = d.y;
+        for (int r = 0; r < ROWS; ++r) {
+            mean[r] *= inv_n;
+            const float2 minus = twice(-mean[r]);
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) {
+                if (at + p * step < end) {          // what lies outside the row stays 0
+                    if constexpr (V == 1) {
+                        h[r][p] -= mean[r];
+                    } else {
+#pragma unroll
+                        for (int e = p * V; e < p * V + V; e += 2) {
+                            const float2 d = add2(make_float2(h[r][e], h[r][e + 1]), minus);
+                            h[r][e] = d.x; h[r][e + 1] = d.y;
+                        }
                     }
                 }
             }
         }
-        if (extra >= 0) hx -= mean;
+        if (extra >= 0) hx -= mean[0];
     }
-    float2 sq = make_float2(hx * hx, 0.f);
 #pragma unroll
-    for (int e = 0; e < EPT; e += 2) sq = fma2(make_float2(h[e], h[e + 1]), make_float2(h[e], h[e + 1]), sq);
-    const float rstd = rsqrtf(row_sum<LANES>(sq.x + sq.y, s_sq, a.warps) * inv_n + a.eps);
-    if (!mine) return;
-    if (at == 0) {
-        if (a.mean) a.mean[i] = mean;
-        if (a.rstd) a.rstd[i] = rstd;
+    for (int r = 0; r < ROWS; ++r) {
+        float2 sq = make_float2(RAGGED ? hx * hx : 0.f, 0.f);
+#pragma unroll
+        for (int e = 0; e < EPT; e += 2) {
+            const float2 d = make_float2(h[r][e], h[r][e + 1]);
+            sq = fma2(d, d, sq);
+        }
+        rstd[r] = sq.x + sq.y;
     }
-    T* y = static_cast<T*>(a.y) + i * a.ldy;
+    row_sums<LANES>(rstd, s_sq, a.warps);
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        rstd[r] = rsqrtf(rstd[r] * inv_n + a.eps);
+        if (at == 0 && row0 + r < a.b) {
+            if (a.mean) a.mean[row[r]] = a.rms ? 0.f : mean[r];
+            if (a.rstd) a.rstd[row[r]] = rstd[r];
+        }
+    }
     const W *w = static_cast<const W*>(a.w), *c = static_cast<const W*>(a.c);
-    if (RAGGED && extra >= 0)
-        y[extra] = from_float<T>(fmaf(hx * rstd, w ? to_float(w[extra]) : 1.f, c ? to_float(c[extra]) : 0.f));
+    if (RAGGED && extra >= 0 && row0 < a.b)
+        static_cast<T*>(a.y)[row[0] * a.ldy + extra] =
+            from_float<T>(fmaf(hx * rstd[0], w ? to_float(w[extra]) : 1.f, c ? to_float(c[extra]) : 0.f));
     const bool w_vec = (reinterpret_cast<uintptr_t>(w + lead) & 15) == 0, c_vec = (reinterpret_cast<uintptr_t>(c + lead) & 15) == 0;
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
@@ -175,25 +214,27 @@ norm_forward_kernel(const __grid_constant__ NormForwardArgs a) {
         if (at + p * step >= end) continue;
         float q[V], k[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) q[e] = 1.f;
+        for (int e = 0; e < V; ++e) {
+            q[e] = 1.f;
+            k[e] = 0.f;
+        }
         if (w) load_row_weights<W, V, RAGGED>(w + col, w_vec, q);
-        if (c) {
-            load_row_weights<W, V, RAGGED>(c + col, c_vec, k);
-        } else {
+        if (c) load_row_weights<W, V, RAGGED>(c + col, c_vec, k);
 #pragma unroll
-            for (int e = 0; e < V; ++e) k[e] = 0.f;
-        }
-        if constexpr (V == 1) {
-            q[0] = fmaf(h[p] * rstd, q[0], k[0]);
-        } else {
+        for (int r = 0; r < ROWS; ++r) {
+            float y[V];
+            if constexpr (V == 1) {
+                y[0] = fmaf(h[r][p] * rstd[r], q[0], k[0]);
+            } else {
 #pragma unroll
-            for (int e = 0; e < V; e += 2) {
-                const float2 u = mul2(make_float2(h[p * V + e], h[p * V + e + 1]), twice(rstd));
-                const float2 v = fma2(u, make_float2(q[e], q[e + 1]), make_float2(k[e], k[e + 1]));
-                q[e] = v.x; q[e + 1] = v.y;
+                for (int e = 0; e < V; e += 2) {
+                    const float2 u = mul2(make_float2(h[r][p * V + e], h[r][p * V + e + 1]), twice(rstd[r]));
+                    const float2 v = fma2(u, make_float2(q[e], q[e + 1]), make_float2(k[e], k[e + 1]));
+                    y[e] = v.x; y[e + 1] = v.y;
+                }
             }
+            if (row0 + r < a.b) P::store(static_cast<T*>(a.y) + row[r] * a.ldy + col, y);
         }
-        P::store(y + col, q);
     }
 }
 
@@ -423,48 +464,46 @@ norm_backward_kernel(const __grid_constant__ NormBackwardArgs a) {
         stage = stage == STAGES - 1 ? 0 : stage + 1;
     }
     if (!a.part) return;
-    float* part = a.part + (int64_t)blockIdx.x * 2 * a.n;
-    if (a.groups == 1) {
-#pragma unroll
-        for (int p = 0; p < PIECES; ++p) {
-            if (at + p * step >= end) continue;
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const int col = lead + at + p * step + e;
-                part[col] = dw[p * V + e];
-                if (SHIFT) part[a.n + col] = dc[p * V + e];
-            }
-        }
-        if (RAGGED && extra >= 0) {
-            part[extra] = dwx;
-            if (SHIFT) part[a.n + extra] = dcx;
-        }
-        return;
-    }
-    // the groups' sums one after the other, in the place of the ring, whose last copies (of no row) are through
+    // the groups' sums one after the other, in the place of the ring, whose last copies (of no row) are through; from there they
+    // go out in whole sectors
     float* cols = reinterpret_cast<float*>(s_ring);
+    float* cols_c = cols + ((a.n + 3) & ~3);
     copy_wait<0>();
     __syncthreads();
+    const auto put = [](float* to, const float* x, bool add, bool vec) {
+        if (V % 4 == 0 && vec) {
+#pragma unroll
+            for (int e = 0; e < V; e += 4) {
+                float4* q = reinterpret_cast<float4*>(to + e);
+                const float4 old = add ? *q : make_float4(0.f, 0.f, 0.f, 0.f);
+                *q = make_float4(old.x + x[e], old.y + x[e + 1], old.z + x[e + 2], old.w + x[e + 3]);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) to[e] = (add ? to[e] : 0.f) + x[e];
+        }
+    };
     for (int k = 0; k < a.groups; ++k) {
         if (k == group) {
 #pragma unroll
             for (int p = 0; p < PIECES; ++p) {
+                const int col = lead + at + p * step;
                 if (at + p * step >= end) continue;
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const int col = lead + at + p * step + e;
-                    cols[col] = dw[p * V + e] + (k ? cols[col] : 0.f);
-                    if (SHIFT) cols[a.n + col] = dc[p * V + e] + (k ? cols[a.n + col] : 0.f);
-                }
+                put(cols + col, dw + p * V, k > 0, lead % 4 == 0);
+                if (SHIFT) put(cols_c + col, dc + p * V, k > 0, lead % 4 == 0);
             }
             if (RAGGED && extra >= 0) {
                 cols[extra] = dwx + (k ? cols[extra] : 0.f);
-                if (SHIFT) cols[a.n + extra] = dcx + (k ? cols[a.n + extra] : 0.f);
+                if (SHIFT) cols_c[extra] = dcx + (k ? cols_c[extra] : 0.f);
             }
         }
         __syncthreads();
     }
-    for (int i = threadIdx.x; i < (SHIFT ? 2 : 1) * a.n; i += blockDim.x) part[i] = cols[i];
+    float* part = a.part + (int64_t)blockIdx.x * 2 * a.n;
+    for (int i = threadIdx.x; i < a.n; i += blockDim.x) {
+        part[i] = cols[i];
+        if (SHIFT) part[a.n + i] = cols_c[i];
+    }
 }
 
 constexpr int NB_WIDE_THREADS = 256;
@@ -474,7 +513,7 @@ template <typename T, int V>
 __global__ void __launch_bounds__(NB_WIDE_THREADS)
 norm_backward_row_kernel(const __grid_constant__ NormBackwardArgs a) {
     using P = Piece<T, V>;
-    __shared__ float s_gu[32], s_g[32];
+    __shared__ float s_sums[2][32];
     grid_dependency_wait();
     grid_launch_dependents();
     const int64_t row = blockIdx.x;
@@ -495,8 +534,10 @@ norm_backward_row_kernel(const __grid_constant__ NormBackwardArgs a) {
         }
     }
     const float inv_n = 1.f / (float)a.n;
-    gu = row_sum<32>(gu, s_gu, NB_WIDE_THREADS / 32) * inv_n;
-    g = a.rms ? 0.f : row_sum<32>(g, s_g, NB_WIDE_THREADS / 32) * inv_n;
+    float sums[2] = {gu, g};
+    row_sums<32>(sums, s_sums, NB_WIDE_THREADS / 32);
+    gu = sums[0] * inv_n;
+    g = a.rms ? 0.f : sums[1] * inv_n;
     T* dx = static_cast<T*>(a.dx) + row * a.lddx;
     const T* dh = a.dh ? static_cast<const T*>(a.dh) + row * a.lddh : nullptr;
     for (int col = threadIdx.x * V; col < a.n; col += NB_WIDE_THREADS * V) {
@@ -536,33 +577,46 @@ norm_backward_columns_kernel(const __grid_constant__ NormBackwardArgs a) {
     part[a.n] = dc;
 }
 
-// The partial sums of all ranges, added in a fixed order: 32 columns a block, 32 strands of the ranges.
-__global__ void __launch_bounds__(1024)
+// The partial sums of all ranges, added in a fixed order: 8 columns (a sector) a block, 64 strands of the ranges.
+constexpr int NB_FINISH_COLS = 8, NB_FINISH_THREADS = 512;
+__global__ void __launch_bounds__(NB_FINISH_THREADS)
 norm_backward_finish_kernel(const __grid_constant__ NormBackwardArgs a) {
-    __shared__ float s_part[2][32][33];
+    constexpr int STRANDS = NB_FINISH_THREADS / NB_FINISH_COLS, WARPS = NB_FINISH_THREADS / 32;
+    __shared__ float2 s_part[WARPS][NB_FINISH_COLS];
     grid_dependency_wait();
     grid_launch_dependents();
-    const int lane = threadIdx.x & 31, strand = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
+    const int c = threadIdx.x % NB_FINISH_COLS, strand = threadIdx.x / NB_FINISH_COLS, col = blockIdx.x * NB_FINISH_COLS + c;
     float dw = 0.f, dc = 0.f;
     if (col < a.n) {
-        for (int s = strand; s < a.splits; s += 32) {
+#pragma unroll 4
+        for (int s = strand; s < a.splits; s += STRANDS) {
             const float* part = a.part + (int64_t)s * 2 * a.n + col;
             dw += part[0];
             if (a.dc) dc += part[a.n];
         }
     }
-    s_part[0][strand][lane] = dw;
-    s_part[1][strand][lane] = dc;
-    __syncthreads();
-    if (strand > 1) return;
-    // the first warp finishes dw, the second dc
-    void* out = strand == 0 ? a.dw : a.dc;
-    if (!out || col >= a.n) return;
-    float sum = 0.f;
 #pragma unroll
-    for (int s = 0; s < 32; ++s) sum += s_part[strand][s][lane];
-    if (a.dw_bf16) static_cast<__nv_bfloat16*>(out)[col] = __float2bfloat16_rn(sum);
-    else static_cast<float*>(out)[col] = sum;
+    for (int o = NB_FINISH_COLS; o < 32; o *= 2) {          // the strands of a warp
+        dw += __shfl_xor_sync(0xffffffffu, dw, o);
+        dc += __shfl_xor_sync(0xffffffffu, dc, o);
+    }
+    if ((threadIdx.x & 31) < NB_FINISH_COLS) s_part[threadIdx.x >> 5][c] = make_float2(dw, dc);
+    __syncthreads();
+    if (threadIdx.x >= NB_FINISH_COLS || col >= a.n) return;
+    dw = dc = 0.f;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) {
+        dw += s_part[w][c].x;
+        dc += s_part[w][c].y;
+    }
+    if (a.dw) {
+        if (a.dw_bf16) static_cast<__nv_bfloat16*>(a.dw)[col] = __float2bfloat16_rn(dw);
+        else static_cast<float*>(a.dw)[col] = dw;
+    }
+    if (a.dc) {
+        if (a.dw_bf16) static_cast<__nv_bfloat16*>(a.dc)[col] = __float2bfloat16_rn(dc);
+        else static_cast<float*>(a.dc)[col] = dc;
+    }
 }
 
 }  // namespace pamm

@@ -570,24 +570,30 @@ RowAccess row_access(const RowMatrix (&m)[N], int64_t n, size_t es, bool weights
     return same ? RowAccess::ragged : RowAccess::elements;
 }
 
-// Elements a thread: few while the rows do not fill the device (a row's latency is what counts), else 32.  Both sides
-// measured: 65536 x 2048 bf16 takes 83 us with 32 and 110 us with 8.
-template <typename T, typename W, int V, bool RAGGED>
+template <typename T, typename W, int V, int EPT, int LANES, int ROWS, bool RAGGED>
 pamm_status launch_norm_forward(NormForwardArgs a, cudaStream_t st) {
-    const int n = a.n;
-    const int64_t thin_warps = (n + 255) / 256;               // of a row at 8 elements a thread
-    const int ept = thin_warps <= 32 && (thin_warps == 1 || a.b * thin_warps <= 8 * sm_count()) ? 8 : n <= 512 || (V == 1 && n <= 16384) ? 16 : 32;
-    a.warps = (n + 32 * ept - 1) / (32 * ept);
-    const int lanes = ept > 8 || n > 128 ? 32 : n > 64 || RAGGED ? 16 : 8;      // a ragged row needs 16 for its ends
-    const int threads = a.warps > 1 ? 32 * a.warps : a.b * lanes >= 256 ? 256 : (int)round_up(a.b * lanes, 32);
-    const int64_t rows_per_block = a.warps > 1 ? 1 : threads / lanes;
-    const dim3 grid((unsigned)((a.b + rows_per_block - 1) / rows_per_block));
-    if (lanes == 8) launch(norm_forward_kernel<T, W, V, 8, RAGGED ? 16 : 8, RAGGED>, grid, dim3(threads), 0, st, true, a);
-    else if (lanes == 16) launch(norm_forward_kernel<T, W, V, 8, 16, RAGGED>, grid, dim3(threads), 0, st, true, a);
-    else if (ept == 8) launch(norm_forward_kernel<T, W, V, 8, 32, RAGGED>, grid, dim3(threads), 0, st, true, a);
-    else if (ept == 16) launch(norm_forward_kernel<T, W, V, 16, 32, RAGGED>, grid, dim3(threads), 0, st, true, a);
-    else launch(norm_forward_kernel<T, W, V, 32, 32, RAGGED>, grid, dim3(threads), 0, st, true, a);
+    a.warps = (a.n + LANES * EPT - 1) / (LANES * EPT);
+    const int64_t jobs = (a.b + ROWS - 1) / ROWS;
+    const int threads = a.warps > 1 ? 32 * a.warps : jobs * LANES >= 256 ? 256 : (int)round_up(jobs * LANES, 32);
+    const int64_t jobs_per_block = a.warps > 1 ? 1 : threads / LANES;
+    launch(norm_forward_kernel<T, W, V, EPT, LANES, ROWS, RAGGED>, dim3((unsigned)((jobs + jobs_per_block - 1) / jobs_per_block)), dim3(threads),
+           0, st, true, a);
     return launch_status();
+}
+// Elements and rows a thread: 8 of one row while the rows do not fill the device (8 warps an SM), then as many as registers hold.
+template <typename T, typename W, int V, bool RAGGED>
+pamm_status launch_norm_forward(const NormForwardArgs& a, cudaStream_t st) {
+    if (a.n <= 64 && !RAGGED) return launch_norm_forward<T, W, V, 8, RAGGED ? 16 : 8, 1, RAGGED>(a, st);
+    if (a.n <= 128) return launch_norm_forward<T, W, V, 8, 16, 1, RAGGED>(a, st);        // a ragged row needs 16 lanes for its ends
+    const int64_t thin_warps = (a.n + 255) / 256;
+    if (thin_warps <= 32 && (thin_warps == 1 || a.b * thin_warps <= 8 * sm_count())) return launch_norm_forward<T, W, V, 8, 32, 1, RAGGED>(a, st);
+    // Two rows a thread where the weights weigh: narrow rows, and fp32 weights (beside bf16 rows, with a bias too).  Both sides measured, one
+    // row and two: 262144 x 512 bf16 111 and 97 us; 65536 x 2048 bf16 with fp32 weights and bias 124 and 102, with bf16 ones 93 and
+    // 98, with bf16 weights alone 84 and 89; 32768 x 2048 fp32 85 and 81.
+    if constexpr (V > 1 && !RAGGED)
+        if ((a.n <= 512 || (a.n <= 4096 && sizeof(W) == 4 && (sizeof(T) == 4 || a.c))) && a.b * ((a.n + 511) / 512) >= 64 * sm_count()) return launch_norm_forward<T, W, V, 16, 32, 2, RAGGED>(a, st);
+    if (a.n <= 512 || (V == 1 && a.n <= 16384)) return launch_norm_forward<T, W, V, 16, 32, 1, RAGGED>(a, st);
+    return launch_norm_forward<T, W, V, 32, 32, 1, RAGGED>(a, st);
 }
 template <typename T, typename W>
 pamm_status launch_norm_forward(const NormForwardArgs& a, RowAccess access, cudaStream_t st) {
@@ -605,7 +611,7 @@ pamm_status launch_norm_backward_fused(NormBackwardArgs& a, cudaStream_t st) {
     while (RAGGED && (a.period * turn) % 16 != 0) a.period *= 2;
     const int threads = 32 * a.warps * a.groups;
     const size_t ring = V > 1 ? (size_t)norm_stages<T, EPT>() * (a.dh ? 3 : 2) * (EPT / V) * threads * 16 : 0;
-    const size_t smem = std::max(ring, a.groups > 1 ? (size_t)2 * a.n * 4 : 0);
+    const size_t smem = std::max(ring, (size_t)2 * round_up(a.n, 4) * 4);
     const auto kernel = !a.rms || a.dc ? norm_backward_kernel<T, V, EPT, true, RAGGED> : norm_backward_kernel<T, V, EPT, false, RAGGED>;
     if (!ensure_dynamic_smem((const void*)kernel, smem)) return PAMM_ERR_CUDA;
     const int64_t want = ((a.b + a.period - 1) / a.period + a.groups - 1) / a.groups;      // blocks of each phase
@@ -618,7 +624,7 @@ template <typename T>
 pamm_status launch_norm_backward(NormBackwardArgs a, RowAccess access, cudaStream_t st) {
     constexpr int V = Vec16<T>::N;
     const bool sums = a.dw || a.dc;
-    const dim3 finish_grid((unsigned)((a.n + 31) / 32));
+    const dim3 finish_grid((unsigned)((a.n + NB_FINISH_COLS - 1) / NB_FINISH_COLS));
     // 32 bytes of each matrix a thread, twice that where the row is wider than 16 such warps
     constexpr int E = 2 * V;
     const bool fused = access == RowAccess::elements ? a.n <= 512 * E : a.n <= 1024 * E;
@@ -639,7 +645,7 @@ pamm_status launch_norm_backward(NormBackwardArgs a, RowAccess access, cudaStrea
         launch(norm_backward_columns_kernel<T>, dim3((unsigned)((a.n + NB_COL_THREADS - 1) / NB_COL_THREADS), (unsigned)a.splits),
                dim3(NB_COL_THREADS), 0, st, true, a);
     }
-    if (sums) launch(norm_backward_finish_kernel, finish_grid, dim3(1024), 0, st, true, a);
+    if (sums) launch(norm_backward_finish_kernel, finish_grid, dim3(NB_FINISH_THREADS), 0, st, true, a);
     if (a.b && !fused) {
         if (access == RowAccess::whole) launch(norm_backward_row_kernel<T, V>, dim3((unsigned)a.b), dim3(NB_WIDE_THREADS), 0, st, true, a);
         else launch(norm_backward_row_kernel<T, 1>, dim3((unsigned)a.b), dim3(NB_WIDE_THREADS), 0, st, true, a);
