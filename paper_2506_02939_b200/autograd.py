@@ -8,6 +8,10 @@ Backward: the weight gradient is ``ApproxMM(C, alpha, f, dZ) = C^T B~`` through 
 the input gradient ``dX = dZ W^T`` is exact (for bf16 layers the library's tensor-core product
 ``pamm_linear_backward_input``, else torch).  Meant for the fused Q|K|V projection: ``W`` is n x m
 with m = |Q| + |K| + |V|, as in the paper's notation.
+
+Around it: ``Norm`` (layer norm or its root-mean-square form, with the residual addition), whose
+output is the projection's input; ``rotary`` on the heads of the projection's output; and
+``clip_grad_norm_`` for the end of a training step.
 """
 from __future__ import annotations
 
@@ -42,8 +46,9 @@ class PammLinearFunction(torch.autograd.Function):
         one_kernel = (X2.dtype == torch.bfloat16 and Wd.dtype == torch.bfloat16 and 16 <= k <= 4096 and n >= 8 and m >= 8
                       and Wd.is_contiguous() and (m * 2) % 16 == 0 and Wd.data_ptr() % 16 == 0)
         if one_kernel:
-            Z2, _, C, _, f, alpha = pamm.linear_forward(X2, Wd, int(k), int(seed), sort_products=sp, f_dtype=f_dtype)
-            Z = Z2.reshape(*X.shape[:-1], m)
+            # made in its final shape, not as a view of a matrix: what follows may then work on it in place
+            Z = torch.empty((*X.shape[:-1], m), dtype=X2.dtype, device=X2.device)
+            _, _, C, _, f, alpha = pamm.linear_forward(X2, Wd, int(k), int(seed), Z=Z.view(-1, m), sort_products=sp, f_dtype=f_dtype)
         else:
             Z = X @ W
             _, C, _, f, alpha = pamm.compress_fused(X2, int(k), int(seed), sort_products=sp, f_dtype=f_dtype)
@@ -91,3 +96,99 @@ class PammLinear(torch.nn.Module):
         k = max(1, min(b, math.ceil(self.r * b)))
         self.calls += 1                                   # fresh generators every step (Appendix "LLaMA-1B Runtime Breakdown")
         return PammLinearFunction.apply(X, self.weight, k, self.seed + self.calls)
+
+
+def _matrix(t: torch.Tensor, n: int) -> torch.Tensor:
+    """(…, n) -> (rows, n) with contiguous rows that do not overlap; copied only where it has to be."""
+    t2 = t.reshape(-1, n)
+    rows = t2.shape[0]
+    if (n > 1 and t2.stride(1) != 1) or (rows > 1 and t2.stride(0) < n):
+        t2 = t2.contiguous()
+    return t2
+
+
+class NormFunction(torch.autograd.Function):
+    """``pamm.norm_forward`` / ``norm_backward`` on the last dimension.  With a residual the outputs are (y, h) and the gradient
+    that reaches h joins dX in the same pass.  Saved: the normalised row (h, or X), mean, rstd and the weight."""
+
+    @staticmethod
+    def forward(ctx, X, weight, bias, residual, eps, rms):
+        n = X.shape[-1]
+        X2 = _matrix(X.detach(), n)
+        R2 = None if residual is None else _matrix(residual.detach().to(X.dtype), n)
+        w, c = (None if p is None else p.detach() for p in (weight, bias))
+        Y, H, mean, rstd = pamm.norm_forward(X2, w, c, residual=R2, eps=eps, rms=rms)
+        ctx.save_for_backward(H, mean, rstd, weight)
+        ctx.has_bias, ctx.shape, ctx.has_residual = bias is not None, X.shape, residual is not None
+        ctx.vector_type = weight.dtype if weight is not None else bias.dtype if bias is not None else X.dtype
+        ctx.set_materialize_grads(False)
+        Y = Y.reshape(X.shape)
+        return Y if residual is None else (Y, H.reshape(X.shape))
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dY, dH=None):
+        H, mean, rstd, weight = ctx.saved_tensors
+        n = H.shape[1]
+        if dY is None and dH is None:
+            return (None,) * 6
+        if dY is None:
+            dY = torch.zeros(ctx.shape, dtype=H.dtype, device=H.device)
+        need_w, need_c = ctx.needs_input_grad[1], ctx.needs_input_grad[2]
+        dX, dw, dc = pamm.norm_backward(_matrix(dY.to(H.dtype), n), H, mean, rstd, None if weight is None else weight.detach(),
+                                        bias=need_c, dH=None if dH is None else _matrix(dH.to(H.dtype), n),
+                                        need_dw=need_w or need_c, dw_dtype=ctx.vector_type)
+        dX = dX.reshape(ctx.shape)
+        return (dX if ctx.needs_input_grad[0] else None, dw if need_w else None, dc if need_c else None,
+                dX if ctx.has_residual and ctx.needs_input_grad[3] else None, None, None)
+
+
+class Norm(torch.nn.Module):
+    """Layer norm over the last dimension, or (``rms``) its root-mean-square form without a bias.  ``norm(X)`` gives y;
+    ``norm(X, residual)`` gives (y, h = X + residual), the step from one block of a network to the next."""
+
+    def __init__(self, n: int, eps: float = 1e-5, rms: bool = False, bias: bool | None = None, dtype=torch.bfloat16, device="cuda"):
+        super().__init__()
+        self.weight = torch.nn.Parameter(torch.ones(n, dtype=dtype, device=device))
+        with_bias = not rms if bias is None else bias
+        self.bias = torch.nn.Parameter(torch.zeros(n, dtype=dtype, device=device)) if with_bias else None
+        self.eps, self.rms = float(eps), bool(rms)
+
+    def forward(self, X, residual=None):
+        return NormFunction.apply(X, self.weight, self.bias, residual, self.eps, self.rms)
+
+
+class RotaryFunction(torch.autograd.Function):
+    """``pamm.rotary`` and its transposed turn.  Nothing but the table and the positions is kept."""
+
+    @staticmethod
+    def forward(ctx, X, table, positions, rotated, interleaved, first, inplace):
+        ctx.save_for_backward(table, positions)
+        ctx.how = dict(rotated=rotated, interleaved=interleaved, first=first)
+        if inplace:
+            ctx.mark_dirty(X)
+        Xd = X.detach()
+        out = pamm.rotary(Xd, table, positions, out=Xd if inplace else None, **ctx.how)
+        return X if inplace else out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dY):
+        table, positions = ctx.saved_tensors
+        if dY.shape[-1] > 1 and dY.stride(-1) != 1:
+            dY = dY.contiguous()
+        return pamm.rotary(dY, table, positions, transposed=True, **ctx.how), None, None, None, None, None, None
+
+
+def rotary(X, table, positions=None, rotated=None, interleaved: bool = False, first: int = 0, inplace: bool = False):
+    """Rotary positions on the first ``rotated`` heads of X, (tokens, heads, head_dim) or (batch, tokens, heads, head_dim), as
+    ``pamm.rotary``; the other heads (V of the fused row) pass through.  ``inplace`` turns X itself, which must not be a leaf
+    or needed by the backward pass of what made it (the projection's output is neither)."""
+    return RotaryFunction.apply(X, table, positions, rotated, interleaved, first, inplace)
+
+
+def clip_grad_norm_(parameters, max_norm: float):
+    """Clip the parameters' gradients in place to a global norm of ``max_norm``; returns the norm before (fp32 on the
+    device), without waiting for it.  Parameters without a gradient are left out."""
+    grads = [p.grad for p in parameters if p.grad is not None]
+    return pamm.clip_grad_norm(grads, max_norm)
