@@ -274,7 +274,7 @@ __device__ __forceinline__ uint4 load_shared16(uint32_t smem) {
     return v;
 }
 
-constexpr int NB_MAX_GROUPS = 8;
+constexpr int NB_WARPS = 8;             // of a block, but where a row has more
 // Rows in shared memory: four of at most 32 bytes a thread and matrix (98 KB for three matrices and 256 threads, two blocks an
 // SM), two where the rows are wider.
 template <typename T, int EPT> __host__ __device__ constexpr int norm_stages() { return EPT * (int)sizeof(T) > 32 ? 2 : 4; }
@@ -285,18 +285,20 @@ template <typename T, int EPT> __host__ __device__ constexpr int norm_stages() {
 // needed for it (elements, V = 1, are loaded when they are needed).  Rows whose offset into the 16-byte grid differs go to
 // different blocks (`period` of them: the row distance's phase repeats after so many rows), which keeps the columns of
 // a thread fixed there too.
+// LANES < 32: narrow rows, several to a warp, each a group.
 // SHIFT: layer norm, or a bias in the RMS form; otherwise there is neither a mean nor dc.
-template <typename T, int V, int EPT, bool SHIFT, bool RAGGED>
+template <typename T, int V, int EPT, int LANES, bool SHIFT, bool RAGGED>
 __global__ void __launch_bounds__(512)
 norm_backward_kernel(const __grid_constant__ NormBackwardArgs a) {
     using P = Piece<T, V>;
     constexpr int PIECES = EPT / V, STAGES = norm_stages<T, EPT>();
-    __shared__ float2 s_part[2][NB_MAX_GROUPS][16];
+    __shared__ float2 s_part[2][NB_WARPS][16];
     extern __shared__ __align__(16) unsigned char s_ring[];       // [stage][array][piece][thread] 16 bytes; in the end [2][n] sums
     grid_dependency_wait();
     grid_launch_dependents();
-    const int group = threadIdx.x / (32 * a.warps), t = threadIdx.x - group * 32 * a.warps;
-    const int step = 32 * a.warps * V, at = t * V, lane = threadIdx.x & 31, warp = t >> 5;
+    const int width = LANES < 32 ? LANES : 32 * a.warps;         // threads of a group
+    const int group = threadIdx.x / width, t = threadIdx.x - group * width;
+    const int step = width * V, at = t * V, lane = threadIdx.x & 31, warp = t >> 5;
     const int64_t cls = blockIdx.x % a.period;
     const int64_t stride = (int64_t)a.period * a.groups * (gridDim.x / a.period);
     const int64_t first = cls + a.period * ((int64_t)(blockIdx.x / a.period) * a.groups);      // of the block
@@ -364,16 +366,18 @@ norm_backward_kernel(const __grid_constant__ NormBackwardArgs a) {
     for (int k = 0; k < STAGES - 1; ++k) fetch(row + k * stride, k);
     fetch_scalars(row);
     int stage = 0, parity = 0;
-    for (; row < a.b; row += stride, parity ^= 1) {        // a group's threads go the same rounds
-        const float s = next_rstd, m = next_mean, yx = next_y, hx = next_h;
+    // a group's threads go the same rounds; where a warp has several groups, all of them as many as its block's first
+    for (; row - (LANES < 32 ? a.period * group : 0) < a.b; row += stride, parity ^= 1) {
+        const bool mine = LANES == 32 || row < a.b;
+        const float s = mine ? next_rstd : 0.f, m = mine ? next_mean : 0.f, yx = next_y, hx = next_h;
         float ux = next_x;
         float u[EPT], g[EPT];
         if constexpr (V > 1) {
             copy_wait<STAGES - 2>();
 #pragma unroll
             for (int p = 0; p < PIECES; ++p) {
-                P::unpack(taken(stage, 0, p), u + p * V);
-                P::unpack(taken(stage, 1, p), g + p * V);
+                P::unpack(mine ? taken(stage, 0, p) : P::zero(), u + p * V);
+                P::unpack(mine ? taken(stage, 1, p) : P::zero(), g + p * V);
             }
         } else {
             typename P::Raw raw[PIECES];
@@ -406,7 +410,7 @@ norm_backward_kernel(const __grid_constant__ NormBackwardArgs a) {
             u[e] = uu.x; u[e + 1] = uu.y; g[e] = gg.x; g[e + 1] = gg.y;
         }
         float gu = gu2.x + gu2.y, gs = g2.x + g2.y, gx = 0.f;
-        if (RAGGED && extra >= 0) {
+        if (RAGGED && extra >= 0 && mine) {
             ux = (ux - m) * s;
             dwx = fmaf(yx, ux, dwx);
             dcx += yx;
@@ -415,11 +419,11 @@ norm_backward_kernel(const __grid_constant__ NormBackwardArgs a) {
             gs += gx;
         }
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
+        for (int o = LANES / 2; o > 0; o >>= 1) {
             gu += __shfl_xor_sync(0xffffffffu, gu, o);
             if (SHIFT) gs += __shfl_xor_sync(0xffffffffu, gs, o);
         }
-        if (a.warps > 1) {          // at most 16; two buffers, so that one barrier a row is enough
+        if (LANES == 32 && a.warps > 1) {          // at most 16; two buffers, so that one barrier a row is enough
             if (lane == 0) s_part[parity][group][warp] = make_float2(gu, gs);
             asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(32 * a.warps) : "memory");
             const float2 v = (lane & 15) < a.warps ? s_part[parity][group][lane & 15] : twice(0.f);
@@ -438,7 +442,7 @@ norm_backward_kernel(const __grid_constant__ NormBackwardArgs a) {
         }
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) {
-            if (at + p * step >= end) continue;
+            if (at + p * step >= end || !mine) continue;
             float q[V], hv[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) hv[e] = 0.f;
@@ -460,10 +464,22 @@ norm_backward_kernel(const __grid_constant__ NormBackwardArgs a) {
             }
             P::store(dx + lead + at + p * step, q);
         }
-        if (RAGGED && extra >= 0) dx[extra] = from_float<T>(fmaf(fmaf(ux, mu, gx + mg), s, hx));
+        if (RAGGED && extra >= 0 && mine) dx[extra] = from_float<T>(fmaf(fmaf(ux, mu, gx + mg), s, hx));
         stage = stage == STAGES - 1 ? 0 : stage + 1;
     }
     if (!a.part) return;
+    if (LANES < 32) {           // a warp's groups have the same columns
+#pragma unroll
+        for (int o = LANES; o < 32; o *= 2) {
+#pragma unroll
+            for (int e = 0; e < EPT; ++e) {
+                dw[e] += __shfl_xor_sync(0xffffffffu, dw[e], o);
+                if (SHIFT) dc[e] += __shfl_xor_sync(0xffffffffu, dc[e], o);
+            }
+            dwx += __shfl_xor_sync(0xffffffffu, dwx, o);
+            dcx += __shfl_xor_sync(0xffffffffu, dcx, o);
+        }
+    }
     // the groups' sums one after the other, in the place of the ring, whose last copies (of no row) are through; from there they
     // go out in whole sectors
     float* cols = reinterpret_cast<float*>(s_ring);
@@ -483,8 +499,9 @@ norm_backward_kernel(const __grid_constant__ NormBackwardArgs a) {
             for (int e = 0; e < V; ++e) to[e] = (add ? to[e] : 0.f) + x[e];
         }
     };
-    for (int k = 0; k < a.groups; ++k) {
-        if (k == group) {
+    const int parts = LANES < 32 ? (int)blockDim.x / 32 : a.groups, mine_of = LANES == 32 ? group : lane < LANES ? (int)threadIdx.x / 32 : -1;
+    for (int k = 0; k < parts; ++k) {
+        if (k == mine_of) {
 #pragma unroll
             for (int p = 0; p < PIECES; ++p) {
                 const int col = lead + at + p * step;

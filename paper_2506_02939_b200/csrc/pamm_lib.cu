@@ -602,22 +602,36 @@ pamm_status launch_norm_forward(const NormForwardArgs& a, RowAccess access, cuda
     return launch_norm_forward<T, W, 1, false>(a, st);
 }
 
-template <typename T, int V, int EPT, bool RAGGED>
+template <typename T, int V, int EPT, int LANES, bool RAGGED>
 pamm_status launch_norm_backward_fused(NormBackwardArgs& a, cudaStream_t st) {
-    a.warps = (a.n + 32 * EPT - 1) / (32 * EPT);
-    a.groups = std::max(1, NB_MAX_GROUPS / a.warps);
+    a.warps = (a.n + LANES * EPT - 1) / (LANES * EPT);
+    const int threads = a.warps > NB_WARPS / 2 ? 32 * a.warps : 32 * a.warps * (NB_WARPS / a.warps);
+    a.groups = threads / (a.warps * LANES);
     const int64_t turn = (a.ldx * (int64_t)sizeof(T)) % 16;
     a.period = 1;
     while (RAGGED && (a.period * turn) % 16 != 0) a.period *= 2;
-    const int threads = 32 * a.warps * a.groups;
     const size_t ring = V > 1 ? (size_t)norm_stages<T, EPT>() * (a.dh ? 3 : 2) * (EPT / V) * threads * 16 : 0;
     const size_t smem = std::max(ring, (size_t)2 * round_up(a.n, 4) * 4);
-    const auto kernel = !a.rms || a.dc ? norm_backward_kernel<T, V, EPT, true, RAGGED> : norm_backward_kernel<T, V, EPT, false, RAGGED>;
-    if (!ensure_dynamic_smem((const void*)kernel, smem)) return PAMM_ERR_CUDA;
+    const auto kernel = !a.rms || a.dc ? norm_backward_kernel<T, V, EPT, LANES, true, RAGGED> : norm_backward_kernel<T, V, EPT, LANES, false, RAGGED>;
+    // the 48 KB that need no asking for hold the kernel's own arrays as well
+    if (!ensure_dynamic_smem((const void*)kernel, smem > 44 * 1024 ? std::max<size_t>(smem, 49 * 1024) : smem)) return PAMM_ERR_CUDA;
     const int64_t want = ((a.b + a.period - 1) / a.period + a.groups - 1) / a.groups;      // blocks of each phase
     a.splits = (int)(a.period * std::min<int64_t>(want, std::max(1, sm_count() * (threads <= 256 ? 2 : 1) / a.period)));
     launch(kernel, dim3((unsigned)a.splits), dim3(threads), smem, st, true, a);
     return launch_status();
+}
+// Elements a thread: 8 of a row of up to 256 in as many lanes as it needs, then 32 bytes of each matrix, and twice that where the row is
+// wider than 16 such warps.
+template <typename T, int V, bool RAGGED>
+pamm_status launch_norm_backward_fused(NormBackwardArgs& a, cudaStream_t st) {
+    constexpr int E = 2 * (int)Vec16<T>::N;
+    if constexpr (V > 1) {
+        if (a.n <= 64 && !RAGGED) return launch_norm_backward_fused<T, V, 8, RAGGED ? 16 : 8, RAGGED>(a, st);
+        if (a.n <= 128) return launch_norm_backward_fused<T, V, 8, 16, RAGGED>(a, st);        // a ragged row needs 16 lanes for its ends
+        if (a.n <= 256) return launch_norm_backward_fused<T, V, 8, 32, RAGGED>(a, st);
+        if (a.n > 512 * E) return launch_norm_backward_fused<T, V, 2 * E, 32, RAGGED>(a, st);
+    }
+    return launch_norm_backward_fused<T, V, E, 32, RAGGED>(a, st);
 }
 
 template <typename T>
@@ -625,18 +639,13 @@ pamm_status launch_norm_backward(NormBackwardArgs a, RowAccess access, cudaStrea
     constexpr int V = Vec16<T>::N;
     const bool sums = a.dw || a.dc;
     const dim3 finish_grid((unsigned)((a.n + NB_FINISH_COLS - 1) / NB_FINISH_COLS));
-    // 32 bytes of each matrix a thread, twice that where the row is wider than 16 such warps
-    constexpr int E = 2 * V;
-    const bool fused = access == RowAccess::elements ? a.n <= 512 * E : a.n <= 1024 * E;
+    const int widest = 1024 * Vec16<T>::N;                        // that 16 warps hold at 32 bytes a thread and matrix
+    const bool fused = a.n <= (access == RowAccess::elements ? widest : 2 * widest);
     a.splits = 0;
     if (fused && a.b) {
-        pamm_status s;
-        if (access == RowAccess::whole)
-            s = a.n <= 512 * E ? launch_norm_backward_fused<T, V, E, false>(a, st) : launch_norm_backward_fused<T, V, 2 * E, false>(a, st);
-        else if (access == RowAccess::ragged)
-            s = a.n <= 512 * E ? launch_norm_backward_fused<T, V, E, true>(a, st) : launch_norm_backward_fused<T, V, 2 * E, true>(a, st);
-        else
-            s = launch_norm_backward_fused<T, 1, E, false>(a, st);
+        const pamm_status s = access == RowAccess::whole    ? launch_norm_backward_fused<T, V, false>(a, st)
+                              : access == RowAccess::ragged ? launch_norm_backward_fused<T, V, true>(a, st)
+                                                            : launch_norm_backward_fused<T, 1, false>(a, st);
         if (s != PAMM_OK) return s;
     } else if (a.b && sums) {
         // rows too wide for registers: the column sums by themselves, before dX may take the place of dY or X

@@ -76,7 +76,7 @@ def test_forward_and_backward_of_all_sizes(b, n, dtype, w_dtype):
 
 
 @pytest.mark.parametrize("b", [1, 2, 31, 147, 149, 1000, 4099, 20000])
-@pytest.mark.parametrize("n,dtype", [(256, BF16), (1024, F32), (2048, BF16)])
+@pytest.mark.parametrize("n,dtype", [(256, BF16), (1024, F32), (2048, BF16), (64, BF16), (40, F32), (128, F32), (100, BF16), (333, BF16)])
 def test_weight_gradients_over_many_rows(b, n, dtype):
     x, _ = rows(b, n, dtype, b)
     dy, _ = rows(b, n, dtype, b + 1, 1e-3)
