@@ -19,7 +19,8 @@ constexpr int GC_UNROLL = 4;            // vectors in flight per thread
 constexpr int GC_BLOCKS_PER_SM = 8;     // of the sum: one wave
 // elements of a chunk: of the sum, by the size of the list; of the scaling
 constexpr int GC_MIN_CHUNK = 4096, GC_MAX_CHUNK = 65536, GC_SCALE_CHUNK = 16384;
-constexpr int GC_SMALL = 24, GC_LARGE = 448;      // list entries per launch: parameters of 1.6 and 29 KB
+// list entries per launch: parameters of 1.8, 7 and 32 KB, which a launch takes 2, 3 and 6 us of host time to hand over
+constexpr int GC_SMALL = 24, GC_MEDIUM = 96, GC_LARGE = 448;
 
 struct GradEntry {
     const void* in;

@@ -548,14 +548,34 @@ namespace {
 
 // Row partition of the norm's column sums, and the scratch that holds their partial sums.
 inline int64_t norm_splits(int64_t b) { return std::max<int64_t>(1, std::min<int64_t>((b + 31) / 32, 2 * sm_count())); }
+// Blocks per SM of the fused backward pass, at most: the registers allow no more where rows are wide.
+inline int norm_backward_blocks(int64_t n) { return n <= 2048 ? 4 : 3; }
 inline size_t norm_backward_ws_bytes(int64_t b, int64_t n) {
-    return (size_t)round_up(std::min<int64_t>(b + 8, 2 * sm_count()) * 2 * n * 4, 256);
+    return (size_t)round_up(std::min<int64_t>(b + 8, norm_backward_blocks(n) * sm_count()) * 2 * n * 4, 256);
 }
 inline int grad_norm_blocks() { return sm_count() * GC_BLOCKS_PER_SM; }
 inline size_t grad_norm_ws_bytes() { return (size_t)round_up((int64_t)grad_norm_blocks() * 8, 256) + 256; }      // and the factor
 
 // An element-aligned row-major matrix of at least one row; leading dimension in elements.
 inline bool matrix_ok(const void* p, int64_t ld, int64_t cols, size_t es) { return p && aligned(p, es) && ld >= cols; }
+
+// How many blocks of a kernel an SM of the current device holds (asked once for each device, kernel and size).
+int blocks_per_sm(const void* kernel, int threads, size_t smem) {
+    static std::mutex mu;
+    static std::map<std::tuple<int, const void*, int, size_t>, int> known;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 1;
+    std::lock_guard<std::mutex> lock(mu);
+    const auto key = std::make_tuple(dev, kernel, threads, smem);
+    const auto it = known.find(key);
+    if (it != known.end()) return it->second;
+    int blocks = 0;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, kernel, threads, smem) != cudaSuccess) {
+        cudaGetLastError();
+        return 1;
+    }
+    return known[key] = blocks;
+}
 
 // How the matrices of a call can be accessed (the three ways are described in norm.cuh).
 enum class RowAccess { whole, ragged, elements };
@@ -616,7 +636,8 @@ pamm_status launch_norm_backward_fused(NormBackwardArgs& a, cudaStream_t st) {
     // the 48 KB that need no asking for hold the kernel's own arrays as well
     if (!ensure_dynamic_smem((const void*)kernel, smem > 44 * 1024 ? std::max<size_t>(smem, 49 * 1024) : smem)) return PAMM_ERR_CUDA;
     const int64_t want = ((a.b + a.period - 1) / a.period + a.groups - 1) / a.groups;      // blocks of each phase
-    a.splits = (int)(a.period * std::min<int64_t>(want, std::max(1, sm_count() * (threads <= 256 ? 2 : 1) / a.period)));
+    const int per_sm = std::max(1, std::min(norm_backward_blocks(a.n), blocks_per_sm((const void*)kernel, threads, smem)));
+    a.splits = (int)(a.period * std::min<int64_t>(want, std::max(1, sm_count() * per_sm / a.period)));
     launch(kernel, dim3((unsigned)a.splits), dim3(threads), smem, st, true, a);
     return launch_status();
 }
@@ -629,7 +650,10 @@ pamm_status launch_norm_backward_fused(NormBackwardArgs& a, cudaStream_t st) {
         if (a.n <= 64 && !RAGGED) return launch_norm_backward_fused<T, V, 8, RAGGED ? 16 : 8, RAGGED>(a, st);
         if (a.n <= 128) return launch_norm_backward_fused<T, V, 8, 16, RAGGED>(a, st);        // a ragged row needs 16 lanes for its ends
         if (a.n <= 256) return launch_norm_backward_fused<T, V, 8, 32, RAGGED>(a, st);
-        if (a.n > 512 * E) return launch_norm_backward_fused<T, V, 2 * E, 32, RAGGED>(a, st);
+        // fp32 with a mean or a bias, measured at 32 and at 64 bytes: 65536 x 1024 149 and 127 us, 16384 x 4096 151 and 123, but 2048 x 512 7.3
+        // and 8.9; without them 120 and 129 us at 65536 x 1024
+        const bool wide32 = sizeof(T) == 4 && (!a.rms || a.dc) && (a.n > 1024 || a.b * a.n > (8 << 20));
+        if (a.n > 512 * E || wide32) return launch_norm_backward_fused<T, V, 2 * E, 32, RAGGED>(a, st);
     }
     return launch_norm_backward_fused<T, V, E, 32, RAGGED>(a, st);
 }
@@ -809,8 +833,10 @@ pamm_status grad_clip(const pamm_tensor* in, const pamm_tensor* out, int64_t cou
     if (!norm || !aligned(norm, 4) || !(max_norm >= 0.0)) return PAMM_ERR_INVALID_ARG;
     if (!workspace || !aligned(workspace, 256) || ws_bytes < grad_norm_ws_bytes()) return PAMM_ERR_WORKSPACE;
     cudaStream_t st = (cudaStream_t)stream;
-    return count <= GC_SMALL ? run_grad_clip<GC_SMALL>(in, out, count, scale, max_norm, norm, (double*)workspace, st)
-                             : run_grad_clip<GC_LARGE>(in, out, count, scale, max_norm, norm, (double*)workspace, st);
+    double* partial = (double*)workspace;
+    if (count <= GC_SMALL) return run_grad_clip<GC_SMALL>(in, out, count, scale, max_norm, norm, partial, st);
+    if (count <= GC_MEDIUM) return run_grad_clip<GC_MEDIUM>(in, out, count, scale, max_norm, norm, partial, st);
+    return run_grad_clip<GC_LARGE>(in, out, count, scale, max_norm, norm, partial, st);
 }
 
 }  // namespace
