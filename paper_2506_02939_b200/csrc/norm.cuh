@@ -116,13 +116,15 @@ norm_forward_kernel(const __grid_constant__ NormForwardArgs a) {
         typename P::Raw xr[ROWS][PIECES];
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) load_row<T, V, PIECES>(static_cast<const T*>(a.x) + row[r] * a.ldx + lead, at, step, end, xr[r]);
-        if (RAGGED && extra >= 0) hx = to_float(x0[extra]);
+        using One = Piece<T, 1>;
+        typename One::Raw x1 = One::zero(), r1 = One::zero();
+        if (RAGGED && extra >= 0) x1 = One::load(x0 + extra);
         if (a.r) {
             typename P::Raw rr[ROWS][PIECES];
             const T* r0 = static_cast<const T*>(a.r) + row[0] * a.ldr;
 #pragma unroll
             for (int r = 0; r < ROWS; ++r) load_row<T, V, PIECES>(static_cast<const T*>(a.r) + row[r] * a.ldr + lead, at, step, end, rr[r]);
-            if (RAGGED && extra >= 0) hx += to_float(r0[extra]);
+            if (RAGGED && extra >= 0) r1 = One::load(r0 + extra);
 #pragma unroll
             for (int r = 0; r < ROWS; ++r) {
 #pragma unroll
@@ -139,6 +141,12 @@ norm_forward_kernel(const __grid_constant__ NormForwardArgs a) {
             for (int r = 0; r < ROWS; ++r)
 #pragma unroll
                 for (int p = 0; p < PIECES; ++p) P::unpack(xr[r][p], h[r] + p * V);
+        }
+        if (RAGGED) {
+            float q;
+            One::unpack(x1, &hx);
+            One::unpack(r1, &q);
+            hx += q;
         }
     }
     if (a.h) {
@@ -242,9 +250,9 @@ struct NormBackwardArgs {
     const void *dy, *x, *w, *dh;
     const float *mean, *rstd;
     void *dx, *dw, *dc;
-    float *part;            // [splits][2][n]: partial sums of dw and dc
+    float *part;            // [splits][2][pitch]: partial sums of dw and dc; the pitch is n in whole sectors
     int64_t lddy, ldx, lddh, lddx, b, rows_per_split;
-    int n, splits, warps, groups, period;
+    int n, pitch, splits, warps, groups, period;
     bool rms, w_bf16, dw_bf16;
 };
 
@@ -278,6 +286,9 @@ constexpr int NB_WARPS = 8;             // of a block, but where a row has more
 // Rows in shared memory: four of at most 32 bytes a thread and matrix (98 KB for three matrices and 256 threads, two blocks an
 // SM), two where the rows are wider.
 template <typename T, int EPT> __host__ __device__ constexpr int norm_stages() { return EPT * (int)sizeof(T) > 32 ? 2 : 4; }
+
+// Floats between the two vectors of a block's sums in shared memory.
+__host__ __device__ constexpr int norm_sums_pitch(int n) { return (n + n / 32 + 4) & ~3; }
 
 // dx and the partial sums of dw (and, SHIFT, of dc) in one pass.  A block has `groups` groups of `warps` warps; a group takes
 // row after row, so that a thread's columns stay the same and their sums stay in its registers.  The rows that follow are
@@ -350,15 +361,17 @@ norm_backward_kernel(const __grid_constant__ NormBackwardArgs a) {
         return r;
     };
     // statistics and the element outside the vectors: one row ahead, in registers
-    float next_mean = 0.f, next_rstd = 0.f, next_x = 0.f, next_y = 0.f, next_h = 0.f;
+    using One = Piece<T, 1>;
+    float next_mean = 0.f, next_rstd = 0.f;
+    typename One::Raw next_x = One::zero(), next_y = One::zero(), next_h = One::zero();
     auto fetch_scalars = [&](int64_t r) {
         if (r >= a.b) return;
         next_rstd = a.rstd[r];
         if (SHIFT && !a.rms) next_mean = a.mean[r];
         if (RAGGED && extra >= 0) {
-            next_x = to_float(X[r * a.ldx + extra]);
-            next_y = to_float(DY[r * a.lddy + extra]);
-            if (DH) next_h = to_float(DH[r * a.lddh + extra]);
+            next_x = One::load(X + r * a.ldx + extra);
+            next_y = One::load(DY + r * a.lddy + extra);
+            if (DH) next_h = One::load(DH + r * a.lddh + extra);
         }
     };
     int64_t row = first + a.period * group;
@@ -369,8 +382,11 @@ norm_backward_kernel(const __grid_constant__ NormBackwardArgs a) {
     // a group's threads go the same rounds; where a warp has several groups, all of them as many as its block's first
     for (; row - (LANES < 32 ? a.period * group : 0) < a.b; row += stride, parity ^= 1) {
         const bool mine = LANES == 32 || row < a.b;
-        const float s = mine ? next_rstd : 0.f, m = mine ? next_mean : 0.f, yx = next_y, hx = next_h;
-        float ux = next_x;
+        const float s = mine ? next_rstd : 0.f, m = mine ? next_mean : 0.f;
+        float ux, yx, hx;
+        One::unpack(next_x, &ux);
+        One::unpack(next_y, &yx);
+        One::unpack(next_h, &hx);
         float u[EPT], g[EPT];
         if constexpr (V > 1) {
             copy_wait<STAGES - 2>();
@@ -483,20 +499,26 @@ norm_backward_kernel(const __grid_constant__ NormBackwardArgs a) {
     // the groups' sums one after the other, in the place of the ring, whose last copies (of no row) are through; from there they
     // go out in whole sectors
     float* cols = reinterpret_cast<float*>(s_ring);
-    float* cols_c = cols + ((a.n + 3) & ~3);
+    // by vectors where the row's offset allows it; else element by element, with a gap every 32 so that lanes hit different banks
+    const bool vec = V % 4 == 0 && lead % 4 == 0;
+    const auto place = [vec](int col) { return vec ? col : col + (col >> 5); };
+    float* cols_c = cols + norm_sums_pitch(a.n);
     copy_wait<0>();
     __syncthreads();
-    const auto put = [](float* to, const float* x, bool add, bool vec) {
+    const auto put = [&](float* to, int col, const float* x, bool add) {
         if (V % 4 == 0 && vec) {
 #pragma unroll
             for (int e = 0; e < V; e += 4) {
-                float4* q = reinterpret_cast<float4*>(to + e);
+                float4* q = reinterpret_cast<float4*>(to + col + e);
                 const float4 old = add ? *q : make_float4(0.f, 0.f, 0.f, 0.f);
                 *q = make_float4(old.x + x[e], old.y + x[e + 1], old.z + x[e + 2], old.w + x[e + 3]);
             }
         } else {
 #pragma unroll
-            for (int e = 0; e < V; ++e) to[e] = (add ? to[e] : 0.f) + x[e];
+            for (int e = 0; e < V; ++e) {
+                float* q = to + place(col + e);
+                *q = (add ? *q : 0.f) + x[e];
+            }
         }
     };
     const int parts = LANES < 32 ? (int)blockDim.x / 32 : a.groups, mine_of = LANES == 32 ? group : lane < LANES ? (int)threadIdx.x / 32 : -1;
@@ -506,20 +528,21 @@ norm_backward_kernel(const __grid_constant__ NormBackwardArgs a) {
             for (int p = 0; p < PIECES; ++p) {
                 const int col = lead + at + p * step;
                 if (at + p * step >= end) continue;
-                put(cols + col, dw + p * V, k > 0, lead % 4 == 0);
-                if (SHIFT) put(cols_c + col, dc + p * V, k > 0, lead % 4 == 0);
+                put(cols, col, dw + p * V, k > 0);
+                if (SHIFT) put(cols_c, col, dc + p * V, k > 0);
             }
             if (RAGGED && extra >= 0) {
-                cols[extra] = dwx + (k ? cols[extra] : 0.f);
-                if (SHIFT) cols_c[extra] = dcx + (k ? cols_c[extra] : 0.f);
+                const int q = place(extra);
+                cols[q] = dwx + (k ? cols[q] : 0.f);
+                if (SHIFT) cols_c[q] = dcx + (k ? cols_c[q] : 0.f);
             }
         }
         __syncthreads();
     }
-    float* part = a.part + (int64_t)blockIdx.x * 2 * a.n;
+    float* part = a.part + (int64_t)blockIdx.x * 2 * a.pitch;
     for (int i = threadIdx.x; i < a.n; i += blockDim.x) {
-        part[i] = cols[i];
-        if (SHIFT) part[a.n + i] = cols_c[i];
+        part[i] = cols[place(i)];
+        if (SHIFT) part[a.pitch + i] = cols_c[place(i)];
     }
 }
 
@@ -589,9 +612,9 @@ norm_backward_columns_kernel(const __grid_constant__ NormBackwardArgs a) {
         dw = fmaf(d, u, dw);
         dc += d;
     }
-    float* part = a.part + (int64_t)blockIdx.y * 2 * a.n + col;
+    float* part = a.part + (int64_t)blockIdx.y * 2 * a.pitch + col;
     part[0] = dw;
-    part[a.n] = dc;
+    part[a.pitch] = dc;
 }
 
 // The partial sums of all ranges, added in a fixed order: 8 columns (a sector) a block, 64 strands of the ranges.
@@ -607,9 +630,9 @@ norm_backward_finish_kernel(const __grid_constant__ NormBackwardArgs a) {
     if (col < a.n) {
 #pragma unroll 4
         for (int s = strand; s < a.splits; s += STRANDS) {
-            const float* part = a.part + (int64_t)s * 2 * a.n + col;
+            const float* part = a.part + (int64_t)s * 2 * a.pitch + col;
             dw += part[0];
-            if (a.dc) dc += part[a.n];
+            if (a.dc) dc += part[a.pitch];
         }
     }
 #pragma unroll

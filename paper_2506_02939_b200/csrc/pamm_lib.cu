@@ -551,7 +551,7 @@ inline int64_t norm_splits(int64_t b) { return std::max<int64_t>(1, std::min<int
 // Blocks per SM of the fused backward pass, at most: the registers allow no more where rows are wide.
 inline int norm_backward_blocks(int64_t n) { return n <= 2048 ? 4 : 3; }
 inline size_t norm_backward_ws_bytes(int64_t b, int64_t n) {
-    return (size_t)round_up(std::min<int64_t>(b + 8, norm_backward_blocks(n) * sm_count()) * 2 * n * 4, 256);
+    return (size_t)round_up(std::min<int64_t>(b + 8, norm_backward_blocks(n) * sm_count()) * 2 * round_up(n, 8) * 4, 256);
 }
 inline int grad_norm_blocks() { return sm_count() * GC_BLOCKS_PER_SM; }
 inline size_t grad_norm_ws_bytes() { return (size_t)round_up((int64_t)grad_norm_blocks() * 8, 256) + 256; }      // and the factor
@@ -631,7 +631,7 @@ pamm_status launch_norm_backward_fused(NormBackwardArgs& a, cudaStream_t st) {
     a.period = 1;
     while (RAGGED && (a.period * turn) % 16 != 0) a.period *= 2;
     const size_t ring = V > 1 ? (size_t)norm_stages<T, EPT>() * (a.dh ? 3 : 2) * (EPT / V) * threads * 16 : 0;
-    const size_t smem = std::max(ring, (size_t)2 * round_up(a.n, 4) * 4);
+    const size_t smem = std::max(ring, (size_t)2 * norm_sums_pitch(a.n) * 4);
     const auto kernel = !a.rms || a.dc ? norm_backward_kernel<T, V, EPT, LANES, true, RAGGED> : norm_backward_kernel<T, V, EPT, LANES, false, RAGGED>;
     // the 48 KB that need no asking for hold the kernel's own arrays as well
     if (!ensure_dynamic_smem((const void*)kernel, smem > 44 * 1024 ? std::max<size_t>(smem, 49 * 1024) : smem)) return PAMM_ERR_CUDA;
@@ -890,7 +890,7 @@ pamm_status pamm_norm_backward(pamm_norm_kind kind, const void* dY, int64_t lddy
     a.dy = dY; a.x = X; a.w = w; a.dh = dH; a.mean = mean; a.rstd = rstd; a.dx = dX; a.dw = dw; a.dc = dc;
     a.part = dw || dc ? (float*)workspace : nullptr;
     a.lddy = lddy; a.ldx = ldx; a.lddh = lddh; a.lddx = lddx; a.b = b; a.rows_per_split = 0;
-    a.n = (int)n; a.splits = a.warps = a.groups = a.period = 0;
+    a.n = (int)n; a.pitch = (int)round_up(n, 8); a.splits = a.warps = a.groups = a.period = 0;
     a.rms = rms; a.w_bf16 = w_dt == PAMM_BF16; a.dw_bf16 = dw_dt == PAMM_BF16;
     const RowMatrix all[] = {{X, ldx}, {dY, lddy}, {dH, lddh}, {dX, lddx}};
     const RowAccess access = row_access(all, n, es, aligned(w, 16));
