@@ -27,7 +27,8 @@ struct GradEntry {
     void* out;
     int64_t rows, cols, ld_in, ld_out;
     int64_t first_chunk, pieces;          // chunks before this entry; of a wide row
-    int in_bf16, out_bf16;
+    short in_bf16, out_bf16;
+    int off;                            // one row: elements from the 16-byte boundary below its start, on which chunks are cut
 };
 template <int CAP>
 struct GradList {
@@ -54,11 +55,37 @@ __device__ __forceinline__ int lead_elements(const T* p, int len) {
 // A square in 64 bits.  Conversions and products keep up with memory (bf16 from HBM: 6.0 TB/s with them, 6.5 without).
 __device__ __forceinline__ void add_square(double& acc, float x) { acc = fma((double)x, (double)x, acc); }
 
-// Calls one(i) for the elements of a span of `len` before its first and behind its last whole vector, and many(first element, k)
-// for its groups of G elements, k = 0 .. U - 1 of them at a time and then one at a time; by STEP threads, this being number t.
-template <int G, int U, int STEP, typename Load, typename Use, typename One>
-__device__ __forceinline__ void walk_span(int lead, int len, int t, Load load, Use use, One one) {
-    const int groups = (len - lead) / G, done = lead + groups * G;
+// The up to V - 1 elements of a span before its first and behind its last 16-byte vector (or group of G elements): thread t has one
+// of each.  Loaded before the vectors and used after them.
+template <typename T, int G>
+struct Ends {
+    using One = Piece<T, 1>;
+    int lead, groups, done, len, t;
+    typename One::Raw a, b;
+    __device__ __forceinline__ Ends(const T* p, int len_, int t_) : lead(lead_elements(p, len_)), len(len_), t(t_), a(One::zero()), b(One::zero()) {
+        groups = (len - lead) / G;
+        done = lead + groups * G;
+        if (t < lead) a = One::load(p + t);
+        if (t < len - done) b = One::load(p + done + t);
+    }
+    template <typename F>
+    __device__ __forceinline__ void use(F f) const {          // f(element, its place)
+        float v;
+        if (t < lead) {
+            One::unpack(a, &v);
+            f(v, t);
+        }
+        if (t < len - done) {
+            One::unpack(b, &v);
+            f(v, done + t);
+        }
+    }
+};
+
+// load(k, first element) and use(k, first element) for a span's groups of G elements by STEP threads: U of them at a time, then half
+// as many, at last one.  (With U loads under a condition each, every load is waited for by itself: half the speed.)
+template <int G, int U, int STEP, typename Load, typename Use>
+__device__ __forceinline__ void walk_span(int lead, int groups, int t, Load load, Use use) {
     int i = t;
     for (; i + (U - 1) * STEP < groups; i += U * STEP) {
 #pragma unroll
@@ -66,27 +93,23 @@ __device__ __forceinline__ void walk_span(int lead, int len, int t, Load load, U
 #pragma unroll
         for (int k = 0; k < U; ++k) use(k, lead + (i + k * STEP) * G);
     }
-    for (; i < groups; i += STEP) {
-        load(0, lead + i * G);
-        use(0, lead + i * G);
-    }
-    if (t < lead) one(t);
-    if (t < len - done) one(done + t);
+    if constexpr (U > 1) walk_span<G, U / 2, STEP>(lead, groups, i, load, use);
 }
 
 template <typename T, int STEP>
 __device__ __forceinline__ void add_squares(const T* p, int len, int t, double& sum) {
     constexpr int V = Vec16<T>::N, U = STEP > 32 ? GC_UNROLL : 1;
     using P = Piece<T, V>;
+    const Ends<T, V> ends(p, len, t);
     typename P::Raw r[U];
-    walk_span<V, U, STEP>(lead_elements(p, len), len, t, [&](int k, int at) { r[k] = P::load(p + at); },
+    walk_span<V, U, STEP>(ends.lead, ends.groups, t, [&](int k, int at) { r[k] = P::load(p + at); },
                           [&](int k, int) {
                               float v[V];
                               P::unpack(r[k], v);
 #pragma unroll
                               for (int e = 0; e < V; ++e) add_square(sum, v[e]);
-                          },
-                          [&](int at) { add_square(sum, to_float(p[at])); });
+                          });
+    ends.use([&](float v, int) { add_square(sum, v); });
 }
 
 // The factor as a product of two, so that one below fp32's normal range keeps its digits; and whether it is 1.
@@ -100,22 +123,22 @@ template <typename TI, typename TO, int STEP>
 __device__ __forceinline__ void scale_span(const TI* p, TO* q, int len, const GradFactor& f, int t) {
     // G elements at a time: 16 bytes on the side of the wider type, so that a warp's accesses have no gaps on either
     constexpr int G = Vec16<TI>::N < Vec16<TO>::N ? Vec16<TI>::N : Vec16<TO>::N, U = STEP > 32 ? GC_UNROLL : 1;
-    const int lead = lead_elements(p, len);
-    if ((reinterpret_cast<uintptr_t>(q + lead) & 15) != 0) {        // the output is not on a 16-byte boundary there
+    if ((reinterpret_cast<uintptr_t>(q + lead_elements(p, len)) & 15) != 0) {        // the output is not on a 16-byte boundary there
         for (int i = t; i < len; i += STEP) q[i] = from_float<TO>(f(to_float(p[i])));
         return;
     }
+    const Ends<TI, G> ends(p, len, t);
     const uint64_t policy = evict_first_policy();       // what is yet to be read stays in L2
     typename Piece<TI, G>::Raw r[U];
-    walk_span<G, U, STEP>(lead, len, t, [&](int k, int at) { r[k] = Piece<TI, G>::load(p + at); },
+    walk_span<G, U, STEP>(ends.lead, ends.groups, t, [&](int k, int at) { r[k] = Piece<TI, G>::load(p + at); },
                           [&](int k, int at) {
                               float v[G];
                               Piece<TI, G>::unpack(r[k], v);
 #pragma unroll
                               for (int e = 0; e < G; ++e) v[e] = f(v[e]);
                               Piece<TO, G>::store(q + at, v, policy);
-                          },
-                          [&](int at) { q[at] = from_float<TO>(f(to_float(p[at]))); });
+                          });
+    ends.use([&](float v, int at) { q[at] = from_float<TO>(f(v)); });
 }
 
 __device__ __forceinline__ double block_sum_double(double x, double* part) {
@@ -146,8 +169,8 @@ __device__ __forceinline__ void for_each_span(const GradList<CAP>& list, bool ba
         const GradEntry& g = list.e[lo];
         const int64_t local = at - g.first_chunk;
         if (g.rows == 1) {
-            const int64_t col = local * list.chunk;
-            wide(g, (int64_t)0, col, (int)(g.cols - col < list.chunk ? g.cols - col : list.chunk));
+            const int64_t from = local * list.chunk - g.off, to = from + list.chunk, col = from < 0 ? 0 : from;
+            wide(g, (int64_t)0, col, (int)((to < g.cols ? to : g.cols) - col));
         } else if (g.cols >= list.chunk) {
             const int64_t row = local / g.pieces, col = (local - row * g.pieces) * list.chunk;
             wide(g, row, col, (int)(g.cols - col < list.chunk ? g.cols - col : list.chunk));

@@ -779,7 +779,8 @@ int64_t fill_grad_list(GradList<CAP>& list, const pamm_tensor* in, const pamm_te
         e.ld_out = o.ld;
         e.first_chunk = list.chunks;
         e.pieces = (e.cols + chunk - 1) / chunk;
-        list.chunks += grad_chunks(e.rows, e.cols, chunk);
+        e.off = dense ? (int)(reinterpret_cast<uintptr_t>(t.data) % 16 / esize((pamm_dtype)t.dt)) : 0;
+        list.chunks += grad_chunks(e.rows, e.cols + e.off, chunk);
     }
     return at;
 }
