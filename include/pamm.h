@@ -1,6 +1,7 @@
 /*
  * pamm.h -- C ABI of the B200 (sm_100a) library for the hot path of
- * Point-Approximate Matrix Multiplication (PAMM) on one fused Q|K|V layer.
+ * Point-Approximate Matrix Multiplication (PAMM) on one fused Q|K|V layer, and for
+ * the operators around that layer in a training step (at the end of this file).
  *
  * Notation follows the paper: A = X is the saved layer input (b tokens x n
  * hidden), B = dY = [dQ|dK|dV] is the upstream gradient (b x m), C holds k

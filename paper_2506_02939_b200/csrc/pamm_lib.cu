@@ -955,6 +955,10 @@ pamm_status pamm_rotary(const void* X, int64_t x_batch, int64_t x_token, int64_t
     if (positions ? !aligned(positions, pos_type == PAMM_POS_I64 ? 8 : 4)
                   : first < 0 || first > table_rows || seq > table_rows - first)
         return PAMM_ERR_INVALID_ARG;
+    // a distance between the only one of something and its next does not count
+    if (batch == 1) x_batch = y_batch = 0;
+    if (seq == 1) x_token = y_token = 0;
+    if (heads == 1) x_head = y_head = 0;
     // the same matrix in and out is turned in place; other overlaps are the caller's error
     const bool in_place = X == (const void*)Y;
     if (in_place && (x_batch != y_batch || x_token != y_token || x_head != y_head)) return PAMM_ERR_INVALID_ARG;

@@ -1,7 +1,8 @@
 """Thin binding to the PAMM CUDA library (C ABI declared in ``include/pamm.h``).
 
 Argument marshalling only: every step of the path runs in the library's kernels.
-torch is used for device memory and streams.  Importing this module fails
+torch is used for device memory and streams.  The calls of the path are marshalled here
+through ctypes, those of the operators around the projection in ``_binding``.  Importing this module fails
 loudly when the library has not been built; there is no CPU fallback.
 """
 from __future__ import annotations
