@@ -19,6 +19,7 @@
 #pragma once
 #include "pamm_common.cuh"
 #include "row_io.cuh"
+#include "sm100_ptx.cuh"
 
 namespace pamm {
 
@@ -253,6 +254,7 @@ struct NormBackwardArgs {
     float *part;            // [splits][2][pitch]: partial sums of dw and dc; the pitch is n in whole sectors
     int64_t lddy, ldx, lddh, lddx, b, rows_per_split;
     int n, pitch, splits, warps, groups, period;
+    int cluster, slice;     // blocks that share a row, and the elements of it that each has
     bool rms, w_bf16, dw_bf16;
 };
 
@@ -297,26 +299,48 @@ __host__ __device__ constexpr int norm_sums_pitch(int n) { return (n + n / 32 + 
 // different blocks (`period` of them: the row distance's phase repeats after so many rows), which keeps the columns of
 // a thread fixed there too.
 // LANES < 32: narrow rows, several to a warp, each a group.
+// CLUSTER: rows wider than a block holds, over the blocks of a cluster, which have a slice of the columns each.  Every warp sends its part of a
+// row's two sums to all blocks (st.async, counted on an mbarrier; a cluster barrier a row instead waits for the stores of dx too:
+// 4096 x 16384 bf16 121 us).
 // SHIFT: layer norm, or a bias in the RMS form; otherwise there is neither a mean nor dc.
-template <typename T, int V, int EPT, int LANES, bool SHIFT, bool RAGGED>
+template <typename T, int V, int EPT, int LANES, bool SHIFT, bool RAGGED, bool CLUSTER>
 __global__ void __launch_bounds__(512)
 norm_backward_kernel(const __grid_constant__ NormBackwardArgs a) {
     using P = Piece<T, V>;
     constexpr int PIECES = EPT / V, STAGES = norm_stages<T, EPT>();
-    __shared__ float2 s_part[2][NB_WARPS][16];
+    __shared__ __align__(8) float2 s_part[2][NB_WARPS][16];         // of the groups' or the cluster's blocks' warps
+    __shared__ uint64_t s_bar[2];
+    __shared__ int s_abort;
     extern __shared__ __align__(16) unsigned char s_ring[];       // [stage][array][piece][thread] 16 bytes; in the end [2][n] sums
     grid_dependency_wait();
     grid_launch_dependents();
     const int width = LANES < 32 ? LANES : 32 * a.warps;         // threads of a group
     const int group = threadIdx.x / width, t = threadIdx.x - group * width;
     const int step = width * V, at = t * V, lane = threadIdx.x & 31, warp = t >> 5;
-    const int64_t cls = blockIdx.x % a.period;
-    const int64_t stride = (int64_t)a.period * a.groups * (gridDim.x / a.period);
-    const int64_t first = cls + a.period * ((int64_t)(blockIdx.x / a.period) * a.groups);      // of the block
+    const int rank = CLUSTER ? (int)ptx::cluster_ctarank() : 0;
+    const unsigned unit = CLUSTER ? blockIdx.x / a.cluster : blockIdx.x, units = CLUSTER ? gridDim.x / a.cluster : gridDim.x;
+    const int64_t cls = unit % a.period;
+    const int64_t stride = (int64_t)a.period * a.groups * (units / a.period);
+    const int64_t first = cls + a.period * ((int64_t)(unit / a.period) * a.groups);      // of the block
     const T *X = static_cast<const T*>(a.x), *DY = static_cast<const T*>(a.dy), *DH = static_cast<const T*>(a.dh);
     const RowShape shape = row_shape<T, V, RAGGED>(X + cls * a.ldx, a.n, t);
-    const int lead = shape.lead, end = shape.whole, extra = shape.extra;
+    // of a cluster's blocks each has the vectors of its slice, the first the elements before them, the last those behind
+    const int lead = shape.lead + (CLUSTER ? rank * a.slice : 0);
+    const int end = CLUSTER ? max(0, min(shape.whole - rank * a.slice, a.slice)) : shape.whole;
+    const int extra = CLUSTER && rank != (t < 8 ? 0 : a.cluster - 1) ? -1 : shape.extra;
     const float inv_n = 1.f / (float)a.n;
+    const uint32_t sent = a.cluster * a.warps * sizeof(float2);         // to a block of a cluster, for a row
+    if constexpr (CLUSTER) {
+        if (threadIdx.x == 0) {
+            s_abort = 0;
+            for (int k = 0; k < 2; ++k) {
+                ptx::mbar_init(&s_bar[k], 1);
+                ptx::mbar_arrive_expect_tx(&s_bar[k], sent);
+            }
+            ptx::fence_barrier_init();
+        }
+        ptx::cluster_sync_all();            // every block's barriers are there before anything is sent to them
+    }
     float w[EPT], dw[EPT], dc[SHIFT ? EPT : 1];
     float wx = 0.f, dwx = 0.f, dcx = 0.f;
 #pragma unroll
@@ -378,7 +402,8 @@ norm_backward_kernel(const __grid_constant__ NormBackwardArgs a) {
 #pragma unroll
     for (int k = 0; k < STAGES - 1; ++k) fetch(row + k * stride, k);
     fetch_scalars(row);
-    int stage = 0, parity = 0;
+    int stage = 0, parity = 0, phase = 0;
+    bool fine = true;
     // a group's threads go the same rounds; where a warp has several groups, all of them as many as its block's first
     for (; row - (LANES < 32 ? a.period * group : 0) < a.b; row += stride, parity ^= 1) {
         const bool mine = LANES == 32 || row < a.b;
@@ -439,7 +464,24 @@ norm_backward_kernel(const __grid_constant__ NormBackwardArgs a) {
             gu += __shfl_xor_sync(0xffffffffu, gu, o);
             if (SHIFT) gs += __shfl_xor_sync(0xffffffffu, gs, o);
         }
-        if (LANES == 32 && a.warps > 1) {          // at most 16; two buffers, so that one barrier a row is enough
+        if constexpr (CLUSTER) {
+            if (lane < a.cluster)
+                ptx::store_async_pair(ptx::map_to_rank(&s_part[parity][rank][warp], lane), gu, gs, ptx::map_to_rank(&s_bar[parity], lane));
+            fine = __all_sync(0xffffffffu, ptx::mbar_wait_cluster(&s_bar[parity], phase, &s_abort));
+            if (!fine) break;
+            if (threadIdx.x == 0) ptx::mbar_arrive_expect_tx(&s_bar[parity], sent);         // for the row after the next
+            phase ^= parity;
+            // two buffers: a warp writes one again when it has every warp's part of the row between, sent after this one was read
+            float2 v = twice(0.f);
+            if ((lane & 15) < a.warps)
+                for (int r = 0; r < a.cluster; ++r) v = add2(v, s_part[parity][r][lane & 15]);
+            gu = v.x; gs = v.y;
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) {
+                gu += __shfl_xor_sync(0xffffffffu, gu, o);
+                if (SHIFT) gs += __shfl_xor_sync(0xffffffffu, gs, o);
+            }
+        } else if (LANES == 32 && a.warps > 1) {          // at most 16; two buffers, so that one barrier a row is enough
             if (lane == 0) s_part[parity][group][warp] = make_float2(gu, gs);
             asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(32 * a.warps) : "memory");
             const float2 v = (lane & 15) < a.warps ? s_part[parity][group][lane & 15] : twice(0.f);
@@ -483,6 +525,11 @@ norm_backward_kernel(const __grid_constant__ NormBackwardArgs a) {
         if (RAGGED && extra >= 0 && mine) dx[extra] = from_float<T>(fmaf(fmaf(ux, mu, gx + mg), s, hx));
         stage = stage == STAGES - 1 ? 0 : stage + 1;
     }
+    if constexpr (CLUSTER) {
+        copy_wait<0>();
+        ptx::cluster_sync_all();            // nothing is sent to a block that has left
+        if (!fine && lane == 0) raise_status(DEV_TIMEOUT);
+    }
     if (!a.part) return;
     if (LANES < 32) {           // a warp's groups have the same columns
 #pragma unroll
@@ -499,10 +546,12 @@ norm_backward_kernel(const __grid_constant__ NormBackwardArgs a) {
     // the groups' sums one after the other, in the place of the ring, whose last copies (of no row) are through; from there they
     // go out in whole sectors
     float* cols = reinterpret_cast<float*>(s_ring);
+    // the block's columns: all of them, or from its slice's first (and the row's first) to the next slice's (and the row's last)
+    const int from = CLUSTER && rank > 0 ? lead : 0, behind = CLUSTER && rank < a.cluster - 1 ? lead + a.slice : a.n;
     // by vectors where the row's offset allows it; else element by element, with a gap every 32 so that lanes hit different banks
-    const bool vec = V % 4 == 0 && lead % 4 == 0;
+    const bool vec = V % 4 == 0 && (lead - from) % 4 == 0;
     const auto place = [vec](int col) { return vec ? col : col + (col >> 5); };
-    float* cols_c = cols + norm_sums_pitch(a.n);
+    float* cols_c = cols + norm_sums_pitch(CLUSTER ? a.slice + 16 : a.n);
     copy_wait<0>();
     __syncthreads();
     const auto put = [&](float* to, int col, const float* x, bool add) {
@@ -526,33 +575,33 @@ norm_backward_kernel(const __grid_constant__ NormBackwardArgs a) {
         if (k == mine_of) {
 #pragma unroll
             for (int p = 0; p < PIECES; ++p) {
-                const int col = lead + at + p * step;
+                const int col = lead - from + at + p * step;
                 if (at + p * step >= end) continue;
                 put(cols, col, dw + p * V, k > 0);
                 if (SHIFT) put(cols_c, col, dc + p * V, k > 0);
             }
             if (RAGGED && extra >= 0) {
-                const int q = place(extra);
+                const int q = place(extra - from);
                 cols[q] = dwx + (k ? cols[q] : 0.f);
                 if (SHIFT) cols_c[q] = dcx + (k ? cols_c[q] : 0.f);
             }
         }
         __syncthreads();
     }
-    float* part = a.part + (int64_t)blockIdx.x * 2 * a.pitch;
-    for (int i = threadIdx.x; i < a.n; i += blockDim.x) {
+    float* part = a.part + (int64_t)unit * 2 * a.pitch + from;
+    for (int i = threadIdx.x; i < behind - from; i += blockDim.x) {
         part[i] = cols[place(i)];
         if (SHIFT) part[a.pitch + i] = cols_c[place(i)];
     }
 }
 
-constexpr int NB_WIDE_THREADS = 256;
+constexpr int NB_WIDE_THREADS = 512;
 
+// Matrices whose rows are aligned differently, in rows too wide for a block's registers: three launches, element by element.
 // One row per block, read twice (the second time from the caches): the two sums, then dx.
-template <typename T, int V>
+template <typename T>
 __global__ void __launch_bounds__(NB_WIDE_THREADS)
 norm_backward_row_kernel(const __grid_constant__ NormBackwardArgs a) {
-    using P = Piece<T, V>;
     __shared__ float s_sums[2][32];
     grid_dependency_wait();
     grid_launch_dependents();
@@ -560,36 +609,23 @@ norm_backward_row_kernel(const __grid_constant__ NormBackwardArgs a) {
     const T* x = static_cast<const T*>(a.x) + row * a.ldx;
     const T* dy = static_cast<const T*>(a.dy) + row * a.lddy;
     const float mean = a.rms ? 0.f : a.mean[row], rstd = a.rstd[row];
-    float gu = 0.f, g = 0.f;
-    for (int col = threadIdx.x * V; col < a.n; col += NB_WIDE_THREADS * V) {
-        float xv[V], dv[V], w[V];
-        P::unpack(P::load(x + col), xv);
-        P::unpack(P::load(dy + col), dv);
-        load_any_weights<V, false>(a.w, a.w_bf16, col, w);
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            const float q = dv[e] * w[e];
-            g += q;
-            gu = fmaf(q, (xv[e] - mean) * rstd, gu);
-        }
+    float sums[2] = {0.f, 0.f};
+    for (int col = threadIdx.x; col < a.n; col += NB_WIDE_THREADS) {
+        float w;
+        load_any_weights<1, false>(a.w, a.w_bf16, col, &w);
+        const float g = to_float(dy[col]) * w;
+        sums[0] = fmaf(g, (to_float(x[col]) - mean) * rstd, sums[0]);
+        sums[1] += g;
     }
-    const float inv_n = 1.f / (float)a.n;
-    float sums[2] = {gu, g};
     row_sums<32>(sums, s_sums, NB_WIDE_THREADS / 32);
-    gu = sums[0] * inv_n;
-    g = a.rms ? 0.f : sums[1] * inv_n;
+    const float gu = sums[0] / (float)a.n, g = a.rms ? 0.f : sums[1] / (float)a.n;
     T* dx = static_cast<T*>(a.dx) + row * a.lddx;
     const T* dh = a.dh ? static_cast<const T*>(a.dh) + row * a.lddh : nullptr;
-    for (int col = threadIdx.x * V; col < a.n; col += NB_WIDE_THREADS * V) {
-        float xv[V], dv[V], w[V], hv[V] = {};
-        P::unpack(P::load(x + col), xv);
-        P::unpack(P::load(dy + col), dv);
-        load_any_weights<V, false>(a.w, a.w_bf16, col, w);
-        if (dh) P::unpack(P::load(dh + col), hv);
-#pragma unroll
-        for (int e = 0; e < V; ++e)
-            dv[e] = fmaf(rstd, dv[e] * w[e] - g - (xv[e] - mean) * rstd * gu, hv[e]);
-        P::store(dx + col, dv);
+    for (int col = threadIdx.x; col < a.n; col += NB_WIDE_THREADS) {
+        float w;
+        load_any_weights<1, false>(a.w, a.w_bf16, col, &w);
+        const float d = to_float(dy[col]) * w - g - (to_float(x[col]) - mean) * rstd * gu;
+        dx[col] = from_float<T>(fmaf(rstd, d, dh ? to_float(dh[col]) : 0.f));
     }
 }
 

@@ -559,22 +559,51 @@ inline size_t grad_norm_ws_bytes() { return (size_t)round_up((int64_t)grad_norm_
 // An element-aligned row-major matrix of at least one row; leading dimension in elements.
 inline bool matrix_ok(const void* p, int64_t ld, int64_t cols, size_t es) { return p && aligned(p, es) && ld >= cols; }
 
-// How many blocks of a kernel an SM of the current device holds (asked once for each device, kernel and size).
-int blocks_per_sm(const void* kernel, int threads, size_t smem) {
+cudaLaunchConfig_t cluster_config(unsigned clusters, int cluster, int threads, size_t smem, cudaStream_t st, cudaLaunchAttribute (&attr)[2]) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(clusters * cluster);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = cluster;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cfg;
+}
+template <typename... P, typename... A>
+void launch_clusters(void (*kern)(P...), unsigned clusters, int cluster, int threads, size_t smem, cudaStream_t st, A... args) {
+    cudaLaunchAttribute attr[2];
+    const cudaLaunchConfig_t cfg = cluster_config(clusters, cluster, threads, smem, st, attr);
+    cudaLaunchKernelEx(&cfg, kern, P(args)...);
+    g_launches += 1;
+}
+
+// How many blocks of a kernel an SM of the current device holds, and how many clusters the device (asked once for each device,
+// kernel and size).
+int resident(const void* kernel, int threads, size_t smem, int cluster) {
     static std::mutex mu;
-    static std::map<std::tuple<int, const void*, int, size_t>, int> known;
+    static std::map<std::tuple<int, const void*, int, size_t, int>, int> known;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return 1;
     std::lock_guard<std::mutex> lock(mu);
-    const auto key = std::make_tuple(dev, kernel, threads, smem);
+    const auto key = std::make_tuple(dev, kernel, threads, smem, cluster);
     const auto it = known.find(key);
     if (it != known.end()) return it->second;
-    int blocks = 0;
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, kernel, threads, smem) != cudaSuccess) {
+    int count = 0;
+    cudaLaunchAttribute attr[2];
+    cudaLaunchConfig_t cfg = cluster_config(1, cluster, threads, smem, nullptr, attr);
+    cfg.numAttrs = 1;
+    const cudaError_t e = cluster == 1 ? cudaOccupancyMaxActiveBlocksPerMultiprocessor(&count, kernel, threads, smem)
+                                       : cudaOccupancyMaxActiveClusters(&count, kernel, &cfg);
+    if (e != cudaSuccess) {
         cudaGetLastError();
         return 1;
     }
-    return known[key] = blocks;
+    return known[key] = std::max(1, count);
 }
 
 // How the matrices of a call can be accessed (the three ways are described in norm.cuh).
@@ -624,36 +653,57 @@ pamm_status launch_norm_forward(const NormForwardArgs& a, RowAccess access, cuda
 
 template <typename T, int V, int EPT, int LANES, bool RAGGED>
 pamm_status launch_norm_backward_fused(NormBackwardArgs& a, cudaStream_t st) {
+    a.cluster = 1;
+    a.slice = a.n;
     a.warps = (a.n + LANES * EPT - 1) / (LANES * EPT);
     const int threads = a.warps > NB_WARPS / 2 ? 32 * a.warps : 32 * a.warps * (NB_WARPS / a.warps);
     a.groups = threads / (a.warps * LANES);
-    const int64_t turn = (a.ldx * (int64_t)sizeof(T)) % 16;
-    a.period = 1;
-    while (RAGGED && (a.period * turn) % 16 != 0) a.period *= 2;
     const size_t ring = V > 1 ? (size_t)norm_stages<T, EPT>() * (a.dh ? 3 : 2) * (EPT / V) * threads * 16 : 0;
     const size_t smem = std::max(ring, (size_t)2 * norm_sums_pitch(a.n) * 4);
-    const auto kernel = !a.rms || a.dc ? norm_backward_kernel<T, V, EPT, LANES, true, RAGGED> : norm_backward_kernel<T, V, EPT, LANES, false, RAGGED>;
+    const auto kernel = !a.rms || a.dc ? norm_backward_kernel<T, V, EPT, LANES, true, RAGGED, false>
+                                       : norm_backward_kernel<T, V, EPT, LANES, false, RAGGED, false>;
     // the 48 KB that need no asking for hold the kernel's own arrays as well
     if (!ensure_dynamic_smem((const void*)kernel, smem > 44 * 1024 ? std::max<size_t>(smem, 49 * 1024) : smem)) return PAMM_ERR_CUDA;
     const int64_t want = ((a.b + a.period - 1) / a.period + a.groups - 1) / a.groups;      // blocks of each phase
-    const int per_sm = std::max(1, std::min(norm_backward_blocks(a.n), blocks_per_sm((const void*)kernel, threads, smem)));
-    a.splits = (int)(a.period * std::min<int64_t>(want, std::max(1, sm_count() * per_sm / a.period)));
+    const int64_t most = (int64_t)sm_count() * std::min(norm_backward_blocks(a.n), resident((const void*)kernel, threads, smem, 1));
+    a.splits = (int)(a.period * std::min<int64_t>(want, std::max<int64_t>(1, most / a.period)));
     launch(kernel, dim3((unsigned)a.splits), dim3(threads), smem, st, true, a);
     return launch_status();
 }
-// Elements a thread: 8 of a row of up to 256 in as many lanes as it needs, then 32 bytes of each matrix, and twice that where the row is
-// wider than 16 such warps.
+template <typename T, int V, bool RAGGED>
+pamm_status launch_norm_backward_clusters(NormBackwardArgs& a, cudaStream_t st) {
+    constexpr int EPT = 16;                           // 8192 elements a block
+    a.cluster = a.n <= 2 * 512 * EPT ? 2 : 4;
+    a.slice = (int)round_up((a.n + a.cluster - 1) / a.cluster, V);
+    a.warps = (a.slice + 32 * EPT - 1) / (32 * EPT);
+    a.groups = 1;
+    const int threads = 32 * a.warps;
+    const size_t ring = (size_t)norm_stages<T, EPT>() * (a.dh ? 3 : 2) * (EPT / V) * threads * 16;
+    const size_t smem = std::max(ring, (size_t)2 * norm_sums_pitch(a.slice + 16) * 4);
+    const auto kernel = !a.rms || a.dc ? norm_backward_kernel<T, V, EPT, 32, true, RAGGED, true> : norm_backward_kernel<T, V, EPT, 32, false, RAGGED, true>;
+    if (!ensure_dynamic_smem((const void*)kernel, std::max<size_t>(smem, 49 * 1024))) return PAMM_ERR_CUDA;
+    const int64_t want = (a.b + a.period - 1) / a.period, most = resident((const void*)kernel, threads, smem, a.cluster);
+    a.splits = (int)(a.period * std::min<int64_t>(want, std::max<int64_t>(1, most / a.period)));
+    launch_clusters(kernel, a.splits, a.cluster, threads, smem, st, a);
+    return launch_status();
+}
+// Elements a thread: 8 of a row of up to 256 in as many lanes as it needs, then 32 bytes of each matrix, or 64 of fp32; rows wider than the
+// 8192 elements that 16 such warps hold go over clusters.
 template <typename T, int V, bool RAGGED>
 pamm_status launch_norm_backward_fused(NormBackwardArgs& a, cudaStream_t st) {
     constexpr int E = 2 * (int)Vec16<T>::N;
+    const int64_t turn = (a.ldx * (int64_t)sizeof(T)) % 16;
+    a.period = 1;
+    while (RAGGED && (a.period * turn) % 16 != 0) a.period *= 2;
     if constexpr (V > 1) {
         if (a.n <= 64 && !RAGGED) return launch_norm_backward_fused<T, V, 8, RAGGED ? 16 : 8, RAGGED>(a, st);
         if (a.n <= 128) return launch_norm_backward_fused<T, V, 8, 16, RAGGED>(a, st);        // a ragged row needs 16 lanes for its ends
         if (a.n <= 256) return launch_norm_backward_fused<T, V, 8, 32, RAGGED>(a, st);
+        if (a.n > 8192) return launch_norm_backward_clusters<T, V, RAGGED>(a, st);
         // fp32 with a mean or a bias, measured at 32 and at 64 bytes: 65536 x 1024 149 and 127 us, 16384 x 4096 151 and 123, but 2048 x 512 7.3
         // and 8.9; without them 120 and 129 us at 65536 x 1024
-        const bool wide32 = sizeof(T) == 4 && (!a.rms || a.dc) && (a.n > 1024 || a.b * a.n > (8 << 20));
-        if (a.n > 512 * E || wide32) return launch_norm_backward_fused<T, V, 2 * E, 32, RAGGED>(a, st);
+        const bool wide32 = (!a.rms || a.dc) && (a.n > 1024 || a.b * a.n > (8 << 20));
+        if (sizeof(T) == 4 && (a.n > 512 * E || wide32)) return launch_norm_backward_fused<T, V, 16, 32, RAGGED>(a, st);
     }
     return launch_norm_backward_fused<T, V, E, 32, RAGGED>(a, st);
 }
@@ -663,8 +713,7 @@ pamm_status launch_norm_backward(NormBackwardArgs a, RowAccess access, cudaStrea
     constexpr int V = Vec16<T>::N;
     const bool sums = a.dw || a.dc;
     const dim3 finish_grid((unsigned)((a.n + NB_FINISH_COLS - 1) / NB_FINISH_COLS));
-    const int widest = 1024 * Vec16<T>::N;                        // that 16 warps hold at 32 bytes a thread and matrix
-    const bool fused = a.n <= (access == RowAccess::elements ? widest : 2 * widest);
+    const bool fused = access != RowAccess::elements || a.n <= 1024 * V;
     a.splits = 0;
     if (fused && a.b) {
         const pamm_status s = access == RowAccess::whole    ? launch_norm_backward_fused<T, V, false>(a, st)
@@ -672,17 +721,14 @@ pamm_status launch_norm_backward(NormBackwardArgs a, RowAccess access, cudaStrea
                                                             : launch_norm_backward_fused<T, 1, false>(a, st);
         if (s != PAMM_OK) return s;
     } else if (a.b && sums) {
-        // rows too wide for registers: the column sums by themselves, before dX may take the place of dY or X
+        // too wide for a block, element by element: the column sums by themselves, before dX may take the place of dY or X
         a.rows_per_split = (a.b + norm_splits(a.b) - 1) / norm_splits(a.b);
         a.splits = (int)((a.b + a.rows_per_split - 1) / a.rows_per_split);
         launch(norm_backward_columns_kernel<T>, dim3((unsigned)((a.n + NB_COL_THREADS - 1) / NB_COL_THREADS), (unsigned)a.splits),
                dim3(NB_COL_THREADS), 0, st, true, a);
     }
     if (sums) launch(norm_backward_finish_kernel, finish_grid, dim3(NB_FINISH_THREADS), 0, st, true, a);
-    if (a.b && !fused) {
-        if (access == RowAccess::whole) launch(norm_backward_row_kernel<T, V>, dim3((unsigned)a.b), dim3(NB_WIDE_THREADS), 0, st, true, a);
-        else launch(norm_backward_row_kernel<T, 1>, dim3((unsigned)a.b), dim3(NB_WIDE_THREADS), 0, st, true, a);
-    }
+    if (a.b && !fused) launch(norm_backward_row_kernel<T>, dim3((unsigned)a.b), dim3(NB_WIDE_THREADS), 0, st, true, a);
     return launch_status();
 }
 

@@ -35,7 +35,7 @@ def vector(n, dtype, seed, centre=1.0):
 
 
 SIZES = [(1, 1), (3, 2), (2, 7), (5, 8), (9, 31), (300, 64), (37, 100), (64, 512), (33, 520), (3, 1000), (17, 1999), (150, 2048),
-         (11, 4096), (5, 5003), (3, 8192), (2, 16384), (2, 16391), (1, 32768)]
+         (11, 4096), (5, 5003), (3, 8192), (2, 16384), (2, 16391), (1, 32768), (90, 8200), (170, 9001), (41, 20000), (39, 32761)]
 
 
 @pytest.mark.parametrize("dtype,w_dtype", [(F32, F32), (BF16, BF16), (BF16, F32), (F32, BF16)])
@@ -73,6 +73,28 @@ def test_forward_and_backward_of_all_sizes(b, n, dtype, w_dtype):
         assert (dc is None) != bias
         if bias:
             assert plain64.within(dc, gc, plain64.stored(bc, gc, w_dtype)) <= 1.0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("b,n", [(70, 31), (40, 1000), (9, 5003), (21, 9001), (5, 20000), (3, 32768)])
+def test_matrices_aligned_differently(b, n, dtype):
+    for rms in (False, True):
+        pads = [(0, 0), (1, 0), (8, 3), (5, 1), (2, 2)]             # of x, r (dy), y (dx), h (dh): distances and bases apart
+        x, r = (rows(b, n, dtype, k, pad=pads[k][0], shift=pads[k][1])[0] for k in (0, 1))
+        w, c = vector(n, F32, 2), vector(n, F32, 3, 0.0)
+        (y, y_room), (h, h_room) = (rows(b, n, dtype, 0, pad=pads[k][0], shift=pads[k][1]) for k in (2, 3))
+        y, h, mean, rstd = pamm.norm_forward(x, w, c, residual=r, rms=rms, Y=y, H=h)
+        want = plain64.norm_forward(x, w, c, r, 1e-5, rms)
+        by, bh, _, _ = plain64.norm_forward_bounds(x, w, c, r, 1e-5, rms)
+        assert plain64.within(y, want[0], plain64.stored(by, want[0], dtype)) <= 1.0 and untouched(y, y_room, *pads[2])
+        assert plain64.within(h, want[1], plain64.stored(bh, want[1], dtype)) <= 1.0 and untouched(h, h_room, *pads[3])
+        dy, dh = (rows(b, n, dtype, 10 + k, 1e-2, *pads[k])[0] for k in (1, 3))
+        dx, dx_room = rows(b, n, dtype, 0, pad=pads[2][0], shift=pads[2][1])
+        dx, dw, dc = pamm.norm_backward(dy, h, mean, rstd, w, bias=True, dH=dh, dX=dx)
+        gx, gw, gc = plain64.norm_backward(dy, h, mean, rstd, w, dh, rms)
+        bx, bw, bc = plain64.norm_backward_bounds(dy, h, mean, rstd, w, dh, rms)
+        assert plain64.within(dx, gx, plain64.stored(bx, gx, dtype)) <= 1.0 and untouched(dx, dx_room, *pads[2])
+        assert plain64.within(dw, gw, plain64.stored(bw, gw, F32)) <= 1.0 and plain64.within(dc, gc, plain64.stored(bc, gc, F32)) <= 1.0
 
 
 @pytest.mark.parametrize("b", [1, 2, 31, 147, 149, 1000, 4099, 20000])
