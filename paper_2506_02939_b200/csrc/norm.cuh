@@ -50,14 +50,52 @@ __device__ __forceinline__ void load_row(const T* p, int at, int step, int end, 
         else raw[i] = Piece<T, V>::zero();
     }
 }
-// V weights from `w` on, which the row's offset may have moved off the 16-byte grid (`vec`: not).
-template <typename W, int V, bool RAGGED>
-__device__ __forceinline__ void load_row_weights(const W* w, bool vec, float* out) {
-    if (!RAGGED || vec) {
-        load_weights<W, V>(w, out);
-    } else {
+// V weights from element `col` on, whose distance from the vector grid, `OFF`, is the same for the whole row: the aligned vectors that hold
+// them, unpacked from the place they lie at.
+template <typename W, int V, int OFF>
+__device__ __forceinline__ void load_shifted(const W* aligned, float* out) {
+    constexpr int A = V < 16 / (int)sizeof(W) ? V : 16 / (int)sizeof(W);      // elements of a vector
+    constexpr int COUNT = V / A + (OFF > 0), WORDS = A * (int)sizeof(W) / 4;
+    uint32_t w[COUNT * WORDS];
 #pragma unroll
-        for (int e = 0; e < V; ++e) out[e] = to_float(w[e]);
+    for (int i = 0; i < COUNT; ++i) {
+        if constexpr (WORDS == 4) {
+            const uint4 t = __ldg(reinterpret_cast<const uint4*>(aligned + i * A));
+            w[4 * i] = t.x; w[4 * i + 1] = t.y; w[4 * i + 2] = t.z; w[4 * i + 3] = t.w;
+        } else {
+            const uint2 t = __ldg(reinterpret_cast<const uint2*>(aligned + i * A));
+            w[2 * i] = t.x; w[2 * i + 1] = t.y;
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        const int j = OFF + e;
+        if constexpr (sizeof(W) == 4) out[e] = __uint_as_float(w[j]);
+        else out[e] = j & 1 ? bf16_hi(w[j / 2]) : bf16_lo(w[j / 2]);
+    }
+}
+template <typename W, int V, int OFF = 0>
+__device__ __forceinline__ void load_at_offset(const W* aligned, int off, float* out) {
+    constexpr int A = V < 16 / (int)sizeof(W) ? V : 16 / (int)sizeof(W);
+    if constexpr (OFF < A) {
+        if (off == OFF) load_shifted<W, V, OFF>(aligned, out);
+        else load_at_offset<W, V, OFF + 1>(aligned, off, out);
+    }
+}
+// Weights col .. col + V - 1 of the n at `w`.
+template <typename W, int V, bool RAGGED>
+__device__ __forceinline__ void load_row_weights(const W* w, int col, int n, float* out) {
+    if constexpr (!RAGGED) {
+        load_weights<W, V>(w + col, out);
+    } else {
+        constexpr int A = V < 16 / (int)sizeof(W) ? V : 16 / (int)sizeof(W);
+        const int off = (int)(reinterpret_cast<uintptr_t>(w + col) / sizeof(W) % A);
+        if (off == 0 || (col >= off && col - off + V + A <= n)) {
+            load_at_offset<W, V>(w + col - off, off, out);
+        } else {            // the vectors would leave the weights
+#pragma unroll
+            for (int e = 0; e < V; ++e) out[e] = to_float(w[col + e]);
+        }
     }
 }
 
@@ -216,7 +254,6 @@ norm_forward_kernel(const __grid_constant__ NormForwardArgs a) {
     if (RAGGED && extra >= 0 && row0 < a.b)
         static_cast<T*>(a.y)[row[0] * a.ldy + extra] =
             from_float<T>(fmaf(hx * rstd[0], w ? to_float(w[extra]) : 1.f, c ? to_float(c[extra]) : 0.f));
-    const bool w_vec = (reinterpret_cast<uintptr_t>(w + lead) & 15) == 0, c_vec = (reinterpret_cast<uintptr_t>(c + lead) & 15) == 0;
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
         const int col = lead + at + p * step;
@@ -227,8 +264,8 @@ norm_forward_kernel(const __grid_constant__ NormForwardArgs a) {
             q[e] = 1.f;
             k[e] = 0.f;
         }
-        if (w) load_row_weights<W, V, RAGGED>(w + col, w_vec, q);
-        if (c) load_row_weights<W, V, RAGGED>(c + col, c_vec, k);
+        if (w) load_row_weights<W, V, RAGGED>(w, col, a.n, q);
+        if (c) load_row_weights<W, V, RAGGED>(c, col, a.n, k);
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             float y[V];
@@ -260,16 +297,14 @@ struct NormBackwardArgs {
 
 // V weights (1 where there are none) of either type.
 template <int V, bool RAGGED>
-__device__ __forceinline__ void load_any_weights(const void* w, bool is_bf16, int col, float* out) {
+__device__ __forceinline__ void load_any_weights(const void* w, bool is_bf16, int col, int n, float* out) {
     if (!w) {
 #pragma unroll
         for (int e = 0; e < V; ++e) out[e] = 1.f;
     } else if (is_bf16) {
-        const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(w) + col;
-        load_row_weights<__nv_bfloat16, V, RAGGED>(p, (reinterpret_cast<uintptr_t>(p) & 15) == 0, out);
+        load_row_weights<__nv_bfloat16, V, RAGGED>(static_cast<const __nv_bfloat16*>(w), col, n, out);
     } else {
-        const float* p = static_cast<const float*>(w) + col;
-        load_row_weights<float, V, RAGGED>(p, (reinterpret_cast<uintptr_t>(p) & 15) == 0, out);
+        load_row_weights<float, V, RAGGED>(static_cast<const float*>(w), col, n, out);
     }
 }
 
@@ -347,9 +382,9 @@ norm_backward_kernel(const __grid_constant__ NormBackwardArgs a) {
     for (int p = 0; p < PIECES; ++p) {
 #pragma unroll
         for (int e = 0; e < V; ++e) w[p * V + e] = 0.f;
-        if (at + p * step < end) load_any_weights<V, RAGGED>(a.w, a.w_bf16, lead + at + p * step, w + p * V);
+        if (at + p * step < end) load_any_weights<V, RAGGED>(a.w, a.w_bf16, lead + at + p * step, a.n, w + p * V);
     }
-    if (RAGGED && extra >= 0) load_any_weights<1, false>(a.w, a.w_bf16, extra, &wx);
+    if (RAGGED && extra >= 0) load_any_weights<1, false>(a.w, a.w_bf16, extra, a.n, &wx);
 #pragma unroll
     for (int e = 0; e < EPT; ++e) dw[e] = 0.f;
 #pragma unroll
@@ -612,7 +647,7 @@ norm_backward_row_kernel(const __grid_constant__ NormBackwardArgs a) {
     float sums[2] = {0.f, 0.f};
     for (int col = threadIdx.x; col < a.n; col += NB_WIDE_THREADS) {
         float w;
-        load_any_weights<1, false>(a.w, a.w_bf16, col, &w);
+        load_any_weights<1, false>(a.w, a.w_bf16, col, a.n, &w);
         const float g = to_float(dy[col]) * w;
         sums[0] = fmaf(g, (to_float(x[col]) - mean) * rstd, sums[0]);
         sums[1] += g;
@@ -623,7 +658,7 @@ norm_backward_row_kernel(const __grid_constant__ NormBackwardArgs a) {
     const T* dh = a.dh ? static_cast<const T*>(a.dh) + row * a.lddh : nullptr;
     for (int col = threadIdx.x; col < a.n; col += NB_WIDE_THREADS) {
         float w;
-        load_any_weights<1, false>(a.w, a.w_bf16, col, &w);
+        load_any_weights<1, false>(a.w, a.w_bf16, col, a.n, &w);
         const float d = to_float(dy[col]) * w - g - (to_float(x[col]) - mean) * rstd * gu;
         dx[col] = from_float<T>(fmaf(rstd, d, dh ? to_float(dh[col]) : 0.f));
     }

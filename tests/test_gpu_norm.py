@@ -151,6 +151,28 @@ def test_rows_of_infinities_nan_and_zeros_keep_to_themselves(n, dtype):
         assert torch.isnan(y[2, n // 2]) if rms else torch.isnan(y[2]).all()
 
 
+@pytest.mark.parametrize("dtype,w_dtype", [(F32, F32), (BF16, BF16), (BF16, F32), (F32, BF16)])
+@pytest.mark.parametrize("n,pad", [(64, 0), (256, 0), (777, 0), (2040, 3), (2048, 0)])
+def test_weights_anywhere(n, pad, dtype, w_dtype):
+    """Weights and biases that start off the 16-byte grid, at the very ends of memory filled with NaN."""
+    b = 37
+    x, dy = rows(b, n, dtype, 1, pad=pad)[0], rows(b, n, dtype, 2, 1e-2, pad)[0]
+    for shift in range(0, 9):
+        room = torch.full((2, shift + n), float("nan"), device="cuda", dtype=w_dtype)
+        w, c = room[0, shift:], room[1, shift:]
+        w.copy_(vector(n, w_dtype, 3))
+        c.copy_(vector(n, w_dtype, 4, 0.0))
+        y, _, mean, rstd = pamm.norm_forward(x, w, c)
+        want = plain64.norm_forward(x, w, c)[0]
+        by = plain64.norm_forward_bounds(x, w, c)[0]
+        assert plain64.within(y, want, plain64.stored(by, want, dtype)) <= 1.0
+        dx, dw, dc = pamm.norm_backward(dy, x, mean, rstd, w, bias=True)
+        gx, gw, gc = plain64.norm_backward(dy, x, mean, rstd, w)
+        bx, bw, bc = plain64.norm_backward_bounds(dy, x, mean, rstd, w)
+        for got, wanted, bound, dt in ((dx, gx, bx, dtype), (dw, gw, bw, w_dtype), (dc, gc, bc, w_dtype)):
+            assert plain64.within(got, wanted, plain64.stored(bound, wanted, dt)) <= 1.0
+
+
 def test_a_large_mean_does_not_cost_the_variance():
     n = 4096
     x = (1000.0 + rows(8, n, F32, 7, 0.01)[0]).contiguous()
