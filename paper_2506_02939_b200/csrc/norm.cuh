@@ -688,15 +688,16 @@ norm_backward_columns_kernel(const __grid_constant__ NormBackwardArgs a) {
     part[a.pitch] = dc;
 }
 
-// The partial sums of all ranges, added in a fixed order: 8 columns (a sector) a block, 64 strands of the ranges.
-constexpr int NB_FINISH_COLS = 8, NB_FINISH_THREADS = 512;
+// The partial sums of all ranges, added in a fixed order: COLS columns (whole sectors) a block, whose other threads are strands of the ranges.
+constexpr int NB_FINISH_THREADS = 512;
+template <int COLS>
 __global__ void __launch_bounds__(NB_FINISH_THREADS)
 norm_backward_finish_kernel(const __grid_constant__ NormBackwardArgs a) {
-    constexpr int STRANDS = NB_FINISH_THREADS / NB_FINISH_COLS, WARPS = NB_FINISH_THREADS / 32;
-    __shared__ float2 s_part[WARPS][NB_FINISH_COLS];
+    constexpr int STRANDS = NB_FINISH_THREADS / COLS, WARPS = NB_FINISH_THREADS / 32;
+    __shared__ float2 s_part[WARPS][COLS];
     grid_dependency_wait();
     grid_launch_dependents();
-    const int c = threadIdx.x % NB_FINISH_COLS, strand = threadIdx.x / NB_FINISH_COLS, col = blockIdx.x * NB_FINISH_COLS + c;
+    const int c = threadIdx.x % COLS, strand = threadIdx.x / COLS, col = blockIdx.x * COLS + c;
     float dw = 0.f, dc = 0.f;
     if (col < a.n) {
 #pragma unroll 4
@@ -707,13 +708,13 @@ norm_backward_finish_kernel(const __grid_constant__ NormBackwardArgs a) {
         }
     }
 #pragma unroll
-    for (int o = NB_FINISH_COLS; o < 32; o *= 2) {          // the strands of a warp
+    for (int o = COLS; o < 32; o *= 2) {          // the strands of a warp
         dw += __shfl_xor_sync(0xffffffffu, dw, o);
         dc += __shfl_xor_sync(0xffffffffu, dc, o);
     }
-    if ((threadIdx.x & 31) < NB_FINISH_COLS) s_part[threadIdx.x >> 5][c] = make_float2(dw, dc);
+    if ((threadIdx.x & 31) < COLS) s_part[threadIdx.x >> 5][c] = make_float2(dw, dc);
     __syncthreads();
-    if (threadIdx.x >= NB_FINISH_COLS || col >= a.n) return;
+    if (threadIdx.x >= COLS || col >= a.n) return;
     dw = dc = 0.f;
 #pragma unroll
     for (int w = 0; w < WARPS; ++w) {
