@@ -2,7 +2,7 @@
 //   N = sqrt(sum over all elements of g^2);  g <- g min(1, max_norm / (N + 1e-6))
 //
 // Three launches, the first and the last bound by memory: every block sums the squares of its share; one block
-// joins the sums in a fixed order; and the scaling reads and writes every element once more (or, in place and below the
+// joins the sums in a fixed order (of a small list, every block of the last launch); and the scaling reads and writes every element once more (or, in place and below the
 // limit, returns at once).  The list travels in the kernels' parameters, so that a call needs no copy and no allocation
 // and can be captured; lists longer than one launch holds take several.  The work is cut into chunks of 4096 to 65536
 // elements, block after block; the scaling goes through them backwards, and so finds in L2 what the sum read last.
@@ -201,17 +201,11 @@ grad_squares_kernel(const __grid_constant__ GradList<CAP> list, double* partial)
     if (threadIdx.x == 0) partial[blockIdx.x] = (list.add ? partial[blockIdx.x] : 0.0) + acc;
 }
 
-// The norm and the factor, by one block.
-__global__ void __launch_bounds__(GC_THREADS)
-grad_norm_finish_kernel(const double* partial, int parts, double max_norm, float* norm, GradFactor* factor) {
-    __shared__ double s_part[GC_THREADS / 32];
-    grid_dependency_wait();
-    grid_launch_dependents();
+// The norm, and the factor, from the blocks' sums: the same in every block that asks.
+__device__ __forceinline__ GradFactor join_sums(const double* partial, int parts, double max_norm, double* s_part, double& total) {
     double acc = 0.0;
     for (int i = threadIdx.x; i < parts; i += GC_THREADS) acc += partial[i];
-    const double total = sqrt(block_sum_double(acc, s_part));
-    if (threadIdx.x != 0) return;
-    *norm = (float)total;
+    total = sqrt(block_sum_double(acc, s_part));
     const double limited = max_norm / (total + 1e-6);
     // no limit at all, or one that is kept: 1; a NaN norm gives NaN, as in the formula
     const bool keep = isinf(max_norm) || limited >= 1.0;
@@ -220,15 +214,37 @@ grad_norm_finish_kernel(const double* partial, int parts, double max_norm, float
         f.first = 0x1p-64f;
         f.second = (float)(limited * 0x1p64);
     }
+    return f;
+}
+
+__global__ void __launch_bounds__(GC_THREADS)
+grad_norm_finish_kernel(const double* partial, int parts, double max_norm, float* norm, GradFactor* factor) {
+    __shared__ double s_part[GC_THREADS / 32];
+    grid_dependency_wait();
+    grid_launch_dependents();
+    double total;
+    const GradFactor f = join_sums(partial, parts, max_norm, s_part, total);
+    if (threadIdx.x != 0) return;
+    *norm = (float)total;
     *factor = f;
 }
 
+// The sums have been joined (parts = 0), or are few and every block does it for itself, which saves a launch: 2 us of a small list's 9.
 template <int CAP>
 __global__ void __launch_bounds__(GC_THREADS, 6)
-grad_scale_kernel(const __grid_constant__ GradList<CAP> list, const GradFactor* factor) {
+grad_scale_kernel(const __grid_constant__ GradList<CAP> list, const GradFactor* factor, const double* partial, int parts, double max_norm,
+                  float* norm) {
+    __shared__ double s_part[GC_THREADS / 32];
     grid_dependency_wait();
     grid_launch_dependents();
-    const GradFactor f = *factor;
+    GradFactor f;
+    if (parts) {
+        double total;
+        f = join_sums(partial, parts, max_norm, s_part, total);
+        if (blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)total;
+    } else {
+        f = *factor;
+    }
     if (f.keep && list.in_place) return;            // g * 1 is there already
     const auto span = [&](auto step, int t, const GradEntry& g, int64_t row, int64_t col, int len) {
         constexpr int STEP = decltype(step)::value;
