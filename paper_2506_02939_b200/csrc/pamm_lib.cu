@@ -546,7 +546,7 @@ __global__ void selftest_bounded_wait_kernel(uint32_t polls) {
 // ---- the operators around the projection ---------------------------------------------------
 namespace {
 
-// Row partition of the norm's column sums, and the scratch that holds their partial sums.
+// Row partition of the norm's column sums where they are a launch of their own, and the scratch that holds the partial sums.
 inline int64_t norm_splits(int64_t b) { return std::max<int64_t>(1, std::min<int64_t>((b + 31) / 32, 2 * sm_count())); }
 // Blocks per SM of the fused backward pass, at most: the registers allow no more where rows are wide.
 inline int norm_backward_blocks(int64_t n) { return n <= 2048 ? 4 : 3; }

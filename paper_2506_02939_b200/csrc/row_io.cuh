@@ -34,20 +34,9 @@ template <typename T> __device__ __forceinline__ T from_float(float x);
 template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
-// floats -> 16 bytes of T, rounded to nearest even
-template <typename T>
-__device__ __forceinline__ uint4 round_vec(const float (&x)[Vec16<T>::N]);
-template <>
-__device__ __forceinline__ uint4 round_vec<float>(const float (&x)[4]) {
-    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
-}
-__device__ __forceinline__ uint32_t round_bf16x2(float lo, float hi) {
+__device__ __forceinline__ uint32_t round_bf16x2(float lo, float hi) {       // to nearest even
     const __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&t);
-}
-template <>
-__device__ __forceinline__ uint4 round_vec<__nv_bfloat16>(const float (&x)[8]) {
-    return make_uint4(round_bf16x2(x[0], x[1]), round_bf16x2(x[2], x[3]), round_bf16x2(x[4], x[5]), round_bf16x2(x[6], x[7]));
 }
 
 // V consecutive elements of a row as they lie in memory, aligned to their size of 2, 4, 8 or 16 bytes.  Loading and unpacking
