@@ -98,11 +98,13 @@ def test_matrices_aligned_differently(b, n, dtype):
 
 
 @pytest.mark.parametrize("b", [1, 2, 31, 147, 149, 1000, 4099, 20000])
-@pytest.mark.parametrize("n,dtype", [(256, BF16), (1024, F32), (2048, BF16), (64, BF16), (40, F32), (128, F32), (100, BF16), (333, BF16)])
+@pytest.mark.parametrize("n,dtype", [(256, BF16), (1024, F32), (2048, BF16), (64, BF16), (40, F32), (128, F32), (100, BF16), (333, BF16), (480, BF16), (200, F32)])
 def test_weight_gradients_over_many_rows(b, n, dtype):
     x, _ = rows(b, n, dtype, b)
     dy, _ = rows(b, n, dtype, b + 1, 1e-3)
-    _, _, mean, rstd = pamm.norm_forward(x)
+    y, _, mean, rstd = pamm.norm_forward(x)
+    want, by = plain64.norm_forward(x)[0], plain64.norm_forward_bounds(x)[0]
+    assert plain64.within(y, want, plain64.stored(by, want, dtype)) <= 1.0
     for w_dtype in (F32, BF16):
         w = vector(n, w_dtype, 3)
         dx, dw, dc = pamm.norm_backward(dy, x, mean, rstd, w, bias=True, dw_dtype=F32)
