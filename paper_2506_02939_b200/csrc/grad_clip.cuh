@@ -19,7 +19,7 @@ constexpr int GC_UNROLL = 4;            // vectors in flight per thread
 constexpr int GC_BLOCKS_PER_SM = 8;     // of the sum: one wave
 // elements of a chunk: of the sum, by the size of the list; of the scaling
 constexpr int GC_MIN_CHUNK = 4096, GC_MAX_CHUNK = 65536, GC_SCALE_CHUNK = 16384;
-// list entries per launch: parameters of 1.8, 7 and 32 KB, which a launch takes 2, 3 and 6 us of host time to hand over
+// list entries per launch: parameters of 1.8, 7 and 32 KB, so that a short list is not handed over as a long one
 constexpr int GC_SMALL = 24, GC_MEDIUM = 96, GC_LARGE = 448;
 
 struct GradEntry {
