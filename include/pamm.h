@@ -383,7 +383,9 @@ typedef enum { PAMM_NORM_LAYER = 0, PAMM_NORM_RMS = 1 } pamm_norm_kind;
  *   w, c   n entries of w_dt, or NULL (1 and 0)
  *   mean, rstd   b fp32 each, or NULL: mu and s for the backward pass (mean receives 0 in the RMS form)
  * Y may be X or R, and H may be X or R (the same base and leading dimension); Y may not be H.
- * A row with a NaN or infinity gives what the formulas give.  Limit: n <= 32768.
+ * A row with a NaN or infinity gives what the formulas give, and so does one whose sums or squares are beyond fp32 (masked rows
+ * hold the type's lowest value); where H takes the place of X or R, such a row is normalised as it is stored there.  h itself
+ * has to fit its type.  A mean square below fp32's range (1e-38) counts as 0 beside eps.  Limit: n <= 32768.
  */
 pamm_status pamm_norm_forward(pamm_norm_kind kind, const void* X, int64_t ldx, const void* R, int64_t ldr, int64_t b, int64_t n,
                               pamm_dtype dt, const void* w, const void* c, pamm_dtype w_dt, float eps, void* Y, int64_t ldy,

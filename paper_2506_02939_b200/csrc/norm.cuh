@@ -10,6 +10,11 @@
 // registers between its one reading and its one writing, and the variance is taken around the true mean.
 // mu and s are those of h before it is rounded to its storage type: y then carries one rounding.
 //
+// Values from 1e19 on (a masked row holds its type's lowest, -3e38) have squares, and sums, beyond fp32, and h - mu
+// reaches twice the type's range.  The forward pass takes such a row a second time, its values times 2^-80; the
+// backward pass takes differences as h / 4 - mu / 4, with the same bits (a multiply-add with a power of two in place of
+// an addition).
+//
 // A thread holds EPT elements of its row in EPT / V pieces; V is a 16-byte vector or one element:
 //   vectors, whole   every row 16-byte aligned, n a multiple of V
 //   vectors, RAGGED  any n and any alignment that all matrices of the call share row by row: the row's whole vectors
@@ -20,10 +25,12 @@
 #include "pamm_common.cuh"
 #include "row_io.cuh"
 #include "sm100_ptx.cuh"
+#include <cfloat>
 
 namespace pamm {
 
 constexpr int64_t NORM_MAX_N = 32768;
+constexpr float NORM_SHRINK = 0x1p-80f;       // 32768 squares of 2 x 2^128 x 2^-80 fit fp32
 
 // A row's whole vectors and this thread's element outside them.
 struct RowShape {
@@ -106,7 +113,7 @@ struct NormForwardArgs {
     int64_t ldx, ldr, ldy, ldh, b;
     int n, warps;           // warps of the block that share a row; 1: LANES lanes have a row
     float eps;
-    bool rms;
+    bool rms, h_over_input; // H takes the place of X or R
 };
 
 // Sums over the warps of a block's rows (all of the block's); every thread gets them.  `part`: [ROWS][32] floats that the
@@ -124,6 +131,80 @@ __device__ __forceinline__ void row_sums(float (&x)[ROWS], float (*part)[32], in
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) x[r] = warp_sum(lane < warps ? part[r][lane] : 0.f);
+}
+
+// A row whose sum of squares is infinite or NaN, from the start with its values times NORM_SHRINK: NaN and infinities among them
+// give what the formulas give, large values their statistics.  Every value is read again for each of the three passes: from H,
+// rounded to its type, where that has taken the place of X or R.  Threads without such a row (`active`) go along for the shuffles.
+// Rare: the hot path pays a comparison and a branch, up to 1% of its time (3% for rows of 257 to 512, whose lanes are half a warp);
+// scaling the sums of every row instead cost up to 4% and more registers, this row kept in registers up to 3%.
+template <typename T, typename W, int V, int LANES, bool RAGGED>
+__device__ __forceinline__ void norm_forward_shrunk_row(const NormForwardArgs& a, int64_t row, bool active, int at, int step, const RowShape& shape,
+                                                        float (*s_sum)[32], float (*s_sq)[32]) {
+    using P = Piece<T, V>;
+    const float inv_n = 1.f / (float)a.n, to = 1.f / NORM_SHRINK;
+    const T* x = a.h_over_input ? static_cast<const T*>(a.h) + row * a.ldh : static_cast<const T*>(a.x) + row * a.ldx;
+    const T* r = a.r && !a.h_over_input ? static_cast<const T*>(a.r) + row * a.ldr : nullptr;
+    const int end = active ? shape.whole : 0, extra = RAGGED && active ? shape.extra : -1;
+    const auto values = [&](int col, float* v) {
+        P::unpack(P::load(x + col), v);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] *= NORM_SHRINK;
+        if (r) {
+            float q[V];
+            P::unpack(P::load(r + col), q);
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = fmaf(q[e], NORM_SHRINK, v[e]);
+        }
+    };
+    float hx = 0.f, v[V], mean = 0.f;
+    if (extra >= 0) hx = fmaf(r ? to_float(r[extra]) : 0.f, NORM_SHRINK, to_float(x[extra]) * NORM_SHRINK);
+    const bool barriers = LANES == 32 && a.warps > 1;
+    if (barriers) __syncthreads();          // every warp has read the parts of the first time
+    if (!a.rms) {
+        float sum[1] = {hx};
+#pragma unroll 1
+        for (int i = at; i < end; i += step) {
+            values(shape.lead + i, v);
+#pragma unroll
+            for (int e = 0; e < V; ++e) sum[0] += v[e];
+        }
+        row_sums<LANES>(sum, s_sum, a.warps);
+        mean = sum[0] * inv_n;
+    }
+    if (extra >= 0) hx -= mean;
+    float sq[1] = {hx * hx};
+#pragma unroll 1
+    for (int i = at; i < end; i += step) {
+        values(shape.lead + i, v);
+#pragma unroll
+        for (int e = 0; e < V; ++e) sq[0] = fmaf(v[e] - mean, v[e] - mean, sq[0]);
+    }
+    row_sums<LANES>(sq, s_sq, a.warps);
+    if (barriers) __syncthreads();          // the caller may come with another row
+    if (!active) return;
+    const float small = sq[0] * inv_n, var = small * to * to;
+    float rstd = rsqrtf(var + a.eps), factor = rstd * to;
+    if (!(var <= FLT_MAX)) {                // beside which eps is nothing
+        factor = rsqrtf(small);
+        rstd = factor * NORM_SHRINK;
+    }
+    if (at == 0) {
+        const float m = mean * to;          // rounded, it may lie above the largest value
+        if (a.mean) a.mean[row] = isinf(m) && !isinf(mean) ? copysignf(FLT_MAX, m) : m;
+        if (a.rstd) a.rstd[row] = rstd;
+    }
+    const W *w = static_cast<const W*>(a.w), *c = static_cast<const W*>(a.c);
+    T* y = static_cast<T*>(a.y) + row * a.ldy;
+    if (extra >= 0) y[extra] = from_float<T>(fmaf(hx * factor, w ? to_float(w[extra]) : 1.f, c ? to_float(c[extra]) : 0.f));
+#pragma unroll 1
+    for (int i = at; i < end; i += step) {
+        const int col = shape.lead + i;
+        values(col, v);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = fmaf((v[e] - mean) * factor, w ? to_float(w[col + e]) : 1.f, c ? to_float(c[col + e]) : 0.f);
+        P::store(y + col, v);
+    }
 }
 
 // Measured on 65536 x 2048 bf16 (268 MB a matrix): the 16-byte copy of the same streams in one-shot blocks runs at 6.5 to
@@ -242,16 +323,24 @@ norm_forward_kernel(const __grid_constant__ NormForwardArgs a) {
         rstd[r] = sq.x + sq.y;
     }
     row_sums<LANES>(rstd, s_sq, a.warps);
+    bool beyond[ROWS], any = false;          // fp32's range: the row is taken again in the end
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
+        beyond[r] = !(rstd[r] <= FLT_MAX);
+        any = any || beyond[r];
         rstd[r] = rsqrtf(rstd[r] * inv_n + a.eps);
         if (at == 0 && row0 + r < a.b) {
             if (a.mean) a.mean[row[r]] = a.rms ? 0.f : mean[r];
             if (a.rstd) a.rstd[row[r]] = rstd[r];
         }
     }
+    constexpr bool ALONE = LANES == 32 && ROWS == 1;         // all of the warp has one row, the same answer with it
+    if (ALONE && any) {
+        norm_forward_shrunk_row<T, W, V, LANES, RAGGED>(a, row[0], row0 < a.b, at, step, shape, s_sum, s_sq);
+        return;
+    }
     const W *w = static_cast<const W*>(a.w), *c = static_cast<const W*>(a.c);
-    if (RAGGED && extra >= 0 && row0 < a.b)
+    if (RAGGED && extra >= 0 && row0 < a.b && (ALONE || !beyond[0]))
         static_cast<T*>(a.y)[row[0] * a.ldy + extra] =
             from_float<T>(fmaf(hx * rstd[0], w ? to_float(w[extra]) : 1.f, c ? to_float(c[extra]) : 0.f));
 #pragma unroll
@@ -279,8 +368,14 @@ norm_forward_kernel(const __grid_constant__ NormForwardArgs a) {
                     y[e] = v.x; y[e + 1] = v.y;
                 }
             }
-            if (row0 + r < a.b) P::store(static_cast<T*>(a.y) + row[r] * a.ldy + col, y);
+            if (row0 + r < a.b && (ALONE || !beyond[r])) P::store(static_cast<T*>(a.y) + row[r] * a.ldy + col, y);
         }
+    }
+    if (LANES < 32) any = __any_sync(0xffffffffu, any);          // rows that share a warp go along
+    if (!ALONE && any) {
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+            norm_forward_shrunk_row<T, W, V, LANES, RAGGED>(a, row[r], beyond[r] && row0 + r < a.b, at, step, shape, s_sum, s_sq);
     }
 }
 
@@ -468,12 +563,15 @@ norm_backward_kernel(const __grid_constant__ NormBackwardArgs a) {
         fetch(row + (STAGES - 1) * stride, stage == 0 ? STAGES - 1 : stage - 1);
         fetch_scalars(row + stride);
         float2 gu2 = twice(0.f), g2 = twice(0.f);
+        const float quarter = -0.25f * m, grown = SHIFT ? 4.f * s : s;
+        // what a thread holds outside the row counts for nothing, where the mean times s is infinite too
+        const auto times = [&](int e) { return at + e / V * step < end ? grown : 0.f; };
 #pragma unroll
         for (int e = 0; e < EPT; e += 2) {
             float2 uu = make_float2(u[e], u[e + 1]);
             const float2 dd = make_float2(g[e], g[e + 1]);
-            if (SHIFT) uu = add2(uu, twice(-m));
-            uu = mul2(uu, twice(s));
+            if (SHIFT) uu = fma2(uu, twice(0.25f), twice(quarter));
+            uu = mul2(uu, make_float2(times(e), times(e + 1)));
             const float2 ww = fma2(dd, uu, make_float2(dw[e], dw[e + 1]));
             dw[e] = ww.x; dw[e + 1] = ww.y;
             if (SHIFT) {
@@ -487,7 +585,7 @@ norm_backward_kernel(const __grid_constant__ NormBackwardArgs a) {
         }
         float gu = gu2.x + gu2.y, gs = g2.x + g2.y, gx = 0.f;
         if (RAGGED && extra >= 0 && mine) {
-            ux = (ux - m) * s;
+            ux = (SHIFT ? fmaf(ux, 0.25f, quarter) : ux) * grown;
             dwx = fmaf(yx, ux, dwx);
             dcx += yx;
             gx = yx * wx;
@@ -643,13 +741,14 @@ norm_backward_row_kernel(const __grid_constant__ NormBackwardArgs a) {
     const int64_t row = blockIdx.x;
     const T* x = static_cast<const T*>(a.x) + row * a.ldx;
     const T* dy = static_cast<const T*>(a.dy) + row * a.lddy;
-    const float mean = a.rms ? 0.f : a.mean[row], rstd = a.rstd[row];
+    const float quarter = a.rms ? 0.f : -0.25f * a.mean[row], rstd = a.rstd[row];
+    const auto unit = [&](int col) { return fmaf(to_float(x[col]), 0.25f, quarter) * (4.f * rstd); };
     float sums[2] = {0.f, 0.f};
     for (int col = threadIdx.x; col < a.n; col += NB_WIDE_THREADS) {
         float w;
         load_any_weights<1, false>(a.w, a.w_bf16, col, a.n, &w);
         const float g = to_float(dy[col]) * w;
-        sums[0] = fmaf(g, (to_float(x[col]) - mean) * rstd, sums[0]);
+        sums[0] = fmaf(g, unit(col), sums[0]);
         sums[1] += g;
     }
     row_sums<32>(sums, s_sums, NB_WIDE_THREADS / 32);
@@ -659,7 +758,7 @@ norm_backward_row_kernel(const __grid_constant__ NormBackwardArgs a) {
     for (int col = threadIdx.x; col < a.n; col += NB_WIDE_THREADS) {
         float w;
         load_any_weights<1, false>(a.w, a.w_bf16, col, a.n, &w);
-        const float d = to_float(dy[col]) * w - g - (to_float(x[col]) - mean) * rstd * gu;
+        const float d = to_float(dy[col]) * w - g - unit(col) * gu;
         dx[col] = from_float<T>(fmaf(rstd, d, dh ? to_float(dh[col]) : 0.f));
     }
 }
@@ -678,8 +777,8 @@ norm_backward_columns_kernel(const __grid_constant__ NormBackwardArgs a) {
     float dw = 0.f, dc = 0.f;
     for (int64_t row = begin; row < end; ++row) {
         const float d = to_float(static_cast<const T*>(a.dy)[row * a.lddy + col]);
-        const float mean = a.rms ? 0.f : a.mean[row];
-        const float u = (to_float(static_cast<const T*>(a.x)[row * a.ldx + col]) - mean) * a.rstd[row];
+        const float quarter = a.rms ? 0.f : -0.25f * a.mean[row];
+        const float u = fmaf(to_float(static_cast<const T*>(a.x)[row * a.ldx + col]), 0.25f, quarter) * (4.f * a.rstd[row]);
         dw = fmaf(d, u, dw);
         dc += d;
     }

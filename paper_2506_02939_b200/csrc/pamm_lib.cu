@@ -925,6 +925,7 @@ pamm_status pamm_norm_forward(pamm_norm_kind kind, const void* X, int64_t ldx, c
     a.ldx = ldx; a.ldr = ldr; a.ldy = ldy; a.ldh = ldh; a.b = b;
     a.n = (int)n; a.warps = 0; a.eps = eps;
     a.rms = kind == PAMM_NORM_RMS;
+    a.h_over_input = H && R && (H == X || H == R);
     const RowMatrix all[] = {{X, ldx}, {R, ldr}, {Y, ldy}, {H, ldh}};
     const RowAccess access = row_access(all, n, es, aligned(w, 16) && aligned(c, 16));
     cudaStream_t st = (cudaStream_t)stream;

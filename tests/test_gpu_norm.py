@@ -298,3 +298,84 @@ def test_prepared_calls():
     dw = torch.zeros_like(w)
     pamm.prepared(pamm.norm_backward, dy, x, None, rstd, w, dw=dw)()
     assert torch.equal(dw, pamm.norm_backward(dy, x, None, rstd, w)[1])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,pad,shift", [(40, 0, 0), (128, 0, 0), (250, 0, 1), (333, 0, 0), (512, 0, 0), (1000, 0, 0), (1999, 0, 3), (2048, 0, 0),
+                                         (8200, 0, 0), (20000, 0, 0)])
+def test_rows_of_the_types_largest_and_lowest_values(n, pad, shift, dtype):
+    """Masked rows hold the type's lowest value; the squares of values from 1e19 on leave fp32's range, mean, s and y do not."""
+    top = torch.finfo(dtype).max
+    x, _ = rows(9, n, dtype, 5, pad=pad, shift=shift)
+    x[1] = -top
+    x[2, 3:] = -top
+    x[3, ::2], x[3, 1::2] = top, -top
+    x[4, n // 2] = top
+    x[5] *= 1e25
+    x[6] = top
+    x[6, n // 3] = -top
+    x[7] *= 1e19
+    dy, dh = rows(9, n, dtype, 6, pad=pad, shift=shift)[0], rows(9, n, dtype, 7, pad=pad, shift=shift)[0]
+    w, c = vector(n, F32, 8), vector(n, F32, 9, 0.0)
+    for rms in (False, True):
+        y, _, mean, rstd = pamm.norm_forward(x, w, c, rms=rms)
+        want = plain64.norm_forward(x, w, c, rms=rms)
+        by, _, bm, bs = plain64.norm_forward_bounds(x, w, c, rms=rms)
+        assert torch.isfinite(y).all() and torch.isfinite(rstd).all() and (rstd > 0).all()
+        assert plain64.within(y, want[0], plain64.stored(by, want[0], dtype)) <= 1.0
+        # s of the largest values is a subnormal of fp32: half a unit of those beside the relative bound
+        assert plain64.within(rstd, want[3], bs + want[3] * plain64.U + 2.0 ** -149) <= 1.0
+        if not rms:
+            assert torch.isfinite(mean).all() and plain64.within(mean, want[2], plain64.stored(bm, want[2], F32)) <= 1.0
+        dx, dw, dc = pamm.norm_backward(dy, x, mean, rstd, w, bias=True, dH=dh)
+        gx, gw, gc = plain64.norm_backward(dy, x, mean, rstd, w, dh, rms)
+        bx, bw, bc = plain64.norm_backward_bounds(dy, x, mean, rstd, w, dh, rms)
+        for got, wanted, bound, dt in ((dx, gx, bx, dtype), (dw, gw, bw, F32), (dc, gc, bc, F32)):
+            assert torch.isfinite(got).all()
+            assert plain64.within(got, wanted, plain64.stored(bound, wanted, dt)) <= 1.0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n", [100, 333, 520, 2048, 9001])
+def test_a_constant_row_of_the_lowest_value_has_finite_gradients(n, dtype):
+    """Its mean is the value itself and s = eps^-1/2: what a thread holds beside the row's end must not count."""
+    top = torch.finfo(dtype).max
+    x = torch.full((3, n), -top, dtype=dtype, device="cuda")
+    dy, w = rows(3, n, dtype, 6)[0], vector(n, F32, 8)
+    mean = x[:, 0].float().contiguous()
+    rstd = torch.full((3,), 1e-5 ** -0.5, device="cuda")
+    dx, dw, dc = pamm.norm_backward(dy, x, mean, rstd, w, bias=True)
+    gx, gw, gc = plain64.norm_backward(dy, x, mean, rstd, w)
+    bx, bw, bc = plain64.norm_backward_bounds(dy, x, mean, rstd, w)
+    for got, wanted, bound, dt in ((dx, gx, bx, dtype), (dw, gw, bw, F32), (dc, gc, bc, F32)):
+        assert plain64.within(got, wanted, plain64.stored(bound, wanted, dt)) <= 1.0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("b,n", [(9, 40), (4800, 250), (9, 333), (4801, 512), (9600, 1024), (9, 2048), (9, 20000)])
+def test_extreme_rows_with_a_residual_in_and_out_of_place(b, n, dtype):
+    top = torch.finfo(dtype).max
+    x, r = rows(b, n, dtype, 1)[0].contiguous(), rows(b, n, dtype, 2, 0.5)[0].contiguous()
+    x[2] = -top
+    x[3, 1:] = -top
+    x[5, ::2] = top
+    x[b - 1] *= 1e25
+    w = vector(n, F32, 3)
+    for rms in (False, True):
+        y, h, mean, rstd = pamm.norm_forward(x, w, residual=r, rms=rms)
+        want = plain64.norm_forward(x, w, None, r, 1e-5, rms)
+        by = plain64.norm_forward_bounds(x, w, None, r, 1e-5, rms)[0]
+        assert torch.isfinite(y).all() and torch.isfinite(h).all()
+        assert plain64.within(y, want[0], plain64.stored(by, want[0], dtype)) <= 1.0
+        # in place: these rows are those of the stored h
+        stored = plain64.norm_forward(h, w, None, None, 1e-5, rms)
+        bs = plain64.norm_forward_bounds(h, w, None, None, 1e-5, rms)[0]
+        extreme = [2, 3, 5, b - 1]
+        for place in range(2):
+            both = [x.clone(), r.clone()]
+            y1, h1, _, _ = pamm.norm_forward(both[0], w, residual=both[1], rms=rms, H=both[place], Y=both[1 - place])
+            assert torch.equal(h1, h)
+            keep = torch.ones(b, dtype=torch.bool, device="cuda")
+            keep[extreme] = False
+            assert torch.equal(y1[keep], y[keep])
+            assert plain64.within(y1[extreme], stored[0][extreme], plain64.stored(bs, stored[0], dtype)[extreme]) <= 1.0
