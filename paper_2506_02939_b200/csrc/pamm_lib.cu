@@ -770,7 +770,9 @@ pamm_status launch_rotary(RotaryArgs a, const RotaryShape& g, cudaStream_t st) {
     a.tokens_per_block = (int)std::max<int64_t>(1, std::min<int64_t>(128 / units, a.tokens));
     const int64_t work = a.tokens_per_block * units, parts = (work + 255) / 256;
     const int threads = (int)round_up((work + parts - 1) / parts, 32);
-    const dim3 grid((unsigned)((a.tokens + a.tokens_per_block - 1) / a.tokens_per_block), (unsigned)parts);
+    // a token of 2^24 units has 65536 parts, one more than a grid's y holds: the largest go along z as well
+    const unsigned deep = (unsigned)((parts + 65534) / 65535);
+    const dim3 grid((unsigned)((a.tokens + a.tokens_per_block - 1) / a.tokens_per_block), (unsigned)((parts + deep - 1) / deep), deep);
     launch(rotary_kernel<T, V, ADJACENT, HEADS>, grid, dim3(threads), 0, st, true, a);
     return launch_status();
 }

@@ -139,3 +139,13 @@ def test_the_64_bit_norm_gradient_against_differences(rms):
     assert abs((loss(x + t * v, w, c) - loss(x - t * v, w, c)) / (2 * t) - float((dx * v).sum())) < 1e-6
     assert abs((loss(x, w + t * vw, c) - loss(x, w - t * vw, c)) / (2 * t) - float((dw * vw).sum())) < 1e-6
     assert abs((loss(x, w, c + t * vw) - loss(x, w, c - t * vw)) / (2 * t) - float((dc * vw).sum())) < 1e-6
+
+
+def test_the_largest_rotary_row_and_one_beyond():
+    def call(heads, d, batch=0):
+        return pamm._lib.pamm_rotary(FAKE, 0, 0, d, FAKE, 0, 0, d, batch, 1, heads, heads, d, 2, 0, 0, 0, FAKE, 4, None, 0, 0, 0, 0, None)
+
+    for heads, d in ((1, 2 ** 24), (2 ** 23, 2), (2 ** 12, 2 ** 12)):
+        assert call(heads, d) == pamm.OK                  # of no sequence: nothing is launched
+        assert call(heads, d + 1, 1) == call(heads, d + 1) == pamm.ERR_UNSUPPORTED
+    assert call(2 ** 24 + 1, 2) == pamm.ERR_UNSUPPORTED

@@ -195,3 +195,16 @@ def test_scaled_amplitude():
     assert abs(amplitude - (0.1 * math.log(8.0) + 1)) < 1e-15
     table = pamm.rotary_table(4, freq, amplitude)
     assert torch.allclose(table[0, :32], torch.tensor(amplitude, dtype=F32, device="cuda"), rtol=1e-7, atol=0) and not table[0, 32:].any()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("heads,rotated", [(1, 1), (1, 0), (2, 1)])
+def test_heads_of_the_largest_size_element_by_element(heads, rotated, interleaved, dtype):
+    d = 2 ** 24 // heads
+    table = pamm.rotary_table(3, *pamm.rotary_frequencies(2))
+    x = torch.randn((heads * d + 1,), device="cuda").to(dtype)[1:].view(1, heads, d)           # off every wider grid
+    got = pamm.rotary(x, table, rotated=rotated, interleaved=interleaved, first=2)
+    assert torch.equal(got[..., 2:], x[..., 2:]) and torch.equal(got[:, rotated:], x[:, rotated:])
+    want = pamm.rotary(x[..., :2].contiguous(), table, rotated=rotated, interleaved=interleaved, first=2)
+    assert torch.equal(got[..., :2], want)
