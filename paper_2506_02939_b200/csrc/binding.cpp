@@ -4,8 +4,8 @@
 // gradients 380.
 //
 // Every function takes its arguments by position (pamm.py has the signatures and the documentation), runs on
-// the current stream of its tensors' device and raises TypeError, ValueError or PammError.  While a call is
-// being prepared (pamm.prepared) the C call is written down instead: its name, its arguments and what has to
+// the current stream of its tensors' device and raises TypeError, ValueError or PammError.  In a thread that is
+// preparing a call (pamm.prepared) the C call is written down instead: its name, its arguments and what has to
 // stay alive for it.
 #include <Python.h>
 
@@ -25,7 +25,7 @@ namespace {
 using at::Tensor;
 
 PyObject* g_error = nullptr;       // PammError(code, where)
-PyObject* g_record = nullptr;      // list of (name, arguments, kept) while a call is being prepared
+thread_local PyObject* g_record = nullptr;      // list of (name, arguments, kept) while this thread prepares a call
 
 // ---- Python values ------------------------------------------------------------------------------------
 struct Failure {};                 // a Python exception is set

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import threading
 from pathlib import Path
 
 import torch
@@ -79,6 +80,36 @@ for _name, (_args, _res) in _SIGNATURES.items():
 EXPORTED = tuple(_SIGNATURES)
 
 
+class _Preparing(threading.local):
+    """What this thread writes down while it prepares a call (``prepared``); other threads' calls are made as ever."""
+    calls = None           # (name, function, arguments) of the library calls
+    keep = None            # what they need alive: the tensors the call allocates, host memory that the library reads
+    direct = None          # (name, arguments, what they need alive) of the compiled binding's calls
+
+
+_preparing = _Preparing()
+
+
+class _Library:
+    """The library's functions; in a thread that is preparing a call, stand-ins that write the call down."""
+
+    def __init__(self, real):
+        self._real = real
+
+    def __getattr__(self, name):
+        fn, calls = getattr(self._real, name), _preparing.calls
+        if calls is None:
+            return fn
+
+        def note(*cargs):
+            calls.append((name, fn, cargs))
+            return OK
+        return note
+
+
+_lib = _Library(_lib)
+
+
 class PammError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -125,21 +156,15 @@ def _stream(stream) -> ctypes.c_void_p:
     return ctypes.c_void_p(s.cuda_stream)
 
 
-_prep_keep = None      # while a call is being prepared: the tensors it allocates, kept alive with the prepared call
-
-
 def _empty(*args, **kwargs) -> torch.Tensor:
-    t = torch.empty(*args, **kwargs)
-    if _prep_keep is not None:
-        _prep_keep.append(t)
-    return t
+    return _kept(torch.empty(*args, **kwargs))
 
 
-def _kept(host):
-    """A host object whose memory the library reads during the call: kept alive with a call that is being prepared."""
-    if _prep_keep is not None:
-        _prep_keep.append(host)
-    return host
+def _kept(memory):
+    """Memory that the library uses during the call: kept alive with a call that is being prepared."""
+    if _preparing.keep is not None:
+        _preparing.keep.append(memory)
+    return memory
 
 
 def alloc_matrix(rows: int, cols: int, dtype, device="cuda") -> torch.Tensor:
@@ -366,40 +391,26 @@ def qkv_step_host(X_host, dY_host, k: int, seed: int, dW_host, arena, f_host=Non
     return dW_host
 
 
-class _RecordingLib:
-    """Stands in for the library while a call is being prepared: notes the C function and its marshalled arguments."""
-
-    def __init__(self, real):
-        self._real, self.calls = real, []
-
-    def __getattr__(self, name):
-        fn = getattr(self._real, name)
-
-        def note(*cargs):
-            self.calls.append((name, fn, cargs))
-            return OK
-        return note
-
-
 def prepared(call, *args, **kwargs):
     """Marshal once, call often.  ``prepared(pamm.compress_fused, X, k, seed, idx_out=..., ...)`` runs nothing; it returns a
     zero-argument callable that repeats exactly that C call (same pointers, sizes, seed and stream), skipping the
     Python-side marshalling -- for loops where a step is only a few microseconds of GPU work.  Outputs the call
-    allocates itself stay alive with the callable but are not handed out: pass in the ones you want to read."""
-    global _lib, _prep_keep
-    real, rec, direct = _lib, _RecordingLib(_lib), []
-    _lib, _prep_keep = rec, []
+    allocates itself stay alive with the callable but are not handed out: pass in the ones you want to read.  Calls of other
+    threads in the meantime are made and not written down."""
+    outer = _preparing.calls, _preparing.keep, _preparing.direct
+    calls, keep, direct = [], [args, kwargs], []   # keep: the tensors behind the pointers, the call's own allocations included
+    _preparing.calls, _preparing.keep, _preparing.direct = calls, keep, direct
     _binding.set_record(direct)
     try:
         call(*args, **kwargs)
-        keep = (args, kwargs, _prep_keep, direct)  # the tensors behind the pointers, the call's own allocations included
     finally:
-        _lib, _prep_keep = real, None
-        _binding.set_record(None)
-    rec.calls += [(name, getattr(real, name), cargs) for name, cargs, _ in direct]
-    if len(rec.calls) != 1:
+        _preparing.calls, _preparing.keep, _preparing.direct = outer
+        _binding.set_record(outer[2])
+    keep.append(direct)
+    calls += [(name, getattr(_lib._real, name), cargs) for name, cargs, _ in direct]
+    if len(calls) != 1:
         raise ValueError("prepared() takes a binding function that makes exactly one library call")
-    name, fn, cargs = rec.calls[0]
+    name, fn, cargs = calls[0]
 
     def run(_fn=fn, _cargs=cargs, _name=name, _keep=keep):
         code = _fn(*_cargs)
