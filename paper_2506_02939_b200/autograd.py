@@ -117,21 +117,24 @@ class NormFunction(torch.autograd.Function):
         X2 = _matrix(X.detach(), n)
         R2 = None if residual is None else _matrix(residual.detach().to(X.dtype), n)
         w, c = (None if p is None else p.detach() for p in (weight, bias))
-        Y, H, mean, rstd = pamm.norm_forward(X2, w, c, residual=R2, eps=eps, rms=rms)
-        ctx.save_for_backward(H, mean, rstd, weight)
-        ctx.has_bias, ctx.shape, ctx.has_residual = bias is not None, X.shape, residual is not None
+        # made in their final shape, not as views of matrices: what follows may then work on y in place
+        Y = torch.empty(X.shape, dtype=X.dtype, device=X.device)
+        H = None if residual is None else torch.empty(X.shape, dtype=X.dtype, device=X.device)
+        _, _, mean, rstd = pamm.norm_forward(X2, w, c, residual=R2, eps=eps, rms=rms, Y=Y.view(-1, n), H=None if H is None else H.view(-1, n))
+        ctx.save_for_backward(X2 if H is None else H, mean, rstd, weight)
+        ctx.shape, ctx.has_residual = X.shape, residual is not None
         ctx.vector_type = weight.dtype if weight is not None else bias.dtype if bias is not None else X.dtype
         ctx.set_materialize_grads(False)
-        Y = Y.reshape(X.shape)
-        return Y if residual is None else (Y, H.reshape(X.shape))
+        return Y if residual is None else (Y, H)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dY, dH=None):
         H, mean, rstd, weight = ctx.saved_tensors
-        n = H.shape[1]
+        n = ctx.shape[-1]
         if dY is None and dH is None:
             return (None,) * 6
+        H = H.reshape(-1, n)
         if dY is None:
             dY = torch.zeros(ctx.shape, dtype=H.dtype, device=H.device)
         need_w, need_c = ctx.needs_input_grad[1], ctx.needs_input_grad[2]

@@ -131,3 +131,35 @@ def test_the_example_learns():
     losses = train_qkv_block.train(steps=150, report=None)
     assert torch.isfinite(losses).all()
     assert float(losses[-10:].mean()) < 0.5 * float(losses[:10].mean())
+
+
+@pytest.mark.parametrize("shape", [(7, 64), (64,), (2, 5, 64)])
+def test_outputs_of_the_norm_can_be_changed_in_place(shape):
+    layer = Norm(64, dtype=F32)
+    X, R, dy = normal(shape, F32, 1), normal(shape, F32, 2), normal(shape, F32, 3)
+    grads = []
+    for inplace in (False, True):
+        x = X.clone().requires_grad_()
+        layer.zero_grad()
+        y = layer(x)
+        assert y.shape == x.shape
+        y = torch.relu_(y) if inplace else torch.relu(y)
+        y.backward(dy)
+        grads.append((x.grad, layer.weight.grad.clone(), layer.bias.grad.clone()))
+    assert all(torch.equal(a, b) for a, b in zip(*grads))
+    # with a residual: y may be changed; h is what the backward pass reads, and changing it is refused there, as by any saved output
+    x, r = X.clone().requires_grad_(), R.clone().requires_grad_()
+    y, h = layer(x, r)
+    y.mul_(2.0)
+    (y + h).backward(dy)
+    x2, r2 = X.clone().requires_grad_(), R.clone().requires_grad_()
+    y2, h2 = layer(x2, r2)
+    (2.0 * y2 + h2).backward(dy)
+    assert torch.equal(x.grad, x2.grad) and torch.equal(r.grad, r2.grad)
+    y, h = layer(X.clone().requires_grad_(), R)
+    h.add_(1.0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        (y + h).backward(dy)
+    with torch.no_grad():
+        y, h = layer(X, R)
+        assert torch.equal(h.add_(1.0), X + R + 1.0)
