@@ -191,7 +191,9 @@ def rotary(X, table, positions=None, rotated=None, interleaved: bool = False, fi
 
 
 def clip_grad_norm_(parameters, max_norm: float):
-    """Clip the parameters' gradients in place to a global norm of ``max_norm``; returns the norm before (fp32 on the
-    device), without waiting for it.  Parameters without a gradient are left out."""
+    """Clip the gradients of ``parameters`` (or of one) in place to a global norm of ``max_norm``; returns the norm before
+    (fp32 on the device), without waiting for it.  Parameters without a gradient are left out."""
+    if isinstance(parameters, torch.Tensor):
+        parameters = [parameters]
     grads = [p.grad for p in parameters if p.grad is not None]
     return pamm.clip_grad_norm(grads, max_norm)

@@ -163,3 +163,14 @@ def test_outputs_of_the_norm_can_be_changed_in_place(shape):
     with torch.no_grad():
         y, h = layer(X, R)
         assert torch.equal(h.add_(1.0), X + R + 1.0)
+
+
+def test_clip_grad_norm_of_one_parameter():
+    p = torch.nn.Parameter(normal((33, 65), F32, 1))
+    p.grad = normal((33, 65), F32, 2)
+    before, total = p.grad.clone(), plain64.global_norm([p.grad])
+    norm = clip_grad_norm_(p, 0.5 * total)
+    assert abs(float(norm) - total) <= 1.01 * plain64.U * total
+    assert torch.allclose(p.grad, before * 0.5, rtol=1e-5)
+    p.grad = None
+    assert float(clip_grad_norm_(p, 1.0)) == 0.0
