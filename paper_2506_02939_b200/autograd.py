@@ -23,9 +23,9 @@ from . import pamm
 
 
 def _rows(t: torch.Tensor, cols: int) -> torch.Tensor:
-    """(…, cols) -> contiguous (rows, cols) view the library accepts (16-byte aligned rows)."""
+    """(…, cols) -> (rows, cols) view the library accepts (16-byte aligned rows that do not overlap)."""
     t2 = t.reshape(-1, cols)
-    if t2.stride(1) != 1 or (t2.stride(0) * t2.element_size()) % 16 or t2.data_ptr() % 16:
+    if t2.stride(1) != 1 or t2.stride(0) < cols or (t2.stride(0) * t2.element_size()) % 16 or t2.data_ptr() % 16:
         padded = pamm.alloc_matrix(t2.shape[0], cols, t2.dtype, t2.device)
         padded.copy_(t2)
         t2 = padded

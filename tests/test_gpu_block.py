@@ -174,3 +174,18 @@ def test_clip_grad_norm_of_one_parameter():
     assert torch.allclose(p.grad, before * 0.5, rtol=1e-5)
     p.grad = None
     assert float(clip_grad_norm_(p, 1.0)) == 0.0
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_the_gradient_of_rows_that_share_one_value_reaches_the_projection(dtype):
+    """The gradient of a sum over the rows is one row, repeated at distance zero."""
+    grads = []
+    for repeated in (True, False):
+        layer = PammLinear(64, 96, r=0.5, dtype=dtype)
+        with torch.no_grad():
+            layer.weight.copy_(normal((64, 96), F32, 1, 0.1))
+        x = normal((40, 64), dtype, 2).requires_grad_()
+        row = normal((96,), dtype, 3)
+        layer(x).backward(row.expand(40, 96) if repeated else row.repeat(40, 1))
+        grads.append((x.grad, layer.weight.grad))
+    assert all(torch.equal(a, b) for a, b in zip(*grads))
