@@ -466,7 +466,8 @@ def rotary_table(length: int, frequencies, amplitude: float = 1.0, first: int = 
             out = _empty((length, rot), dtype=torch.float32, device=device)
     if out.shape != (length, rot) or out.dtype != torch.float32 or not out.is_contiguous() or not out.is_cuda:
         raise ValueError(f"the table is a contiguous CUDA float32 matrix of {length} x {rot}")
-    _check(_lib.pamm_rotary_table(_ptr(freq), rot, amplitude, first, length, _ptr(out), _stream(stream)), "pamm_rotary_table")
+    with torch.cuda.device(out.device):
+        _check(_lib.pamm_rotary_table(_ptr(freq), rot, amplitude, first, length, _ptr(out), _stream(stream)), "pamm_rotary_table")
     return out
 
 

@@ -149,3 +149,33 @@ def test_the_largest_rotary_row_and_one_beyond():
         assert call(heads, d) == pamm.OK                  # of no sequence: nothing is launched
         assert call(heads, d + 1, 1) == call(heads, d + 1) == pamm.ERR_UNSUPPORTED
     assert call(2 ** 24 + 1, 2) == pamm.ERR_UNSUPPORTED
+
+
+def test_a_rotary_table_is_computed_on_its_own_device(monkeypatch):
+    """With stand-ins for a second device: the launch happens while the table's device is the current one."""
+    current, launched = [0], []
+
+    class Device:
+        def __init__(self, device):
+            self.index = torch.device(device).index
+
+        def __enter__(self):
+            self.before, current[0] = current[0], self.index
+
+        def __exit__(self, *_):
+            current[0] = self.before
+
+    class Table:
+        shape, dtype, device, is_cuda = (5, 8), torch.float32, torch.device("cuda", 1), True
+        is_contiguous, data_ptr = (lambda self: True), (lambda self: FAKE)
+
+    class Library:
+        def pamm_rotary_table(self, *args):
+            launched.append((current[0], args[-1]))
+            return pamm.OK
+
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(pamm, "_lib", Library())
+    monkeypatch.setattr(pamm, "_stream", lambda stream: ("the stream of", current[0]))
+    pamm.rotary_table(5, torch.ones(4, dtype=torch.float64), out=Table())
+    assert launched == [(1, ("the stream of", 1))] and current == [0]
