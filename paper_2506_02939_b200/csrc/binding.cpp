@@ -87,6 +87,14 @@ PyObject* value(E v) { return PyLong_FromLong((long)v); }
 template <typename... T>
 PyObject* keep(const T&... t) { return g_record ? tuple_of(t...) : nullptr; }
 
+// Lets other Python threads run, as ctypes does: a call waits where the launch queue is full.
+struct Unlocked {
+    PyThreadState* state = PyEval_SaveThread();
+    Unlocked() = default;
+    ~Unlocked() { PyEval_RestoreThread(state); }
+    Unlocked(const Unlocked&) = delete;
+};
+
 // `kept`: a new reference, given up here.
 template <typename F, typename... A>
 void call(const char* name, F function, PyObject* kept, A... a) {
@@ -102,7 +110,11 @@ void call(const char* name, F function, PyObject* kept, A... a) {
         if (rc < 0) throw Failure();
         return;
     }
-    const pamm_status s = function(a...);
+    pamm_status s;
+    {
+        const Unlocked unlocked;
+        s = function(a...);
+    }
     if (s != PAMM_OK) {
         PyObject* e = PyObject_CallFunction(g_error, "is", (int)s, name);
         if (e) {

@@ -2,6 +2,7 @@
 // Every step of the path runs in the kernels included below; nothing here
 // computes on the host apart from pamm_draw_indices_host.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdio>
 #include <cstring>
@@ -110,7 +111,7 @@ constexpr int64_t MAX_ROWS = (1ll << 31) - 1024;   // row ids, counts and offset
 
 // Kernel launches issued so far (all streams), and optional event pairs that
 // bracket the dominant kernel of a step so a benchmark can time it in place.
-unsigned long long g_launches = 0;
+std::atomic<unsigned long long> g_launches{0};
 cudaEvent_t g_prof[3][2] = {{nullptr, nullptr}, {nullptr, nullptr}, {nullptr, nullptr}};
 inline void prof_begin(int kind, cudaStream_t st) { if (g_prof[kind][0]) cudaEventRecord(g_prof[kind][0], st); }
 inline void prof_end(int kind, cudaStream_t st) { if (g_prof[kind][1]) cudaEventRecord(g_prof[kind][1], st); }

@@ -1,5 +1,6 @@
 """Calls of several Python threads."""
 import threading
+import time
 
 import pytest
 import torch
@@ -86,3 +87,34 @@ def test_an_operator_of_another_thread_runs_while_one_is_prepared():
     assert all(torch.equal(a, b) for a, b in zip(seen[0], wanted)) and not y.any()
     run()
     assert torch.equal(y, wanted[0])
+
+
+@pytest.mark.gpu
+def test_other_threads_go_on_while_a_call_waits_for_the_launch_queue():
+    x = torch.randn((64, 2, 64), device="cuda")
+    table = pamm.rotary_table(64, *pamm.rotary_frequencies(64))
+    out = torch.empty_like(x)
+    pamm.rotary(x, table, out=out)
+    torch.cuda.synchronize()
+    stop, gap = threading.Event(), [0.0]
+
+    def watch():
+        last = time.perf_counter()
+        while not stop.is_set():
+            time.sleep(0.001)
+            now = time.perf_counter()
+            gap[0] = max(gap[0], now - last)
+            last = now
+    t = threading.Thread(target=watch)
+    t.start()
+    longest = 0.0
+    torch.cuda._sleep(2_000_000_000)            # about a second of the device, which launches queue up behind
+    for _ in range(6000):
+        start = time.perf_counter()
+        pamm.rotary(x, table, out=out)
+        longest = max(longest, time.perf_counter() - start)
+    stop.set()
+    t.join()
+    torch.cuda.synchronize()
+    assert longest > 0.2, longest               # the queue was full: the call waited
+    assert gap[0] < 0.5 * longest, (gap[0], longest)
