@@ -2,17 +2,21 @@
 
 Argument marshalling only: every step of the path runs in the library's kernels.
 torch is used for device memory and streams.  The calls of the path are marshalled here
-through ctypes, those of the operators around the projection in ``_binding``.  Importing this module fails
-loudly when the library has not been built; there is no CPU fallback.
+through ctypes, those of the operators around the projection in ``_binding``, which is compiled against torch.  Importing
+this module fails loudly when the library has not been built, and those operators' calls when the binding has
+not been built for this Python and torch; there is no CPU fallback.
 """
 from __future__ import annotations
 
 import contextlib
 import ctypes
+import importlib.util
 import threading
 from pathlib import Path
 
 import torch
+
+from .build import binding_path
 
 _LIB_PATH = Path(__file__).resolve().parent / "libpamm_b200.so"
 if not _LIB_PATH.exists():
@@ -20,7 +24,38 @@ if not _LIB_PATH.exists():
         f"{_LIB_PATH} is missing: build it with `python -m paper_2506_02939_b200.build` "
         "(nvcc, sm_100a). The PAMM path has no fallback.")
 _lib = ctypes.CDLL(str(_LIB_PATH))
-from . import _binding  # noqa: E402  (linked against the library; built next to it)
+
+
+class _NoBinding:
+    """In the place of a binding that is not there: the path works, the operators' calls raise."""
+
+    def __init__(self, why):
+        self._why = why
+
+    def set_error(self, error):
+        pass
+
+    def set_record(self, record):
+        pass
+
+    def __getattr__(self, name):
+        raise ImportError(f"{name} needs the compiled binding: build it with `python -m paper_2506_02939_b200.build` ({self._why})")
+
+
+def _load_binding():
+    path = binding_path()
+    if not path.exists():
+        return _NoBinding(f"there is no {path.name}")
+    try:
+        spec = importlib.util.spec_from_file_location(f"{__package__}._binding", path)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+    except ImportError as e:
+        return _NoBinding(e)
+    return module
+
+
+_binding = _load_binding()
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT, ERR_BAD_INDEX = range(7)
 F32, BF16 = 0, 1
