@@ -19,8 +19,10 @@ constexpr int GC_UNROLL = 4;            // vectors in flight per thread
 constexpr int GC_BLOCKS_PER_SM = 8;     // of the sum: one wave
 // elements of a chunk: of the sum, by the size of the list; of the scaling
 constexpr int GC_MIN_CHUNK = 4096, GC_MAX_CHUNK = 65536, GC_SCALE_CHUNK = 16384;
-// list entries per launch: parameters of 1.8, 7 and 32 KB, so that a short list is not handed over as a long one
-constexpr int GC_SMALL = 24, GC_MEDIUM = 96, GC_LARGE = 448;
+// List entries per launch: a power of two, four times as many, and as many as the parameters of a launch hold (2.3, 9 and 32 KB).  What
+// a list has no use for still goes to the device with every launch.  Calls in place one after the other, of 4 and 28 small
+// tensors: with room for 32 4.7 and 5.3 us, for 128 5.1 and 5.7, for 448 7.0 and 7.7; of 40 and 120: for 128 6.0 and 8.3, for 448 8.0 and 10.0.
+constexpr int GC_SMALL = 32, GC_MEDIUM = 128, GC_LARGE = 448;
 
 struct GradEntry {
     const void* in;
