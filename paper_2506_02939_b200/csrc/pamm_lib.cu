@@ -871,9 +871,10 @@ pamm_status run_grad_clip(const pamm_tensor* in, const pamm_tensor* out, int64_t
     }
     const double* sums = partial;
     GradFactor* factor = (GradFactor*)(partial + round_up(grad_norm_blocks(), 32));
-    // sums that the scaling's blocks join themselves, while these are one wave at most: 1 to 2 us less (24 tensors of 25 MB in place 9.2 and
-    // 8.8 us on the device and a launch less on the host; but 19 MB into others 15.1 and 18.0 us)
-    int self = scale && total <= (out ? 4 << 20 : 14 << 20) ? parts : 0;
+    // Few sums are joined by each of the scaling's blocks, which saves a launch.  24 fp32 tensors, joined there and apart: in place, below the
+    // limit, 6 M elements 7.8 and 8.1 us, 14 M 13.4 and 13.4 (13.7 and 14.0 a call among others), 18 M 17.1 and 16.3; into others, where all blocks
+    // go on, 1 M 7.0 and 8.0, 2 M 7.9 and 8.6 (10.0 and 9.3 a call), 3 M 9.7 and 10.4 (12.2 and 11.5), 4 M 16.1 and 11.8
+    int self = scale && total <= (out ? 2 << 20 : 14 << 20) ? parts : 0;
     if (!self) launch_in_place((const void*)grad_norm_finish_kernel, 1, GC_THREADS, st, &sums, &parts, &max_norm, &norm, &factor);
     if (!scale) return launch_status();
     at = 0;
