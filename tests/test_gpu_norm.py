@@ -379,3 +379,79 @@ def test_extreme_rows_with_a_residual_in_and_out_of_place(b, n, dtype):
             keep[extreme] = False
             assert torch.equal(y1[keep], y[keep])
             assert plain64.within(y1[extreme], stored[0][extreme], plain64.stored(bs, stored[0], dtype)[extreme]) <= 1.0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n", [40, 2048, 2051, 20000])
+def test_gradients_of_rows_of_infinities_and_nan(n, dtype):
+    """NaN exactly where the formula has it, in dx, dw and dc; the other rows and columns as without them."""
+    x, _ = rows(6, n, dtype, 5)
+    x[2, n // 2] = float("inf")
+    x[3, n - 1] = float("nan")
+    dy, _ = rows(6, n, dtype, 6)
+    dy[4, 1] = float("nan")
+    dy[5, 2] = float("-inf")
+    w = vector(n, F32, 8)
+    for rms in (False, True):
+        _, _, mean, rstd = pamm.norm_forward(x, w, rms=rms)
+        dx, dw, dc = pamm.norm_backward(dy, x, mean, rstd, w, bias=True)
+        want = plain64.norm_backward(dy, x, mean, rstd, w, None, rms)
+        bounds = plain64.norm_backward_bounds(dy, x, mean, rstd, w, None, rms)
+        for got, wanted, bound, dt in zip((dx, dw, dc), want, bounds, (dtype, F32, F32)):
+            assert torch.equal(torch.isnan(got), torch.isnan(wanted))
+            fine = torch.isfinite(wanted)
+            assert torch.equal(got[~fine & ~torch.isnan(wanted)].double(), wanted[~fine & ~torch.isnan(wanted)])
+            assert plain64.within(got[fine], wanted[fine], plain64.stored(bound, wanted, dt)[fine]) <= 1.0
+
+
+@pytest.mark.parametrize("dtype,w_dtype", [(F32, F32), (BF16, BF16), (BF16, F32), (F32, BF16)])
+@pytest.mark.parametrize("n,b", [(40, 20001), (128, 20001), (250, 20001), (480, 20001), (481, 20001), (512, 20001), (1024, 20001), (2048, 20001), (1999, 9001)])
+def test_many_rows_in_every_form(n, b, dtype, w_dtype):
+    """Rows enough for the kernels of large batches: two rows a thread (an odd number of them), parts of a warp, a shared-memory
+    ring that goes round, with the residual, its gradient and the bias each there and not there."""
+    x, r = rows(b, n, dtype, 1)[0], rows(b, n, dtype, 2, 0.5)[0]
+    dy, dh = rows(b, n, dtype, 3, 1e-2)[0], rows(b, n, dtype, 4, 1e-2)[0]
+    w, c = vector(n, w_dtype, 5), vector(n, w_dtype, 6, 0.0)
+    for rms in (False, True):
+        for add in (False, True):
+            for bias in (False, True):
+                args = (x, w, c if bias else None, r if add else None, 1e-5, rms)
+                y, h, mean, rstd = pamm.norm_forward(x, w, args[2], residual=args[3], rms=rms)
+                want = plain64.norm_forward(*args)
+                by, bh, bm, bs = plain64.norm_forward_bounds(*args)
+                assert plain64.within(y, want[0], plain64.stored(by, want[0], dtype)) <= 1.0
+                assert plain64.within(rstd, want[3], plain64.stored(bs, want[3], F32)) <= 1.0
+                if add:
+                    assert plain64.within(h, want[1], plain64.stored(bh, want[1], dtype)) <= 1.0
+                if not rms:
+                    assert plain64.within(mean, want[2], plain64.stored(bm, want[2], F32)) <= 1.0
+                dx, dw, dc = pamm.norm_backward(dy, h, mean, rstd, w, bias=bias, dH=dh if add else None)
+                args = (dy, h, mean, rstd, w, dh if add else None, rms)
+                gx, gw, gc = plain64.norm_backward(*args)
+                bx, bw, bc = plain64.norm_backward_bounds(*args)
+                assert plain64.within(dx, gx, plain64.stored(bx, gx, dtype)) <= 1.0
+                assert plain64.within(dw, gw, plain64.stored(bw, gw, w_dtype)) <= 1.0
+                if bias:
+                    assert plain64.within(dc, gc, plain64.stored(bc, gc, w_dtype)) <= 1.0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("b,n", [(9001, 250), (9001, 509), (5001, 2048), (3001, 8200)])
+def test_many_rows_of_matrices_aligned_differently(b, n, dtype):
+    pads = [(0, 0), (1, 0), (8, 3), (5, 1)]             # of x, r (dy), y (dx), h (dh)
+    x, r = (rows(b, n, dtype, k, pad=pads[k][0], shift=pads[k][1])[0] for k in (0, 1))
+    w, c = vector(n, F32, 2), vector(n, F32, 3, 0.0)
+    for rms in (False, True):
+        (y, y_room), (h, h_room) = (rows(b, n, dtype, 0, pad=pads[k][0], shift=pads[k][1]) for k in (2, 3))
+        y, h, mean, rstd = pamm.norm_forward(x, w, c, residual=r, rms=rms, Y=y, H=h)
+        want = plain64.norm_forward(x, w, c, r, 1e-5, rms)
+        by, bh, _, _ = plain64.norm_forward_bounds(x, w, c, r, 1e-5, rms)
+        assert plain64.within(y, want[0], plain64.stored(by, want[0], dtype)) <= 1.0 and untouched(y, y_room, *pads[2])
+        assert plain64.within(h, want[1], plain64.stored(bh, want[1], dtype)) <= 1.0 and untouched(h, h_room, *pads[3])
+        dy, dh = (rows(b, n, dtype, 10 + k, 1e-2, *pads[k])[0] for k in (1, 3))
+        dx, dx_room = rows(b, n, dtype, 0, pad=pads[2][0], shift=pads[2][1])
+        dx, dw, dc = pamm.norm_backward(dy, h, mean, rstd, w, bias=True, dH=dh, dX=dx)
+        gx, gw, gc = plain64.norm_backward(dy, h, mean, rstd, w, dh, rms)
+        bx, bw, bc = plain64.norm_backward_bounds(dy, h, mean, rstd, w, dh, rms)
+        assert plain64.within(dx, gx, plain64.stored(bx, gx, dtype)) <= 1.0 and untouched(dx, dx_room, *pads[2])
+        assert plain64.within(dw, gw, plain64.stored(bw, gw, F32)) <= 1.0 and plain64.within(dc, gc, plain64.stored(bc, gc, F32)) <= 1.0
