@@ -167,3 +167,73 @@ def test_on_another_stream_in_a_graph_and_prepared():
         t.zero_()
     pamm.prepared(pamm.clip_grad_norm, g, 0.1, out=out)()
     assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+def bucket(total, dtype, seed, step=977):
+    """Views of odd sizes of one piece of memory."""
+    flat, views, at, i = normal((total,), dtype, seed), [], 0, 0
+    while at < total:
+        size = min(total - at, total // 40 + 1 + (i * step) % 5003)
+        views.append(flat[at:at + size])
+        at, i = at + size, i + 1
+    return views
+
+
+def large_lists():
+    """Total sizes on both sides of the switches of the scaling (2^21 elements into others, 14 2^20 in place) and of the sum's chunks."""
+    def apart(k):          # rows narrower and wider than a chunk, at a distance
+        return [normal((20_000 * k, 96), BF16, 1)[:, :91], normal((5, 70_008 * k), F32, 2)[:, 3:70_004 * k], normal((3000, 1), F32, 3)]
+    yield "2 M", bucket(2 ** 21 - 100, F32, 14)
+    yield "2 M and some", bucket(2 ** 21 + 100, BF16, 15)
+    yield "4 M", bucket(2 ** 22 - 100, BF16, 4)
+    yield "4 M and some", bucket(2 ** 22 + 100, F32, 5)
+    yield "rows apart", apart(1) + bucket(2_000_003, F32, 6) + bucket(1_000_001, BF16, 7)
+    yield "14 M", bucket(7 * 2 ** 20, BF16, 8) + bucket(7 * 2 ** 20 - 100, F32, 9)
+    yield "14 M and some", bucket(7 * 2 ** 20, BF16, 10) + bucket(7 * 2 ** 20 + 100, F32, 11)
+    yield "80 M", apart(4) + bucket(50_000_001, BF16, 12) + bucket(22_000_003, F32, 13)
+    yield "600 tensors", [normal((19_997 + 7 * i,), (BF16, F32)[i % 3 == 0], 100 + i) for i in range(600)]
+    yield "600 larger ones", [normal((59_999 + 7 * i,), (F32, BF16)[i % 3 == 0], 100 + i) for i in range(600)]
+
+
+LARGE = ["2 M", "2 M and some", "4 M", "4 M and some", "rows apart", "14 M", "14 M and some", "80 M", "600 tensors", "600 larger ones"]
+
+
+def check(grads, total, norm, limit, src, out):
+    factor = min(1.0, limit / (total + 1e-6))
+    got = pamm.clip_grad_norm(src, limit, out=out)
+    assert torch.equal(got, norm)
+    for g, s, t in zip(grads, src, src if out is None else out):
+        want = g.double() * factor
+        assert plain64.within(t, want, plain64.stored(2.1 * plain64.U * want.abs(), want, t.dtype)) <= 1.0
+        if out is not None:
+            assert torch.equal(s, g)
+        elif factor == 1.0:
+            assert torch.equal(t, g)
+
+
+@pytest.mark.parametrize("which", LARGE)
+def test_large_lists(which):
+    grads = next(g for name, g in large_lists() if name == which)
+    total = plain64.global_norm(grads)
+    norm = pamm.grad_norm(grads)
+    assert abs(float(norm) - total) <= 1.01 * plain64.U * total
+    assert torch.equal(norm, pamm.grad_norm(grads))
+    for limit in (0.3 * total, 2 * total + 1):
+        for out_dtype in (None, F32, BF16):
+            src = [torch.empty_strided(g.shape, g.stride(), dtype=g.dtype, device="cuda").copy_(g) for g in grads] if out_dtype is None else grads
+            out = None if out_dtype is None else [torch.empty_strided(g.shape, g.stride(), dtype=out_dtype, device="cuda") for g in grads]
+            check(grads, total, norm, limit, src, out)
+
+
+@pytest.mark.parametrize("size", [300, 200_000])
+@pytest.mark.parametrize("count", [1, 23, 24, 25, 31, 32, 33, 95, 96, 97, 127, 128, 129, 447, 448, 449, 897])
+def test_any_number_of_tensors(count, size):
+    """Lists around what one launch holds, of tensors that the scaling joins the sums of itself and that it does not."""
+    if size * count > 30_000_000:
+        size = 30_000_000 // count
+    grads = [normal((size + i % 5,), (BF16, F32)[i % 2], 100 + i) for i in range(count)]
+    total = plain64.global_norm(grads)
+    norm = pamm.grad_norm(grads)
+    assert abs(float(norm) - total) <= 1.01 * plain64.U * total
+    check(grads, total, norm, 0.4 * total, grads, [torch.empty_like(g) for g in grads])
+    check(grads, total, norm, 0.4 * total, [g.clone() for g in grads], None)
