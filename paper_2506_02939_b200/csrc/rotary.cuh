@@ -17,15 +17,18 @@ constexpr int ROTARY_MAX_ROT = 512;
 constexpr int64_t ROTARY_MAX_ROW = 1 << 24;       // heads times head_dim
 constexpr int ROTARY_THREADS = 256;
 
-// Division of 0 <= n < 2^31 by a fixed d >= 1: a product with 2^32 (2^l / d - 1), rounded up, and a shift by l = ceil(log2 d).
+// Division of 0 <= n < 2^31 by a fixed 1 <= d < 2^31 as a product with a rounded-up reciprocal: Granlund and Montgomery, Division by
+// Invariant Integers using Multiplication (PLDI 1994), theorem 4.2 for N = 31.  With l = ceil(log2 d) and m = ceil(2^(31 + l) / d), which
+// fits 32 bits, n / d = n m >> (31 + l); of 2 n, which fits as well, the product's upper half has 32 of those places off.
 struct Divisor {
-    uint32_t d, factor, shift;
-    __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return (__umulhi(n, factor) + n) >> shift; }
+    uint32_t d, reciprocal, shift;
+    __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return __umulhi(2 * n, reciprocal) >> shift; }
 };
 inline Divisor make_divisor(uint32_t d) {
-    uint32_t l = 0;
-    while ((1ull << l) < d) ++l;
-    return {d, (uint32_t)(((1ull << 32) * ((1ull << l) - d)) / d + 1), l};
+    uint32_t log = 0;
+    while ((uint64_t)d > (1ull << log)) ++log;
+    const uint64_t dividend = 1ull << (31 + log);
+    return {d, (uint32_t)((dividend + d - 1) / d), log};
 }
 
 struct RotaryArgs {
