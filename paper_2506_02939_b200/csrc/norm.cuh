@@ -209,7 +209,7 @@ __device__ __forceinline__ void norm_forward_shrunk_row(const NormForwardArgs& a
 
 // Measured on 65536 x 2048 bf16 (268 MB a matrix): the 16-byte copy of the same streams in one-shot blocks runs at 6.5 to
 // 6.7 TB/s, in persistent ones at 6.0, hence a block (or a part of one) for its rows and no loop over rows.
-// 158 us with the residual addition (6.8 TB/s), 84 without.  A thread may have ROWS = 2 rows, which share its weights (the launch says when).  8 elements a thread repeat the row's
+// 158 us with the residual addition (6.8 TB/s), 85 without.  A thread may have ROWS = 2 rows, which share its weights (the launch says when).  8 elements a thread repeat the row's
 // overhead in more threads and are for calls with few rows, where the time is one row's latency.
 template <typename T, typename W, int V, int EPT, int LANES, int ROWS, bool RAGGED>
 __global__ void __launch_bounds__(1024)

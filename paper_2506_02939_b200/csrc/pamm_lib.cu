@@ -637,15 +637,15 @@ pamm_status launch_norm_forward(const NormForwardArgs& a, cudaStream_t st) {
     const int64_t thin_warps = (a.n + 255) / 256;
     const bool many = a.b >= 32 * sm_count();
     if (a.n <= 64 && !RAGGED) return launch_norm_forward<T, W, V, 8, RAGGED ? 16 : 8, 1, RAGGED>(a, st);
-    // 8 elements a thread, and 16 or 32 where there are rows enough: 10^6 x 128 bf16 101 and 90 us, 500000 x 256 107 and 90, 262144 x 512 with bias
-    // (16 elements of a row or of two, and 32) 111, 95 and 88
+    // 8 elements a thread, and 16 or 32 where there are rows enough: 10^6 x 128 bf16 101 and 92 us, 500000 x 256 107 and 91, 262144 x 512 with bias
+    // (16 elements of a row or of two, and 32) 111, 95 and 91
     if (a.n <= 128 && !RAGGED && many) return launch_norm_forward<T, W, V, 16, RAGGED ? 16 : 8, 1, RAGGED>(a, st);
     if (a.n <= 128 && !many) return launch_norm_forward<T, W, V, 8, 16, 1, RAGGED>(a, st);
     if (a.n <= 256 && many) return launch_norm_forward<T, W, V, 16, 16, 1, RAGGED>(a, st);
     if (thin_warps <= 32 && (thin_warps == 1 || a.b * thin_warps <= 8 * sm_count())) return launch_norm_forward<T, W, V, 8, 32, 1, RAGGED>(a, st);
     if (a.n <= 512 && many && V > 1) return launch_norm_forward<T, W, V, (V > 1 ? 32 : 16), 16, 1, RAGGED>(a, st);
     // Two rows a thread where the weights weigh: fp32 weights, beside bf16 rows with a bias too.  Both sides measured, one row and two: 65536 x 2048
-    // bf16 with fp32 weights and bias 124 and 102, with bf16 ones 93 and 98, with bf16 weights alone 84 and 89; 32768 x 2048 fp32 85
+    // bf16 with fp32 weights and bias 124 and 98, with bf16 ones 93 and 98, with bf16 weights alone 85 and 89; 32768 x 2048 fp32 85
     // and 81.
     if constexpr (V > 1 && !RAGGED)
         if (a.n <= 4096 && sizeof(W) == 4 && (sizeof(T) == 4 || a.c) && a.b * ((a.n + 511) / 512) >= 64 * sm_count())
