@@ -122,7 +122,7 @@ class NormFunction(torch.autograd.Function):
         H = None if residual is None else torch.empty(X.shape, dtype=X.dtype, device=X.device)
         _, _, mean, rstd = pamm.norm_forward(X2, w, c, residual=R2, eps=eps, rms=rms, Y=Y.view(-1, n), H=None if H is None else H.view(-1, n))
         ctx.save_for_backward(X2 if H is None else H, mean, rstd, weight)
-        ctx.shape, ctx.has_residual = X.shape, residual is not None
+        ctx.shape, ctx.residual_shape = X.shape, None if residual is None else residual.shape
         ctx.vector_type = weight.dtype if weight is not None else bias.dtype if bias is not None else X.dtype
         ctx.set_materialize_grads(False)
         return Y if residual is None else (Y, H)
@@ -142,8 +142,10 @@ class NormFunction(torch.autograd.Function):
                                         bias=need_c, dH=None if dH is None else _matrix(dH.to(H.dtype), n),
                                         need_dw=need_w or need_c, dw_dtype=ctx.vector_type)
         dX = dX.reshape(ctx.shape)
-        return (dX if ctx.needs_input_grad[0] else None, dw if need_w else None, dc if need_c else None,
-                dX if ctx.has_residual and ctx.needs_input_grad[3] else None, None, None)
+        dR = None
+        if ctx.needs_input_grad[3]:         # one tensor for both inputs, which autograd then copies; a view of it would be shared
+            dR = dX if ctx.residual_shape == ctx.shape else dX.reshape(ctx.residual_shape).clone()
+        return dX if ctx.needs_input_grad[0] else None, dw if need_w else None, dc if need_c else None, dR, None, None
 
 
 class Norm(torch.nn.Module):

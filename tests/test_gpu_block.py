@@ -189,3 +189,11 @@ def test_the_gradient_of_rows_that_share_one_value_reaches_the_projection(dtype)
         layer(x).backward(row.expand(40, 96) if repeated else row.repeat(40, 1))
         grads.append((x.grad, layer.weight.grad))
     assert all(torch.equal(a, b) for a, b in zip(*grads))
+
+
+def test_the_gradient_of_a_residual_has_its_own_shape():
+    layer = Norm(64, dtype=F32)
+    X, R = normal((2, 3, 64), F32, 1).requires_grad_(), normal((6, 64), F32, 2).requires_grad_()       # rows of another shape
+    dy, dh = normal((2, 3, 64), F32, 3), normal((2, 3, 64), F32, 4)
+    torch.autograd.backward(layer(X, R), (dy, dh))
+    assert R.grad.shape == R.shape and torch.equal(R.grad, X.grad.view(6, 64)) and R.grad.data_ptr() != X.grad.data_ptr()
