@@ -73,7 +73,8 @@ typedef enum {
     PAMM_WS_CONTRACT = 1,            /* also covers pamm_contract_weight_grad */
     PAMM_WS_STEP_HOST = 2,           /* device arena of pamm_qkv_step_host    */
     PAMM_WS_NORM_BACKWARD = 3,       /* pamm_norm_backward of b rows of n (m and k are not looked at; b may be 0) */
-    PAMM_WS_GRAD_NORM = 4            /* pamm_grad_norm, pamm_clip_grad_norm (no size is looked at) */
+    PAMM_WS_GRAD_NORM = 4,           /* pamm_grad_norm, pamm_clip_grad_norm (no size is looked at) */
+    PAMM_WS_ATTENTION_BACKWARD = 5   /* pamm_attention_backward of b tokens (of all sequences) and n query heads (m, k and dt are not looked at) */
 } pamm_ws_kind;
 
 /* Human-readable name of a status code (static string, never NULL). */
@@ -476,6 +477,65 @@ typedef struct {
 pamm_status pamm_grad_norm(const pamm_tensor* grads, int64_t count, float* norm, void* workspace, size_t ws_bytes, void* stream);
 pamm_status pamm_clip_grad_norm(const pamm_tensor* grads, const pamm_tensor* out, int64_t count, double max_norm, float* norm,
                                 void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Attention over the heads of the fused row [Q|K|V].  Query head h of a token reads key and value head h / (heads / kv_heads).
+ * With J(i) the valid tokens of token i's sequence, up to i itself where `causal` is set:
+ *   s_ij = scale q_i k_j;  lse_i = log sum_{j in J(i)} exp(s_ij);  o_i = sum_{j in J(i)} exp(s_ij - lse_i) v_j
+ * A token that is not valid has o = 0 and lse = -infinity, and nothing of it reaches another token, whatever its row holds (NaN
+ * and infinities too).  Among valid tokens a value that is not finite reaches what the formulas say, and may reach other
+ * rows of its sequence as 0 times infinity does.
+ *   pamm_heads   element (b, s, h, d) of a tensor lies at data + b batch + s token + h head + d, distances in elements, of any
+ *                sign and order; 0 repeats (not in outputs).  Q, O: `heads` heads; K, V: kv_heads, a divisor.
+ *   lse          batch x heads x seq fp32, contiguous; NULL in the forward call: not wanted
+ *   scale        positive and finite
+ *   lengths      NULL, or `batch` entries: the first lengths[b] tokens of sequence b are valid
+ *   starts       NULL, or sequences + 1 entries that do not fall: packed sequences along the one token axis of batch = 1; sequence i
+ *                has the tokens starts[i] .. starts[i+1] - 1, all of them valid; tokens before starts[0] and from
+ *                starts[sequences] on are in no sequence: not valid
+ *   index_type   of lengths or starts (device arrays; one of them at most)
+ * An entry that is negative, larger than seq or falls raises PAMM_ERR_BAD_INDEX in the device status and is taken as the nearest
+ * possible one.  No output overlaps an input or another output.  Limits: head_dim <= 256, batch x seq x heads < 2^40,
+ * seq < 2^31 - 1024, fewer than 2^31 tiles of 64 rows over all heads and sequences.
+ * bf16 heads of up to 128, in multiples of 8, with 16-byte aligned rows are computed on the tensor cores, with probabilities (and, in
+ * the backward pass, score gradients) rounded to bf16 as operands of their products; everything else is fp32.
+ */
+typedef struct {
+    void* data;
+    int64_t batch, token, head;
+} pamm_heads;
+pamm_status pamm_attention_forward(const pamm_heads* Q, const pamm_heads* K, const pamm_heads* V, const pamm_heads* O, float* lse,
+                                   int64_t batch, int64_t seq, int64_t heads, int64_t kv_heads, int64_t head_dim, pamm_dtype dt,
+                                   float scale, int causal, const void* lengths, const void* starts, int64_t sequences,
+                                   pamm_position_type index_type, void* stream);
+
+/*
+ * Its backward pass, which makes the probabilities anew:
+ *   p_ij = exp(s_ij - lse_i);  delta_i = do_i o_i;  ds_ij = p_ij (do_i v_j - delta_i)
+ *   dq_i = scale sum_j ds_ij k_j;  dk_j = scale sum_i ds_ij q_i;  dv_j = sum_i p_ij do_i
+ * (dk, dv: over the query heads that share the head).  O and lse are the forward call's; the gradients of tokens that are not
+ * valid are zero, and what dO holds there is not looked at.  Every sum is taken in a fixed order.
+ *   workspace  pamm_workspace_bytes(PAMM_WS_ATTENTION_BACKWARD, batch * seq, heads, ...)
+ */
+pamm_status pamm_attention_backward(const pamm_heads* dO, const pamm_heads* Q, const pamm_heads* K, const pamm_heads* V,
+                                    const pamm_heads* O, const float* lse, const pamm_heads* dQ, const pamm_heads* dK,
+                                    const pamm_heads* dV, int64_t batch, int64_t seq, int64_t heads, int64_t kv_heads,
+                                    int64_t head_dim, pamm_dtype dt, float scale, int causal, const void* lengths, const void* starts,
+                                    int64_t sequences, pamm_position_type index_type, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Dropout with a residual:  y = r + (kept ? x / (1 - p) : 0), fp32, rounded once to dt.  The mask is never stored: element
+ * e = row n + column is kept where word e % 4 of the block of counter (e / 4, offset), 64 bits each, of Philox 4x32 with
+ * ten rounds (Salmon et al., SC 2011) under the key `seed` is not below floor(p 2^32).  The same seed, offset and
+ * shape give the same mask, so the gradient of X is this call on the gradient of Y, without R.
+ *   R        b x n or NULL: 0
+ *   p        0 <= p <= 1; with 1 nothing is kept
+ *   counter  NULL, or one number on the device that is added to `offset` (modulo 2^64) when the call runs: a captured graph
+ *            gets a fresh mask in every replay from a program that counts it up in between
+ * Y may be X or R (the same base and leading dimension).
+ */
+pamm_status pamm_dropout(const void* X, int64_t ldx, const void* R, int64_t ldr, int64_t b, int64_t n, pamm_dtype dt, double p,
+                         uint64_t seed, uint64_t offset, const int64_t* counter, void* Y, int64_t ldy, void* stream);
 
 /*
  * Reads and clears the current device's status word WITHOUT waiting for any of the

@@ -10,8 +10,8 @@ the input gradient ``dX = dZ W^T`` is exact (for bf16 layers the library's tenso
 with m = |Q| + |K| + |V|, as in the paper's notation.
 
 Around it: ``Norm`` (layer norm or its root-mean-square form, with the residual addition), whose
-output is the projection's input; ``rotary`` on the heads of the projection's output; and
-``clip_grad_norm_`` for the end of a training step.
+output is the projection's input; ``rotary`` on the heads of the projection's output; ``attention`` over
+them; ``dropout`` with the residual addition; and ``clip_grad_norm_`` for the end of a training step.
 """
 from __future__ import annotations
 
@@ -190,6 +190,93 @@ def rotary(X, table, positions=None, rotated=None, interleaved: bool = False, fi
     ``pamm.rotary``; the other heads (V of the fused row) pass through.  ``inplace`` turns X itself, which must not be a leaf
     or needed by the backward pass of what made it (the projection's output is neither)."""
     return RotaryFunction.apply(X, table, positions, rotated, interleaved, first, inplace)
+
+
+class AttentionFunction(torch.autograd.Function):
+    """``pamm.attention_forward`` / ``attention_backward`` on the fused row.  Saved: the row itself, O, the rows' log-sums, and the
+    lengths or starts; the gradient is one row [dQ|dK|dV], as the projection takes it."""
+
+    @staticmethod
+    def forward(ctx, Z, lengths, starts, kv_heads, causal, scale):
+        Zd = Z.detach()
+        if Zd.shape[-1] > 1 and Zd.stride(-1) != 1:
+            Zd = Zd.contiguous()
+        heads = Zd.shape[-2] - 2 * kv_heads
+        ctx.parts = (heads, kv_heads, kv_heads)
+        ctx.how = dict(causal=causal, scale=scale)
+        O, lse = pamm.attention_forward(*Zd.split(ctx.parts, -2), lengths=lengths, starts=starts, **ctx.how)
+        ctx.save_for_backward(Z if Zd.data_ptr() == Z.data_ptr() else Zd, O, lse, lengths, starts)
+        return O
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dO):
+        Z, O, lse, lengths, starts = ctx.saved_tensors
+        Zd = Z.detach()
+        dO = dO.to(Zd.dtype)
+        if dO.shape[-1] > 1 and dO.stride(-1) != 1:
+            dO = dO.contiguous()
+        dZ = torch.empty(Zd.shape, dtype=Zd.dtype, device=Zd.device)
+        dQ, dK, dV = dZ.split(ctx.parts, -2)
+        pamm.attention_backward(dO, *Zd.split(ctx.parts, -2), O, lse, lengths=lengths, starts=starts, dQ=dQ, dK=dK, dV=dV, **ctx.how)
+        return dZ, None, None, None, None, None
+
+
+def attention(Z, kv_heads, lengths=None, starts=None, causal: bool = True, scale: float | None = None):
+    """Attention over the fused row: Z is (batch, tokens, heads + 2 kv_heads, head_dim), or (tokens, ...) with packed sequences between
+    ``starts``; its last 2 ``kv_heads`` heads are K and V, shared evenly by the others.  Returns the heads' outputs in Q's shape; tokens
+    from ``lengths`` on have zero outputs and gradients.  See ``pamm.attention_forward``."""
+    if not 0 < 2 * kv_heads < Z.shape[-2]:
+        raise ValueError(f"{kv_heads} heads of K and as many of V leave none for Q in a row of {Z.shape[-2]}")
+    return AttentionFunction.apply(Z, lengths, starts, int(kv_heads), bool(causal), scale)
+
+
+class DropoutFunction(torch.autograd.Function):
+    """``pamm.dropout``.  No mask is kept: the backward pass makes it again from the seed, the offset and the counter."""
+
+    @staticmethod
+    def forward(ctx, X, residual, counter, p, seed, offset):
+        ctx.save_for_backward(counter)
+        ctx.how = (p, seed, offset)
+        R = None if residual is None else residual.detach().to(X.dtype).contiguous()
+        ctx.residual = None if residual is None else residual.dtype
+        return pamm.dropout(X.detach().contiguous(), p, seed, offset, counter=counter, residual=R)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dY):
+        counter, = ctx.saved_tensors
+        p, seed, offset = ctx.how
+        dX = pamm.dropout(dY.contiguous(), p, seed, offset, counter=counter) if ctx.needs_input_grad[0] else None
+        return dX, dY.to(ctx.residual) if ctx.needs_input_grad[1] else None, None, None, None, None
+
+
+def dropout(X, p: float, seed: int, offset: int = 0, counter=None, residual=None):
+    """``residual`` + X / (1 - p) where the generator keeps it, as ``pamm.dropout``; ``residual`` has X's shape.  A ``counter`` must not
+    change between the forward and the backward pass."""
+    if residual is not None and residual.shape != X.shape:
+        raise ValueError("the residual has X's shape")
+    return DropoutFunction.apply(X, residual, counter, float(p), int(seed), int(offset))
+
+
+class Dropout(torch.nn.Module):
+    """Dropout with an optional residual addition, ``dropout(X)`` or ``dropout(X, residual)``: a fresh mask every call, the same ones for
+    the same ``seed``.  In evaluation mode X (+ residual) passes.  Two modules with one seed have the same masks: give each its own.
+
+    ``counter``: a one-element int64 tensor on the device that numbers the calls in a captured graph (counted up by the program
+    between replays); without it a graph replays the mask that it was captured with."""
+
+    def __init__(self, p: float = 0.1, seed: int = 0, counter=None):
+        super().__init__()
+        if not 0.0 <= p <= 1.0:
+            raise ValueError(f"p is a probability, got {p}")
+        self.p, self.seed, self.counter, self.calls = float(p), int(seed), counter, 0
+
+    def forward(self, X, residual=None):
+        if not self.training or self.p == 0.0:
+            return X if residual is None else X + residual
+        self.calls += 1
+        return dropout(X, self.p, self.seed, self.calls << 32, self.counter, residual)
 
 
 def clip_grad_norm_(parameters, max_norm: float):

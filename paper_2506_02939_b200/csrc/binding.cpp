@@ -1,4 +1,4 @@
-// The Python side of the operators around the projection (norm, rotary positions, gradient clipping):
+// The Python side of the operators around the projection (norm, rotary positions, attention, dropout, gradient clipping):
 // argument checks, output allocation and the C call, without the interpreter in between.  A call of a few
 // rows runs for two microseconds on the GPU; marshalling it in Python took seventeen, and a list of 192
 // gradients 380.
@@ -15,6 +15,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
 #include <cstring>
 #include <vector>
 
@@ -377,6 +378,188 @@ PyObject* clip(PyObject* const* o) {
     return wrapped(norm);
 }
 
+// ---- attention --------------------------------------------------------------------------------------------------
+// The sizes that Q, K and V give, and the tensors as the library takes them.
+struct AttentionCall {
+    const Place at;
+    const int64_t dims;
+    int64_t batch, seq, heads, kv_heads, d, sequences = 0;
+    pamm_dtype dt;
+    c10::ScalarType type;
+    pamm_position_type index_type = PAMM_POS_I32;
+    const void *lengths = nullptr, *starts = nullptr;
+    bool causal;
+    float scale;
+
+    AttentionCall(const Tensor& Q, const Tensor& K, const Tensor& V, PyObject* causal_, PyObject* lengths_, PyObject* starts_, PyObject* scale_)
+        : at(Q, "Q"), dims(Q.dim()) {
+        dt = type_of(Q, "Q");
+        type = Q.scalar_type();
+        if (dims != 3 && dims != 4)
+            fail(PyExc_ValueError, "Q is (tokens, heads, head_dim) or (batch, tokens, heads, head_dim), got %lld dimensions", (long long)dims);
+        if (K.dim() != dims) fail(PyExc_ValueError, "K has as many dimensions as Q");
+        batch = dims == 4 ? Q.size(0) : 1;
+        seq = Q.size(dims - 3);
+        heads = Q.size(dims - 2);
+        d = Q.size(dims - 1);
+        kv_heads = K.size(dims - 2);
+        if (heads > 0 && (kv_heads < 1 || heads % kv_heads))
+            fail(PyExc_ValueError, "%lld query heads cannot share %lld key heads evenly", (long long)heads, (long long)kv_heads);
+        holds(Q, "Q", heads);
+        holds(K, "K", kv_heads);
+        holds(V, "V", kv_heads);
+        causal = truth(causal_);
+        const double s = is_none(scale_) ? 1.0 / std::sqrt((double)(d > 0 ? d : 1)) : number(scale_);
+        scale = (float)s;
+        const Tensor l = optional_tensor(lengths_, "lengths"), b = optional_tensor(starts_, "starts");
+        if (l.defined() && b.defined()) fail(PyExc_ValueError, "lengths are for padded batches, starts for packed sequences: give one of them");
+        if (l.defined()) lengths = entries(l, "lengths", batch);
+        if (b.defined()) {
+            if (dims != 3) fail(PyExc_ValueError, "packed sequences are (tokens, heads, head_dim)");
+            if (b.dim() != 1 || b.size(0) < 1) fail(PyExc_ValueError, "starts are a vector of one entry more than there are sequences");
+            sequences = b.size(0) - 1;
+            starts = entries(b, "starts", sequences + 1);
+        }
+    }
+    const void* entries(const Tensor& t, const char* what, int64_t n) {
+        at.holds(t, what);
+        if (t.scalar_type() != at::kInt && t.scalar_type() != at::kLong) fail(PyExc_TypeError, "%s are int32 or int64, got %s", what, text(t.scalar_type()));
+        if (t.dim() != 1 || t.size(0) != n || !t.is_contiguous()) fail(PyExc_ValueError, "%s are a contiguous vector of %lld", what, (long long)n);
+        index_type = t.scalar_type() == at::kInt ? PAMM_POS_I32 : PAMM_POS_I64;
+        return t.data_ptr();
+    }
+    void holds(const Tensor& t, const char* what, int64_t count) const {
+        at.holds(t, what);
+        if (t.scalar_type() != type) fail(PyExc_TypeError, "%s is of %s, got %s", what, text(type), text(t.scalar_type()));
+        if (t.dim() != dims || (dims == 4 && t.size(0) != batch) || t.size(dims - 3) != seq || t.size(dims - 2) != count || t.size(dims - 1) != d)
+            fail(PyExc_ValueError, "%s is of %lld sequences of %lld tokens of %lld heads of %lld", what, (long long)batch, (long long)seq,
+                 (long long)count, (long long)d);
+        if (d > 1 && t.stride(dims - 1) != 1) fail(PyExc_ValueError, "%s needs contiguous heads", what);
+    }
+    void output(const Tensor& t, const char* what, int64_t count) const {
+        holds(t, what, count);
+        for (int64_t i = 0; i < dims; ++i)
+            if (t.size(i) > 1 && t.stride(i) == 0) fail(PyExc_ValueError, "%s needs heads that do not overlap", what);
+    }
+    pamm_heads view(const Tensor& t) const { return {t.data_ptr(), dims == 4 ? t.stride(0) : 0, t.stride(dims - 3), t.stride(dims - 2)}; }
+    std::vector<int64_t> shape(int64_t count) const {
+        return dims == 4 ? std::vector<int64_t>{batch, seq, count, d} : std::vector<int64_t>{seq, count, d};
+    }
+    std::vector<int64_t> row_shape() const {
+        return dims == 4 ? std::vector<int64_t>{batch, heads, seq} : std::vector<int64_t>{heads, seq};
+    }
+    float* rows(const Tensor& t, const char* what) const {
+        at.holds(t, what);
+        if (t.scalar_type() != at::kFloat || !t.is_contiguous() || t.sizes() != at::IntArrayRef(row_shape()))
+            fail(PyExc_ValueError, "%s is a contiguous float32 tensor of %lld x %lld x %lld", what, (long long)batch, (long long)heads, (long long)seq);
+        return (float*)t.data_ptr();
+    }
+};
+
+// The tensors' descriptions where the library finds them: on the stack, or with a call that is written down.
+template <int N, typename... T>
+const pamm_heads* described(const pamm_heads (&local)[N], PyObject*& kept, const T&... owned) {
+    if (!g_record) return local;
+    const Held bytes(PyBytes_FromStringAndSize((const char*)local, sizeof local));
+    const Held tensors(tuple_of(owned...));
+    kept = PyTuple_Pack(2, bytes.o, tensors.o);
+    if (!kept) throw Failure();
+    return (const pamm_heads*)PyBytes_AS_STRING(bytes.o);
+}
+
+PyObject* attention_forward(PyObject* const* o) {
+    const Tensor &Q = tensor(o[0], "Q"), &K = tensor(o[1], "K"), &V = tensor(o[2], "V");
+    Tensor O = optional_tensor(o[7], "O"), lse = optional_tensor(o[8], "lse");
+    const AttentionCall c(Q, K, V, o[3], o[4], o[5], o[6]);
+    if (O.defined()) c.output(O, "O", c.heads);
+    else O = c.at.empty(c.shape(c.heads), c.type);
+    if (!lse.defined()) lse = c.at.empty(c.row_shape(), at::kFloat);
+    float* rows = c.rows(lse, "lse");
+    const pamm_heads local[4] = {c.view(Q), c.view(K), c.view(V), c.view(O)};
+    PyObject* kept = nullptr;
+    const pamm_heads* t = described(local, kept, O, lse);
+    call("pamm_attention_forward", pamm_attention_forward, kept, t, t + 1, t + 2, t + 3, rows, c.batch, c.seq, c.heads, c.kv_heads, c.d, c.dt,
+         c.scale, (int)c.causal, c.lengths, c.starts, c.sequences, c.index_type, c.at.stream());
+    return tuple_of(O, lse);
+}
+
+PyObject* attention_backward(PyObject* const* o) {
+    const Tensor &dO = tensor(o[0], "dO"), &Q = tensor(o[1], "Q"), &K = tensor(o[2], "K"), &V = tensor(o[3], "V"), &O = tensor(o[4], "O");
+    const Tensor& lse = tensor(o[5], "lse");
+    Tensor dQ = optional_tensor(o[10], "dQ"), dK = optional_tensor(o[11], "dK"), dV = optional_tensor(o[12], "dV");
+    Tensor workspace = optional_tensor(o[13], "workspace");
+    const AttentionCall c(Q, K, V, o[6], o[7], o[8], o[9]);
+    c.holds(dO, "dO", c.heads);
+    c.holds(O, "O", c.heads);
+    const float* rows = c.rows(lse, "lse");
+    if (!dQ.defined() && !dK.defined() && !dV.defined()) {      // one row [dQ|dK|dV], as the projection's backward pass takes it
+        const Tensor dZ = c.at.empty(c.shape(c.heads + 2 * c.kv_heads), c.type);
+        dQ = dZ.narrow(-2, 0, c.heads);
+        dK = dZ.narrow(-2, c.heads, c.kv_heads);
+        dV = dZ.narrow(-2, c.heads + c.kv_heads, c.kv_heads);
+    }
+    const auto given = [&](Tensor& t, const char* what, int64_t count) {
+        if (t.defined()) c.output(t, what, count);
+        else t = c.at.empty(c.shape(count), c.type);
+    };
+    given(dQ, "dQ", c.heads);
+    given(dK, "dK", c.kv_heads);
+    given(dV, "dV", c.kv_heads);
+    if (!workspace.defined()) {
+        const size_t bytes = pamm_workspace_bytes(PAMM_WS_ATTENTION_BACKWARD, c.batch * c.seq, c.heads, 1, 1, c.dt);
+        workspace = c.at.empty({bytes == (size_t)-1 ? 256 : (int64_t)bytes}, at::kByte);
+    }
+    workspace_ok(c.at, workspace);
+    const pamm_heads local[8] = {c.view(dO), c.view(Q), c.view(K), c.view(V), c.view(O), c.view(dQ), c.view(dK), c.view(dV)};
+    PyObject* kept = nullptr;
+    const pamm_heads* t = described(local, kept, dQ, dK, dV, workspace);
+    call("pamm_attention_backward", pamm_attention_backward, kept, t, t + 1, t + 2, t + 3, t + 4, rows, t + 5, t + 6, t + 7, c.batch, c.seq,
+         c.heads, c.kv_heads, c.d, c.dt, c.scale, (int)c.causal, c.lengths, c.starts, c.sequences, c.index_type, workspace.data_ptr(),
+         (size_t)workspace.numel(), c.at.stream());
+    return tuple_of(dQ, dK, dV);
+}
+
+// ---- dropout ----------------------------------------------------------------------------------------------------
+uint64_t word(PyObject* o) {
+    const unsigned long long v = PyLong_AsUnsignedLongLong(o);
+    if (v == (unsigned long long)-1 && PyErr_Occurred()) throw Failure();
+    return v;
+}
+
+PyObject* dropout(PyObject* const* o) {
+    const Tensor& X = tensor(o[0], "X");
+    const double p = number(o[1]);
+    const uint64_t seed = word(o[2]), offset = word(o[3]);
+    const Tensor counter = optional_tensor(o[4], "counter"), R = optional_tensor(o[5], "residual");
+    Tensor Y = optional_tensor(o[6], "Y");
+    const pamm_dtype dt = type_of(X, "X");
+    const Place at(X, "X");
+    if (!Y.defined()) Y = at.empty(X.sizes(), X.scalar_type());
+    int64_t b = 1, n = X.numel(), ldx = n, ldr = n, ldy = n;
+    const auto like = [&](const Tensor& t, const char* what) {
+        at.holds(t, what);
+        if (t.sizes() != X.sizes()) fail(PyExc_ValueError, "%s is of X's shape", what);
+        if (t.scalar_type() != X.scalar_type()) fail(PyExc_TypeError, "%s is of %s, got %s", what, text(X.scalar_type()), text(t.scalar_type()));
+    };
+    like(Y, "Y");
+    if (R.defined()) like(R, "the residual");
+    if (!X.is_contiguous() || !Y.is_contiguous() || (R.defined() && !R.is_contiguous())) {
+        if (X.dim() != 2) fail(PyExc_ValueError, "X, Y and the residual are contiguous, or matrices with contiguous rows");
+        b = X.size(0);
+        n = X.size(1);
+        ldx = matrix(at, X, "X", b, n, X.scalar_type());
+        ldy = matrix(at, Y, "Y", b, n, X.scalar_type());
+        if (R.defined()) ldr = matrix(at, R, "the residual", b, n, X.scalar_type());
+    }
+    if (counter.defined()) {
+        at.holds(counter, "counter");
+        if (counter.numel() != 1 || counter.scalar_type() != at::kLong) fail(PyExc_ValueError, "counter is one int64");
+    }
+    call("pamm_dropout", pamm_dropout, keep(Y), X.data_ptr(), ldx, address(R), ldr, b, n, dt, p, seed, offset, (const int64_t*)address(counter),
+         Y.data_ptr(), ldy, at.stream());
+    return wrapped(Y);
+}
+
 // ---- the module ---------------------------------------------------------------------------------------------
 template <PyObject* (*F)(PyObject* const*), Py_ssize_t N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t count) {
@@ -414,6 +597,7 @@ PyObject* set_record(PyObject*, PyObject* list) {
 #define ENTRY(name, n) {#name, (PyCFunction)(void (*)(void))entry<name, n>, METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {
     ENTRY(norm_forward, 10), ENTRY(norm_backward, 13), ENTRY(rotary, 9), ENTRY(clip, 5),
+    ENTRY(attention_forward, 9), ENTRY(attention_backward, 14), ENTRY(dropout, 7),
     {"set_error", set_error, METH_O, nullptr}, {"set_record", set_record, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -30,6 +30,8 @@
 #include "norm.cuh"
 #include "rotary.cuh"
 #include "grad_clip.cuh"
+#include "attention.cuh"
+#include "dropout.cuh"
 
 using namespace pamm;
 
@@ -554,6 +556,7 @@ inline int norm_backward_blocks(int64_t n) { return n <= 2048 ? 4 : 3; }
 inline size_t norm_backward_ws_bytes(int64_t b, int64_t n) {
     return (size_t)round_up(std::min<int64_t>(b + 8, norm_backward_blocks(n) * sm_count()) * 2 * round_up(n, 8) * 4, 256);
 }
+inline size_t attention_backward_ws_bytes(int64_t tokens, int64_t heads) { return (size_t)round_up(tokens * heads * 4, 256); }
 inline int grad_norm_blocks() { return sm_count() * GC_BLOCKS_PER_SM; }
 inline size_t grad_norm_ws_bytes() { return (size_t)round_up((int64_t)grad_norm_blocks() * 8, 256) + 256; }      // and the factor
 
@@ -909,9 +912,162 @@ pamm_status grad_clip(const pamm_tensor* in, const pamm_tensor* out, int64_t cou
     return run_grad_clip<GC_LARGE>(in, out, count, scale, max_norm, norm, partial, st);
 }
 
+// ---- attention ------------------------------------------------------------------------------------
+struct AttentionShape { int64_t batch, seq, heads, kv_heads, d, sequences; };
+
+// A tensor of the call: its address and distances, where a distance between the only one of something and its next does not count.
+bool heads_view(const pamm_heads* t, const AttentionShape& g, int64_t heads, size_t es, bool output, HeadsView& out) {
+    if (!t || !t->data || !aligned(t->data, es)) return false;
+    out = {t->data, g.batch > 1 ? t->batch : 0, g.seq > 1 ? t->token : 0, heads > 1 ? t->head : 0};
+    return !output || ((g.batch == 1 || out.batch != 0) && (g.seq == 1 || out.token != 0) && (heads == 1 || out.head != 0));
+}
+// Whole 16-byte vectors on memory's grid in every row.
+bool heads_aligned(const HeadsView& t, size_t es) {
+    const auto on = [&](int64_t stride) { return stride * (int64_t)es % 16 == 0; };
+    return aligned(t.p, 16) && on(t.batch) && on(t.token) && on(t.head);
+}
+
+pamm_status check_attention(const AttentionShape& g, pamm_dtype dt, float scale, const void* lengths, const void* starts,
+                            pamm_position_type index_type) {
+    if (!dtype_ok(dt) || ((lengths || starts) && index_type != PAMM_POS_I32 && index_type != PAMM_POS_I64)) return PAMM_ERR_UNSUPPORTED;
+    if (g.batch < 0 || g.seq < 0 || g.heads < 0 || g.kv_heads < 0 || g.d < 1 || !(scale > 0.f) || !std::isfinite(scale)) return PAMM_ERR_INVALID_ARG;
+    if (lengths && starts) return PAMM_ERR_INVALID_ARG;
+    if (starts && (g.batch != 1 || g.sequences < 0)) return PAMM_ERR_INVALID_ARG;
+    if (g.heads > 0 && (g.kv_heads == 0 || g.heads % g.kv_heads)) return PAMM_ERR_INVALID_ARG;
+    const size_t entry = index_type == PAMM_POS_I64 ? 8 : 4;
+    if ((lengths && !aligned(lengths, entry)) || (starts && !aligned(starts, entry))) return PAMM_ERR_INVALID_ARG;
+    if (g.d > ATT_MAX_DIM || g.batch > MAX_ROWS || g.seq > MAX_ROWS || g.heads > MAX_ROWS || (starts && g.sequences > MAX_ROWS - 2))
+        return PAMM_ERR_UNSUPPORTED;
+    if (g.batch == 0 || g.seq == 0 || g.heads == 0) return PAMM_OK;
+    const int64_t most = 1ll << 40;
+    if (g.batch > most / g.seq || g.batch * g.seq > most / g.heads) return PAMM_ERR_UNSUPPORTED;
+    const int64_t tiles = starts ? g.seq / 64 + g.sequences + 2 : g.batch * ((g.seq + 63) / 64);
+    return tiles > MAX_ROWS / g.heads ? PAMM_ERR_UNSUPPORTED : PAMM_OK;
+}
+inline int tiles_of(const Sequences& s, int64_t size) {
+    return (int)(s.starts ? s.seq / size + s.count + 2 : s.batch * ((s.seq + size - 1) / size));
+}
+Sequences sequences_of(const AttentionShape& g, const void* lengths, const void* starts, pamm_position_type index_type) {
+    return {lengths, starts, g.seq, (int)g.batch, starts ? (int)g.sequences : 0, 0, index_type == PAMM_POS_I64};
+}
+
+template <typename T, int DP>
+pamm_status launch_attention_forward_generic(AttentionArgs a, cudaStream_t st) {
+    const size_t smem = ag_smem<DP>(2);
+    if (!ensure_dynamic_smem((const void*)attention_forward_generic_kernel<T, DP>, smem)) return PAMM_ERR_CUDA;
+    a.s.items = tiles_of(a.s, AG_TILE);
+    launch(attention_forward_generic_kernel<T, DP>, dim3((unsigned)a.s.items * a.heads), dim3(AG_THREADS), smem, st, true, a);
+    return launch_result("attention_forward_generic_kernel launch");
+}
+template <typename T, int DP>
+pamm_status launch_attention_backward_generic(AttentionArgs a, cudaStream_t st) {
+    const size_t smem = ag_smem<DP>(3);
+    if (!ensure_dynamic_smem((const void*)attention_backward_generic_kernel<T, DP, false>, smem) ||
+        !ensure_dynamic_smem((const void*)attention_backward_generic_kernel<T, DP, true>, smem))
+        return PAMM_ERR_CUDA;
+    a.s.items = tiles_of(a.s, AG_TILE);
+    launch(attention_backward_generic_kernel<T, DP, false>, dim3((unsigned)a.s.items * a.heads), dim3(AG_THREADS), smem, st, true, a);
+    launch(attention_backward_generic_kernel<T, DP, true>, dim3((unsigned)a.s.items * (a.heads / a.group)), dim3(AG_THREADS), smem, st, true, a);
+    return launch_result("attention_backward_generic_kernel launch");
+}
+template <typename T>
+pamm_status run_attention_generic(const AttentionArgs& a, bool back, cudaStream_t st) {
+    if (a.d <= 64) return back ? launch_attention_backward_generic<T, 64>(a, st) : launch_attention_forward_generic<T, 64>(a, st);
+    if (a.d <= 128) return back ? launch_attention_backward_generic<T, 128>(a, st) : launch_attention_forward_generic<T, 128>(a, st);
+    return back ? launch_attention_backward_generic<T, 256>(a, st) : launch_attention_forward_generic<T, 256>(a, st);
+}
+pamm_status run_attention(const AttentionArgs& a, pamm_dtype dt, bool back, cudaStream_t st) {
+    return dt == PAMM_F32 ? run_attention_generic<float>(a, back, st) : run_attention_generic<__nv_bfloat16>(a, back, st);
+}
+
+template <typename T>
+pamm_status run_dropout(DropoutArgs a, cudaStream_t st) {
+    constexpr int V = 16 / (int)sizeof(T);
+    const auto grid = [](const void* p, int64_t ld, int64_t rows) { return !p || (aligned(p, 16) && (rows == 1 || ld % V == 0)); };
+    const bool whole = (a.rows == 1 || a.n % V == 0) && grid(a.x, a.ldx, a.rows) && grid(a.r, a.ldr, a.rows) && grid(a.y, a.ldy, a.rows);
+    const int64_t per = 256 * (whole ? V : 4);
+    const dim3 blocks((unsigned)((a.total + per - 1) / per));
+    if (whole) {
+        if (a.r) launch(dropout_kernel<T, V, true>, blocks, dim3(256), 0, st, true, a);
+        else launch(dropout_kernel<T, V, false>, blocks, dim3(256), 0, st, true, a);
+    } else {
+        if (a.r) launch(dropout_kernel<T, 1, true>, blocks, dim3(256), 0, st, true, a);
+        else launch(dropout_kernel<T, 1, false>, blocks, dim3(256), 0, st, true, a);
+    }
+    return launch_result("dropout_kernel launch");
+}
+
 }  // namespace
 
 extern "C" {
+
+pamm_status pamm_attention_forward(const pamm_heads* Q, const pamm_heads* K, const pamm_heads* V, const pamm_heads* O, float* lse,
+                                   int64_t batch, int64_t seq, int64_t heads, int64_t kv_heads, int64_t head_dim, pamm_dtype dt,
+                                   float scale, int causal, const void* lengths, const void* starts, int64_t sequences,
+                                   pamm_position_type index_type, void* stream) {
+    const AttentionShape g = {batch, seq, heads, kv_heads, head_dim, sequences};
+    const pamm_status s = check_attention(g, dt, scale, lengths, starts, index_type);
+    if (s != PAMM_OK || batch == 0 || seq == 0 || heads == 0) return s;
+    const size_t es = esize(dt);
+    AttentionArgs a = {};
+    if (!heads_view(Q, g, heads, es, false, a.q) || !heads_view(K, g, kv_heads, es, false, a.k) || !heads_view(V, g, kv_heads, es, false, a.v) ||
+        !heads_view(O, g, heads, es, true, a.o) || !aligned(lse, 4))
+        return PAMM_ERR_INVALID_ARG;
+    a.lse = lse;
+    a.s = sequences_of(g, lengths, starts, index_type);
+    a.heads = (int)heads; a.group = (int)(heads / kv_heads); a.d = (int)head_dim;
+    a.scale = scale; a.causal = causal != 0;
+    a.vectors = head_dim * (int64_t)es % 16 == 0 && heads_aligned(a.q, es) && heads_aligned(a.k, es) && heads_aligned(a.v, es) && heads_aligned(a.o, es);
+    return run_attention(a, dt, false, (cudaStream_t)stream);
+}
+
+pamm_status pamm_attention_backward(const pamm_heads* dO, const pamm_heads* Q, const pamm_heads* K, const pamm_heads* V,
+                                    const pamm_heads* O, const float* lse, const pamm_heads* dQ, const pamm_heads* dK,
+                                    const pamm_heads* dV, int64_t batch, int64_t seq, int64_t heads, int64_t kv_heads,
+                                    int64_t head_dim, pamm_dtype dt, float scale, int causal, const void* lengths, const void* starts,
+                                    int64_t sequences, pamm_position_type index_type, void* workspace, size_t ws_bytes, void* stream) {
+    const AttentionShape g = {batch, seq, heads, kv_heads, head_dim, sequences};
+    const pamm_status s = check_attention(g, dt, scale, lengths, starts, index_type);
+    if (s != PAMM_OK || batch == 0 || seq == 0 || heads == 0) return s;
+    const size_t es = esize(dt);
+    AttentionArgs a = {};
+    if (!heads_view(dO, g, heads, es, false, a.d_o) || !heads_view(Q, g, heads, es, false, a.q) || !heads_view(K, g, kv_heads, es, false, a.k) ||
+        !heads_view(V, g, kv_heads, es, false, a.v) || !heads_view(O, g, heads, es, false, a.o) || !heads_view(dQ, g, heads, es, true, a.dq) ||
+        !heads_view(dK, g, kv_heads, es, true, a.dk) || !heads_view(dV, g, kv_heads, es, true, a.dv) || !lse || !aligned(lse, 4))
+        return PAMM_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 16) || ws_bytes < attention_backward_ws_bytes(batch * seq, heads)) return PAMM_ERR_WORKSPACE;
+    a.lse_in = lse;
+    a.delta = static_cast<float*>(workspace);
+    a.s = sequences_of(g, lengths, starts, index_type);
+    a.heads = (int)heads; a.group = (int)(heads / kv_heads); a.d = (int)head_dim;
+    a.scale = scale; a.causal = causal != 0;
+    a.vectors = head_dim * (int64_t)es % 16 == 0;
+    for (const HeadsView* t : {&a.q, &a.k, &a.v, &a.o, &a.d_o, &a.dq, &a.dk, &a.dv}) a.vectors = a.vectors && heads_aligned(*t, es);
+    return run_attention(a, dt, true, (cudaStream_t)stream);
+}
+
+pamm_status pamm_dropout(const void* X, int64_t ldx, const void* R, int64_t ldr, int64_t b, int64_t n, pamm_dtype dt, double p,
+                         uint64_t seed, uint64_t offset, const int64_t* counter, void* Y, int64_t ldy, void* stream) {
+    if (!dtype_ok(dt)) return PAMM_ERR_UNSUPPORTED;
+    if (b < 0 || n < 0 || !(p >= 0.0 && p <= 1.0) || !aligned(counter, 8)) return PAMM_ERR_INVALID_ARG;
+    if (b > (1ll << 40) || n > (1ll << 40) || (n > 0 && b > (1ll << 38) / n)) return PAMM_ERR_UNSUPPORTED;
+    if (b == 0 || n == 0) return PAMM_OK;
+    const size_t es = esize(dt);
+    if (b == 1) ldx = ldr = ldy = n;
+    if (!matrix_ok(X, ldx, n, es) || !matrix_ok(Y, ldy, n, es) || (R && !matrix_ok(R, ldr, n, es))) return PAMM_ERR_INVALID_ARG;
+    if ((Y == X && ldy != ldx) || (Y == R && ldy != ldr)) return PAMM_ERR_INVALID_ARG;
+    if (ldx == n && ldy == n && (!R || ldr == n)) {       // without gaps the rows are one
+        n *= b;
+        ldx = ldr = ldy = n;
+        b = 1;
+    }
+    DropoutArgs a = {};
+    a.x = X; a.r = R; a.y = Y; a.rows = b; a.n = n; a.ldx = ldx; a.ldr = ldr; a.ldy = ldy; a.total = b * n;
+    a.counter = counter; a.seed = seed; a.offset = offset;
+    a.threshold = (uint64_t)(p * 4294967296.0);
+    a.factor = p < 1.0 ? (float)(1.0 / (1.0 - p)) : 0.f;
+    return dt == PAMM_F32 ? run_dropout<float>(a, (cudaStream_t)stream) : run_dropout<__nv_bfloat16>(a, (cudaStream_t)stream);
+}
 
 pamm_status pamm_norm_forward(pamm_norm_kind kind, const void* X, int64_t ldx, const void* R, int64_t ldr, int64_t b, int64_t n,
                               pamm_dtype dt, const void* w, const void* c, pamm_dtype w_dt, float eps, void* Y, int64_t ldy,
@@ -1122,6 +1278,10 @@ size_t pamm_workspace_bytes(pamm_ws_kind kind, int64_t b, int64_t n, int64_t m, 
         return norm_backward_ws_bytes(b, n);
     }
     if (kind == PAMM_WS_GRAD_NORM) return grad_norm_ws_bytes();
+    if (kind == PAMM_WS_ATTENTION_BACKWARD) {
+        if (b < 0 || n < 0 || (n > 0 && b > (1ll << 40) / n)) return (size_t)-1;
+        return std::max<size_t>(256, attention_backward_ws_bytes(b, n));
+    }
     if (!dtype_ok(dt) || b < 1 || k < 1 || k > b || b > MAX_ROWS) return (size_t)-1;
     switch (kind) {
         case PAMM_WS_COMPRESS:

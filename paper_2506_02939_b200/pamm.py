@@ -61,7 +61,7 @@ OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT, ERR_
 F32, BF16 = 0, 1
 DW_NM, DW_MN = 0, 1                      # layout of the weight gradient: n x m (the paper's), or m x n (out x in)
 IDX_I32, IDX_U16, IDX_U8 = 0, 1, 2       # storage type of the assignment f
-WS_COMPRESS, WS_CONTRACT, WS_STEP_HOST, WS_NORM_BACKWARD, WS_GRAD_NORM = 0, 1, 2, 3, 4
+WS_COMPRESS, WS_CONTRACT, WS_STEP_HOST, WS_NORM_BACKWARD, WS_GRAD_NORM, WS_ATTENTION_BACKWARD = 0, 1, 2, 3, 4, 5
 NORM_LAYER, NORM_RMS = 0, 1
 PAIRS_HALF, PAIRS_ADJACENT = 0, 1        # rotary pairs (i, i + rot/2), or (2i, 2i + 1)
 ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_PARTS = 0, 1, 2, 3     # scalings for long contexts
@@ -102,6 +102,9 @@ _SIGNATURES = {
                      _vp, _ci, _i64, _i64, _i64, _vp], _ci),
     "pamm_grad_norm": ([_vp, _i64, _vp, _vp, _sz, _vp], _ci),
     "pamm_clip_grad_norm": ([_vp, _vp, _i64, _f64, _vp, _vp, _sz, _vp], _ci),
+    "pamm_attention_forward": ([_vp] * 5 + [_i64] * 5 + [_ci, _f32, _ci, _vp, _vp, _i64, _ci, _vp], _ci),
+    "pamm_attention_backward": ([_vp] * 9 + [_i64] * 5 + [_ci, _f32, _ci, _vp, _vp, _i64, _ci, _vp, _sz, _vp], _ci),
+    "pamm_dropout": ([_vp, _i64, _vp, _i64, _i64, _i64, _ci, _f64, _u64, _u64, _vp, _vp, _i64, _vp], _ci),
     "pamm_last_device_status": ([_vp], _ci),
     "pamm_selftest_bounded_wait": ([_vp], _ci),
     "pamm_probe_read": ([_ci, _vp, _i64, _i64, _i64, _vp, _vp, _vp], _ci),
@@ -454,7 +457,7 @@ def prepared(call, *args, **kwargs):
     return run
 
 
-# ---- the operators around the projection: norm, rotary positions, gradient clipping ----------------
+# ---- the operators around the projection: norm, rotary positions, attention, dropout, gradient clipping ----
 # Checks, allocation and the C call are in the compiled binding (csrc/binding.cpp).  A call runs on the current
 # stream of its tensors' device, or on `stream`; what it allocates belongs to that stream.
 
@@ -514,6 +517,30 @@ def rotary(X, table, positions=None, rotated: int | None = None, rot_dim: int | 
     ``rot_dim`` has to be where it is given.  ``positions``: int32 or int64 of shape (tokens,) or (batch, tokens); None: ``first`` +
     the token's index.  ``transposed`` gives the gradient's turn.  ``out=X`` turns in place."""
     return _binding_on(stream, _binding.rotary, X, table, positions, rotated, rot_dim, interleaved, transposed, first, out)
+
+
+def attention_forward(Q, K, V, causal: bool = False, lengths=None, starts=None, scale: float | None = None, O=None, lse=None, stream=None):
+    """Softmax attention; see pamm_attention_forward.  ``Q`` is (batch, tokens, heads, head_dim) or (tokens, heads, head_dim), ``K`` and
+    ``V`` the same with as many heads or a divisor, all of any strides with contiguous heads -- for instance
+    ``Z.split((heads, kv_heads, kv_heads), -2)`` of the fused row.  ``lengths`` (batch,): the valid tokens of each padded sequence;
+    ``starts`` (sequences + 1,): where sequences packed along the one token axis begin, and the last one's end; both on the
+    device, int32 or int64.  ``scale`` is 1 / sqrt(head_dim) by default.  Returns O, contiguous by token unless given, and the rows' log-sums
+    (batch, heads, tokens) or (heads, tokens), fp32; rows of tokens that are not valid are 0 and -infinity."""
+    return _binding_on(stream, _binding.attention_forward, Q, K, V, causal, lengths, starts, scale, O, lse)
+
+
+def attention_backward(dO, Q, K, V, O, lse, causal: bool = False, lengths=None, starts=None, scale: float | None = None, dQ=None, dK=None,
+                       dV=None, workspace=None, stream=None):
+    """Gradients of ``attention_forward`` from its inputs, its outputs and the gradient of O; see pamm_attention_backward.  Where none of
+    the outputs is given, dQ, dK and dV are the parts of one new row [dQ|dK|dV], which the projection's backward pass takes as it is."""
+    return _binding_on(stream, _binding.attention_backward, dO, Q, K, V, O, lse, causal, lengths, starts, scale, dQ, dK, dV, workspace)
+
+
+def dropout(X, p: float, seed: int, offset: int = 0, counter=None, residual=None, Y=None, stream=None):
+    """``residual`` + X / (1 - p) where the generator keeps it; see pamm_dropout.  ``X`` is contiguous, or a matrix with contiguous rows;
+    ``seed`` and ``offset`` are 64 bits each and, with X's shape, determine the mask; ``counter``: one int64 on the device that is
+    added to ``offset``.  The gradient of X is this call on the gradient of Y, without the residual.  ``Y`` may be ``X`` or ``residual``."""
+    return _binding_on(stream, _binding.dropout, X, p, seed, offset, counter, residual, Y)
 
 
 def grad_norm(grads, norm=None, workspace=None, stream=None):
