@@ -31,6 +31,7 @@
 #include "rotary.cuh"
 #include "grad_clip.cuh"
 #include "attention.cuh"
+#include "attention_umma.cuh"
 #include "dropout.cuh"
 
 using namespace pamm;
@@ -976,7 +977,37 @@ pamm_status run_attention_generic(const AttentionArgs& a, bool back, cudaStream_
     if (a.d <= 128) return back ? launch_attention_backward_generic<T, 128>(a, st) : launch_attention_forward_generic<T, 128>(a, st);
     return back ? launch_attention_backward_generic<T, 256>(a, st) : launch_attention_forward_generic<T, 256>(a, st);
 }
+
+template <int DP>
+pamm_status launch_attention_forward(AttentionArgs a, const AttentionMaps& m, cudaStream_t st) {
+    using Plan = ForwardPlan<DP>;
+    if (!ensure_dynamic_smem((const void*)attention_forward_kernel<DP>, Plan::SMEM)) return PAMM_ERR_CUDA;
+    a.s.items = tiles_of(a.s, AF_QUERIES);
+    const int works = a.s.items * a.heads, blocks = std::min(works, sm_count());
+    launch(attention_forward_kernel<DP>, dim3((unsigned)blocks), dim3(AF_THREADS), Plan::SMEM, st, true, a, m,
+           attention_order(a.s, a.heads, AF_QUERIES, blocks, a.causal), works);
+    return launch_result("attention_forward_kernel launch");
+}
+
+// Tensor maps need distances that go up, of whole 16-byte vectors (checked: a.vectors).
+bool attention_on_tensor_cores(const AttentionArgs& a, pamm_dtype dt, bool back) {
+    if (dt != PAMM_BF16 || a.d > 128 || !a.vectors) return false;
+    const auto fits = [&](const HeadsView& t, int heads) {
+        const auto up = [](int64_t n, int64_t ld) { return n == 1 || (ld > 0 && ld < (1ll << 38)); };
+        return up(a.s.batch, t.batch) && up(a.s.seq, t.token) && up(heads, t.head);
+    };
+    const int kv = a.heads / a.group;
+    return fits(a.q, a.heads) && fits(a.k, kv) && fits(a.v, kv) && (!back || fits(a.d_o, a.heads));
+}
 pamm_status run_attention(const AttentionArgs& a, pamm_dtype dt, bool back, cudaStream_t st) {
+    if (!back && attention_on_tensor_cores(a, dt, back)) {
+        AttentionMaps m;
+        const int kv = a.heads / a.group;
+        if (!attention_map(&m.q, a.q, a.s, a.heads, a.d) || !attention_map(&m.k, a.k, a.s, kv, a.d) || !attention_map(&m.v, a.v, a.s, kv, a.d))
+            return tensor_map_failed();
+        m.d_o = m.q;
+        return a.d <= 64 ? launch_attention_forward<64>(a, m, st) : launch_attention_forward<128>(a, m, st);
+    }
     return dt == PAMM_F32 ? run_attention_generic<float>(a, back, st) : run_attention_generic<__nv_bfloat16>(a, back, st);
 }
 
