@@ -32,6 +32,7 @@
 #include "grad_clip.cuh"
 #include "attention.cuh"
 #include "attention_umma.cuh"
+#include "attention_umma_backward.cuh"
 #include "dropout.cuh"
 
 using namespace pamm;
@@ -989,6 +990,22 @@ pamm_status launch_attention_forward(AttentionArgs a, const AttentionMaps& m, cu
     return launch_result("attention_forward_kernel launch");
 }
 
+template <int DP>
+pamm_status launch_attention_backward(AttentionArgs a, const AttentionMaps& m, cudaStream_t st) {
+    using Plan = BackwardPlan<DP>;
+    if (!ensure_dynamic_smem((const void*)attention_queries_backward_kernel<DP>, Plan::SMEM) ||
+        !ensure_dynamic_smem((const void*)attention_keys_backward_kernel<DP>, Plan::SMEM))
+        return PAMM_ERR_CUDA;
+    a.s.items = tiles_of(a.s, AU_ROWS);
+    const int kv = a.heads / a.group, rows = a.s.items * a.heads, keys = a.s.items * kv, sms = sm_count();
+    const int row_blocks = std::min(rows, sms), key_blocks = std::min(keys, sms);
+    launch(attention_queries_backward_kernel<DP>, dim3((unsigned)row_blocks), dim3(AB_THREADS), Plan::SMEM, st, true, a, m,
+           attention_order(a.s, a.heads, AU_ROWS, row_blocks, a.causal), rows);
+    launch(attention_keys_backward_kernel<DP>, dim3((unsigned)key_blocks), dim3(AB_THREADS), Plan::SMEM, st, true, a, m,
+           attention_order(a.s, kv, AU_ROWS, key_blocks, false), keys);
+    return launch_result("attention_keys_backward_kernel launch");
+}
+
 // Tensor maps need distances that go up, of whole 16-byte vectors (checked: a.vectors).
 bool attention_on_tensor_cores(const AttentionArgs& a, pamm_dtype dt, bool back) {
     if (dt != PAMM_BF16 || a.d > 128 || !a.vectors) return false;
@@ -1000,12 +1017,16 @@ bool attention_on_tensor_cores(const AttentionArgs& a, pamm_dtype dt, bool back)
     return fits(a.q, a.heads) && fits(a.k, kv) && fits(a.v, kv) && (!back || fits(a.d_o, a.heads));
 }
 pamm_status run_attention(const AttentionArgs& a, pamm_dtype dt, bool back, cudaStream_t st) {
-    if (!back && attention_on_tensor_cores(a, dt, back)) {
+    if (attention_on_tensor_cores(a, dt, back)) {
         AttentionMaps m;
         const int kv = a.heads / a.group;
         if (!attention_map(&m.q, a.q, a.s, a.heads, a.d) || !attention_map(&m.k, a.k, a.s, kv, a.d) || !attention_map(&m.v, a.v, a.s, kv, a.d))
             return tensor_map_failed();
-        m.d_o = m.q;
+        m.d_o = m.q;       // not looked at in the forward pass
+        if (back) {
+            if (!attention_map(&m.d_o, a.d_o, a.s, a.heads, a.d)) return tensor_map_failed();
+            return a.d <= 64 ? launch_attention_backward<64>(a, m, st) : launch_attention_backward<128>(a, m, st);
+        }
         return a.d <= 64 ? launch_attention_forward<64>(a, m, st) : launch_attention_forward<128>(a, m, st);
     }
     return dt == PAMM_F32 ? run_attention_generic<float>(a, back, st) : run_attention_generic<__nv_bfloat16>(a, back, st);
