@@ -86,14 +86,13 @@ __device__ __forceinline__ bool au_produce(TileRing& r, const CUtensorMap* tm, c
     if (!warp_wait(&r.empty[r.slot], r.phase ^ 1u, r.abort_flag)) return false;
     uint8_t* dst = r.tiles + (size_t)r.slot * (DP / 64) * AU_BLOCK_BYTES;
     const int valid = t.len - at;
-    const bool lane0 = (threadIdx.x & 31) == 0;
     if (!clear || valid >= AU_ROWS) {
-        if (lane0) {
+        if (ptx::elect_one()) {
             ptx::mbar_arrive_expect_tx(&r.full[r.slot], DP / 64 * AU_BLOCK_BYTES);
             au_load<DP>(dst, tm, t, head, at, &r.full[r.slot]);
         }
     } else {
-        if (lane0) {
+        if (ptx::elect_one()) {
             ptx::mbar_arrive_expect_tx(r.tail, DP / 64 * AU_BLOCK_BYTES);
             au_load<DP>(dst, tm, t, head, at, r.tail);
         }
@@ -106,7 +105,7 @@ __device__ __forceinline__ bool au_produce(TileRing& r, const CUtensorMap* tm, c
                 *reinterpret_cast<uint4*>(dst + c * AU_BLOCK_BYTES + i * 16) = make_uint4(0, 0, 0, 0);
         ptx::fence_proxy_async();
         __syncwarp();
-        if (lane0) ptx::mbar_arrive(&r.full[r.slot]);
+        if (ptx::elect_one()) ptx::mbar_arrive(&r.full[r.slot]);
     }
     __syncwarp();
     r.next();
@@ -229,7 +228,7 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
                 ok = warp_wait(&s_qempty[x], q_phase[x] ^ 1u, abort_flag);
                 if (!ok) break;
                 q_phase[x] ^= 1u;
-                if (lane == 0) {
+                if (ptx::elect_one()) {
                     ptx::mbar_arrive_expect_tx(&s_qfull[x], Plan::TILE_BYTES);
                     au_load<DP>(queries + x * Plan::TILE_BYTES, &m.q, t, h, t.at + x * AU_ROWS, &s_qfull[x]);
                 }
@@ -250,7 +249,6 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
         const uint32_t q_addr = ptx::smem_u32(queries), ring_addr = ptx::smem_u32(ring_tiles);
         uint32_t q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
         uint32_t count = 0;                     // ring tiles of earlier items
-        const bool leader = lane == 0;
         const auto slot_of = [&](uint32_t i) { return i % Plan::SLOTS; };
         const auto tile_ready = [&](uint32_t i) { return warp_wait(&s_full[slot_of(i)], (i / Plan::SLOTS) & 1u, abort_flag); };
         for (int w = blockIdx.x; w < works && ok; w += gridDim.x) {
@@ -261,7 +259,7 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
             const int n0 = af_key_tiles(t, a.causal, 0), n1 = af_key_tiles(t, a.causal, 1), n = max(n0, n1);
             // S of tile x and key tile j; the last use of key tile j frees its slot
             const auto scores = [&](int x, int j) {
-                if (leader) {
+                if (ptx::elect_one()) {
                     au_scores(tmem + x * 128, q_addr + x * Plan::TILE_BYTES, ring_addr + slot_of(count + 2 * j) * Plan::TILE_BYTES, steps, idesc_s);
                     ptx::umma_commit(&s_scores[x]);
                     if (j == (x ? n1 : n0) - 1) ptx::umma_commit(&s_qempty[x]);
@@ -284,7 +282,7 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
                     p_phase[x] ^= 1u;
                     if (!ok) break;
                     ptx::tc_fence_after_sync();
-                    if (leader) {
+                    if (ptx::elect_one()) {
                         au_weighted(tmem + 256 + x * 128, tmem + x * 128, ring_addr + slot_of(count + 2 * j + 1) * Plan::TILE_BYTES, idesc_o, j > 0);
                         if (j == mine - 1) ptx::umma_commit(&s_done[x]);
                         if (x == 1 || j >= n1) ptx::umma_commit(&s_empty[slot_of(count + 2 * j + 1)]);

@@ -52,7 +52,7 @@ __device__ __forceinline__ bool ab_load_fixed(uint8_t* tiles, const CUtensorMap*
     constexpr int BYTES = DP / 64 * AU_BLOCK_BYTES;
     for (int x = 0; x < 2; ++x) {
         if (!warp_wait(&empty[x], phase ^ 1u, abort_flag)) return false;
-        if ((threadIdx.x & 31) == 0) {
+        if (ptx::elect_one()) {
             ptx::mbar_arrive_expect_tx(&full[x], BYTES);
             au_load<DP>(tiles + x * BYTES, x ? m1 : m0, t, head, t.at, &full[x]);
         }
@@ -132,7 +132,6 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
         const uint32_t f_addr = ptx::smem_u32(fixed), ring_addr = ptx::smem_u32(ring_tiles);
         uint32_t f_phase = 0, r_phase = 0, d_phase[2] = {0, 0};
         uint32_t count = 0;
-        const bool leader = lane == 0;
         const auto slot_of = [&](uint32_t i) { return i % Plan::SLOTS; };
         const auto address = [&](uint32_t i) { return ring_addr + slot_of(i) * Plan::TILE_BYTES; };
         const auto tile_ready = [&](uint32_t i) { return warp_wait(&s_full[slot_of(i)], (i / Plan::SLOTS) & 1u, abort_flag); };
@@ -145,7 +144,7 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
             const auto scores = [&](int j) {
                 if (!tile_ready(count + 2 * j)) return false;
                 ptx::tc_fence_after_sync();
-                if (leader) {
+                if (ptx::elect_one()) {
                     au_scores(tmem + (j & 1) * 128, f_addr, address(count + 2 * j), steps, idesc_s);
                     ptx::umma_commit(&s_scores[j & 1]);
                     if (j == n - 1) ptx::umma_commit(&s_fempty[0]);
@@ -156,7 +155,7 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
             const auto grads = [&](int j) {
                 if (!tile_ready(count + 2 * j + 1)) return false;
                 ptx::tc_fence_after_sync();
-                if (leader) {
+                if (ptx::elect_one()) {
                     au_scores(tmem + 256, f_addr + Plan::TILE_BYTES, address(count + 2 * j + 1), steps, idesc_s);
                     ptx::umma_commit(&s_grads);
                     ptx::umma_commit(&s_empty[slot_of(count + 2 * j + 1)]);
@@ -176,7 +175,7 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
                 d_phase[j & 1] ^= 1u;
                 if (!ok) break;
                 ptx::tc_fence_after_sync();
-                if (leader) {
+                if (ptx::elect_one()) {
                     ab_weighted(tmem + 384, tmem + (j & 1) * 128, address(count + 2 * j), idesc_g, j > 0);
                     ptx::umma_commit(&s_empty[slot_of(count + 2 * j)]);
                     if (j == n - 1) ptx::umma_commit(&s_done);
@@ -380,7 +379,6 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
         const uint32_t f_addr = ptx::smem_u32(fixed), ring_addr = ptx::smem_u32(ring_tiles);
         uint32_t f_phase = 0, p_phase = 0, d_phase = 0;
         uint32_t count = 0;
-        const bool leader = lane == 0;
         const auto slot_of = [&](uint32_t i) { return i % Plan::SLOTS; };
         const auto address = [&](uint32_t i) { return ring_addr + slot_of(i) * Plan::TILE_BYTES; };
         const auto tile_ready = [&](uint32_t i) { return warp_wait(&s_full[slot_of(i)], (i / Plan::SLOTS) & 1u, abort_flag); };
@@ -394,7 +392,7 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
             const auto scores = [&](int what, int i) {
                 if (!tile_ready(count + 2 * i + what)) return false;
                 ptx::tc_fence_after_sync();
-                if (leader) {
+                if (ptx::elect_one()) {
                     au_scores(tmem + what * 128, f_addr + what * Plan::TILE_BYTES, address(count + 2 * i + what), steps, idesc_s);
                     ptx::umma_commit(what ? &s_grads : &s_scores);
                     if (i == n - 1) ptx::umma_commit(&s_fempty[what]);
@@ -409,7 +407,7 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
                 p_phase ^= 1u;
                 if (!ok) break;
                 ptx::tc_fence_after_sync();
-                if (leader) {
+                if (ptx::elect_one()) {
                     ab_weighted(tmem + 256, tmem, address(count + 2 * i + 1), idesc_g, i > 0);
                     ptx::umma_commit(&s_empty[slot_of(count + 2 * i + 1)]);
                 }
@@ -419,7 +417,7 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
                 d_phase ^= 1u;
                 if (!ok) break;
                 ptx::tc_fence_after_sync();
-                if (leader) {
+                if (ptx::elect_one()) {
                     ab_weighted(tmem + 384, tmem + 128, address(count + 2 * i), idesc_g, i > 0);
                     ptx::umma_commit(&s_empty[slot_of(count + 2 * i)]);
                     if (i == n - 1) ptx::umma_commit(&s_done);
