@@ -98,7 +98,7 @@ struct AttentionArgs {
     Sequences s;
     int heads, group, d;            // query heads; how many of them share a key head
     float scale;
-    bool causal, vectors;           // vectors: every row is on the 16-byte grid with whole vectors
+    bool causal, vectors, wide;     // vectors: every row is on the 16-byte grid with whole vectors; wide: outputs on the 32-byte grid
     __device__ __forceinline__ int64_t row_number(const Tile& t, int h) const { return (t.b * heads + h) * s.seq + t.first; }
 };
 

@@ -7,13 +7,17 @@
 #pragma once
 #include "attention.cuh"
 #include "sm100_ptx.cuh"
-#include "weight_grad_common.cuh"      // umma_desc_mn_sw128
 
 namespace pamm {
 
 constexpr int AU_ROWS = 128, AU_BLOCK_BYTES = AU_ROWS * 128;       // of a tile, and of 64 of its columns
-constexpr int AU_TMA_WARP = 8, AU_MMA_WARP = 9;                    // behind eight warps that own rows
-constexpr size_t AU_SMEM_LIMIT = 232448;
+
+// The 16 warps of a block: eight own rows of scores, four take accumulators out of tensor memory (a warp reaches the 32
+// lanes of its number modulo 4 only), and one each copies tiles in, issues the products, fetches numbers of rows and finds the
+// next items.  Registers: 128 a thread at the launch; the rows' warps take what the others give back.
+constexpr int AU_THREADS = 512, AU_FINISH_WARP = 8, AU_TMA_WARP = 12, AU_MMA_WARP = 13, AU_STATS_WARP = 14, AU_ITEMS_WARP = 15;
+constexpr int AU_ROW_REGS = 168, AU_OTHER_REGS = 88;
+static_assert(256 * AU_ROW_REGS + 256 * AU_OTHER_REGS <= 65536, "what is taken has to have been given back");
 
 // The order of work.  Whole and padded batches: (batch, head) pairs in groups of about one per block, in a group the tiles of every pair
 // from the last to the first -- the long ones first where causal -- so that a pair's keys are read again while they
@@ -65,6 +69,81 @@ __device__ __forceinline__ void au_load(uint8_t* dst, const CUtensorMap* tm, con
 // A wait of a whole warp: the same answer in every lane.
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
     return __all_sync(0xffffffffu, ptx::mbar_wait(bar, parity, abort_flag));
+}
+// The block's items, found ahead by one warp and read by all others (`readers` warps: each gives an entry back as soon as it has it in
+// registers).  An entry with rows < 0 is the end.
+constexpr int AU_ITEMS = 4;
+struct Item { Tile t; int head; };
+struct ItemQueue {
+    Item items[AU_ITEMS];
+    uint64_t full[AU_ITEMS], empty[AU_ITEMS];
+    __device__ __forceinline__ void init(int readers) {
+        for (int i = 0; i < AU_ITEMS; ++i) { ptx::mbar_init(&full[i], 1); ptx::mbar_init(&empty[i], readers); }
+    }
+};
+struct ItemReader {
+    ItemQueue* q;
+    volatile int* abort_flag;
+    uint32_t count = 0;
+    // False at the end and where a wait ran out (`ok`).
+    __device__ __forceinline__ bool next(Item& item, bool& ok) {
+        const uint32_t slot = count % AU_ITEMS;
+        if (!warp_wait(&q->full[slot], (count / AU_ITEMS) & 1u, abort_flag)) { ok = false; return false; }
+        item = q->items[slot];
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(&q->empty[slot]);
+        ++count;
+        return item.t.rows >= 0;
+    }
+    // The same for a thread that reads for its warp.
+    __device__ __forceinline__ bool next_alone(Item& item, bool& ok) {
+        const uint32_t slot = count % AU_ITEMS;
+        if (!ptx::mbar_wait(&q->full[slot], (count / AU_ITEMS) & 1u, abort_flag)) { ok = false; return false; }
+        item = q->items[slot];
+        ptx::mbar_arrive(&q->empty[slot]);
+        ++count;
+        return item.t.rows >= 0;
+    }
+};
+// A place in the ring of a thread that goes through it.
+template <int SLOTS>
+struct RingPlace {
+    uint32_t slot = 0, phase = 0;
+    __device__ __forceinline__ void move(uint32_t by) {      // by at most SLOTS
+        slot += by;
+        if (slot >= SLOTS) {
+            slot -= SLOTS;
+            phase ^= 1u;
+        }
+    }
+    __device__ __forceinline__ void to(uint32_t tile) {
+        slot = tile % SLOTS;
+        phase = (tile / SLOTS) & 1u;
+    }
+};
+// The warp that finds them.
+template <int SIZE>
+__device__ __forceinline__ bool au_find_items(ItemQueue& q, const Sequences& s, const AttentionOrder& order, int works, volatile int* abort_flag) {
+    uint32_t count = 0;
+    for (int w = blockIdx.x;; w += gridDim.x) {
+        Item item;
+        item.t.rows = -1;
+        if (w < works) {
+            int number;
+            order.at(w, number, item.head);
+            item.t = find_tile<SIZE>(s, number);
+            if (!item.t.any) continue;
+        }
+        const uint32_t slot = count % AU_ITEMS;
+        if (!warp_wait(&q.empty[slot], ((count / AU_ITEMS) & 1u) ^ 1u, abort_flag)) return false;
+        if ((threadIdx.x & 31) == 0) {
+            q.items[slot] = item;
+            ptx::mbar_arrive(&q.full[slot]);
+        }
+        __syncwarp();
+        ++count;
+        if (w >= works) return true;
+    }
 }
 // The producer's ring of tiles.  Called by the whole warp.
 struct TileRing {
@@ -122,19 +201,64 @@ __device__ __forceinline__ void au_drain(const TileRing& r) {
     }
 }
 
-// D (+)= A B^T over the heads' d columns, both tiles K-major: d = 16 steps.  One thread.
+// The products.  One thread.  A product is issued only shortly before it runs, so what this thread computes between two of them counts.
+// D = A B^T over the heads' columns, both tiles K-major: steps of 16 columns.
+template <int DP>
 __device__ __forceinline__ void au_scores(uint32_t d_tmem, uint32_t a, uint32_t b, int steps, uint32_t idesc) {
-    const uint64_t da = ptx::umma_desc_k_sw128(a), db = ptx::umma_desc_k_sw128(b);
-    for (int k = 0; k < steps; ++k) {
-        const uint64_t off = (uint64_t)((k >> 2) * (AU_BLOCK_BYTES >> 4) + (k & 3) * 2);
-        ptx::umma_bf16(d_tmem, da + off, db + off, idesc, k > 0);
+    const uint32_t la = ptx::umma_desc_lower_k(a), lb = ptx::umma_desc_lower_k(b);
+#pragma unroll
+    for (int k = 0; k < DP / 16; ++k) {
+        const uint32_t off = (uint32_t)((k >> 2) * (AU_BLOCK_BYTES >> 4) + (k & 3) * 2);
+        if (k < steps) ptx::umma_bf16_lower(d_tmem, la + off, lb + off, idesc, k > 0);
     }
 }
-// D (+)= W B over 128 rows of B: W bf16 in tensor memory, B MN-major.  One thread.
-__device__ __forceinline__ void au_weighted(uint32_t d_tmem, uint32_t w_tmem, uint32_t b, uint32_t idesc, bool accumulate) {
+// D (+)= W B over half of B's 128 rows: W bf16 in tensor memory, its two halves 64 columns apart (each over the scores it came
+// from), B MN-major.
+__device__ __forceinline__ void au_weighted_half(uint32_t d_tmem, uint32_t w_tmem, uint32_t b, int half, uint32_t idesc, bool accumulate) {
+    const uint32_t lb = ptx::umma_desc_lower_mn(b, AU_BLOCK_BYTES) + half * (4 * 2048 >> 4);
 #pragma unroll
-    for (int k = 0; k < AU_ROWS / 16; ++k)
-        ptx::umma_bf16_ts(d_tmem, w_tmem + 8 * k, umma_desc_mn_sw128(b + k * 2048, AU_BLOCK_BYTES, 1024), idesc, accumulate || k > 0);
+    for (int k = 0; k < 4; ++k) ptx::umma_bf16_ts(d_tmem, w_tmem + half * 64 + k * 8, lb + k * (2048 >> 4), idesc, accumulate || k > 0);
+}
+__device__ __forceinline__ void au_weighted(uint32_t d_tmem, uint32_t w_tmem, uint32_t b, uint32_t idesc, bool accumulate) {
+    au_weighted_half(d_tmem, w_tmem, b, 0, idesc, accumulate);
+    au_weighted_half(d_tmem, w_tmem, b, 1, idesc, true);
+}
+// A row's accumulator times `factor` to memory (zero where the token is not valid).  `loaded`: there is one.  A whole warp, one row a
+// thread: a store of 32 bytes a row costs the memory pipe as much as one of 16.  `free`: arrived on once the accumulator is read.
+__device__ __forceinline__ void st32(void* p, const uint32_t (&v)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]),
+                 "r"(v[6]), "r"(v[7]) : "memory");
+}
+__device__ __forceinline__ void au_store(uint32_t t_acc, __nv_bfloat16* out, int d, float factor, bool loaded, bool valid, bool written, bool wide, uint64_t* free) {
+#pragma unroll 1
+    for (int i = 0; i < d; i += 32) {
+        uint32_t o[32];
+        if (loaded) {
+            ptx::tmem_ld_32x32(t_acc + i, o);
+            ptx::tmem_ld_wait();
+            ptx::tmem_ld_tie(o);
+            if (i + 32 >= d) {
+                ptx::tc_fence_before_sync();
+                __syncwarp();
+                if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(free);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 32; e += 16) {
+            uint32_t v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                v[u] = valid ? round_bf16x2(__uint_as_float(o[e + 2 * u]) * factor, __uint_as_float(o[e + 2 * u + 1]) * factor) : 0u;
+            if (written && i + e < d) {
+                if (wide) {
+                    st32(out + i + e, v);
+                } else {
+                    st16(out + i + e, make_uint4(v[0], v[1], v[2], v[3]));
+                    if (i + e + 8 < d) st16(out + i + e + 8, make_uint4(v[4], v[5], v[6], v[7]));
+                }
+            }
+        }
+    }
 }
 
 struct AttentionMaps { CUtensorMap q, k, v, d_o; };
@@ -146,52 +270,75 @@ inline bool attention_map(CUtensorMap* tm, const HeadsView& t, const Sequences& 
 // ---- forward ------------------------------------------------------------------------------------------------------------
 // A block works on 256 rows of one query head at a time: two tiles, each with four warps whose threads own a row.  Per tile of 128
 // keys: S = Q K^T into tensor memory; the row's thread takes its 128 scores, its maximum and exponentials and puts P back as bf16 over
-// S; O += P V with P as the operand in tensor memory.  While one tile's warps are at their exponentials the tensor cores work for
-// the other.  O stays in tensor memory; it is scaled down only where a row's maximum has risen by more than 2^8 since the
-// reference that its exponentials are taken from (exact: l and O share the reference, and p <= 2^8 keeps its relative rounding).
-// The rounding of P to bf16 is the operand's; its sum l is taken before it, in fp32.
-constexpr int AF_THREADS = 384, AF_QUERIES = 2 * AU_ROWS;
-// 168 registers a thread at the launch; a row's 128 scores and what goes with them take more, the other four warps (two of them idle)
-// less: 256 x 208 + 128 x 88 = 384 x 168.
-constexpr int AU_LAUNCH_REGS = 168, AU_ROW_REGS = 208, AU_OTHER_REGS = 88;
-static_assert(256 * AU_ROW_REGS + 128 * AU_OTHER_REGS <= AF_THREADS * AU_LAUNCH_REGS, "what is taken has to have been given back");
+// S; O += P V with P as the operand in tensor memory, the second half of the keys first, as soon as it is there.  While one tile's
+// warps are at their exponentials the tensor cores work for the other.  O stays in tensor memory; it is scaled down only where
+// a row's maximum has risen by more than 2^8 since the reference that its exponentials are taken from (exact: the sum l and O share
+// the reference, and p <= 2^8 keeps its relative rounding).  The rounding of P to bf16 is the operand's; l is taken before it.
+// An item's first scores are computed as soon as the last product of the item before is issued, and O leaves through warps
+// of its own, so that short rows of tiles follow each other without a gap.
+constexpr int AF_QUERIES = 2 * AU_ROWS;
 constexpr float AF_RISE = 8.f;
 
 template <int DP>
-struct ForwardPlan {
+struct AttentionPlan {
     static constexpr int TILE_BYTES = DP / 64 * AU_BLOCK_BYTES;
     static constexpr int SLOTS = DP == 128 ? 5 : 8;
-    static constexpr size_t SMEM = 1024 + (size_t)(2 + SLOTS) * TILE_BYTES;
+    static constexpr size_t SMEM = 1024 + (size_t)(2 + SLOTS) * TILE_BYTES;        // two fixed tiles and the ring
 };
 
-// Tiles of keys that query tile x (0 or 1) of the item meets.
-__device__ __forceinline__ int af_key_tiles(const Tile& t, bool causal, int x) {
+// Tiles of keys that query tile x of the item meets.
+__device__ __forceinline__ int au_key_tiles(const Tile& t, bool causal, int x) {
     const int at = t.at + x * AU_ROWS;
     if (at >= t.len) return 0;
     const int end = causal ? min(t.len, at + AU_ROWS) : t.len;
     return (end + AU_ROWS - 1) / AU_ROWS;
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float y;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+    return y;
+}
+// The maximum of 32 scores and x; NaN are passed over.
+__device__ __forceinline__ float max_of(const uint32_t (&s)[32], float x) {
+    float a = __uint_as_float(s[0]), b = x;
+#pragma unroll
+    for (int e = 1; e + 3 < 32; e += 4) {
+        a = max3(a, __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+        b = max3(b, __uint_as_float(s[e + 2]), __uint_as_float(s[e + 3]));
+    }
+    return fmaxf(max3(a, __uint_as_float(s[29]), __uint_as_float(s[30])), fmaxf(b, __uint_as_float(s[31])));
+}
+__device__ __forceinline__ void mask_behind(uint32_t (&s)[32], int limit, uint32_t value) {      // entries behind `limit`
+#pragma unroll
+    for (int e = 0; e < 32; ++e) s[e] = e <= limit ? s[e] : value;
+}
 
 template <int DP>
-__global__ void __launch_bounds__(AF_THREADS, 1)
+__global__ void __launch_bounds__(AU_THREADS, 1)
 attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_constant__ AttentionMaps m, const __grid_constant__ AttentionOrder order,
                          const int works) {
-    using Plan = ForwardPlan<DP>;
+    using Plan = AttentionPlan<DP>;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t s_full[Plan::SLOTS], s_empty[Plan::SLOTS], s_qfull[2], s_qempty[2], s_scores[2], s_probs[2], s_done[2], s_tail;
+    __shared__ ItemQueue s_queue;
+    __shared__ uint64_t s_full[Plan::SLOTS], s_empty[Plan::SLOTS], s_qfull[2], s_qempty[2], s_scores[2], s_probs[2][2], s_done[2], s_sums[2], s_free[2], s_tail;
+    __shared__ float s_sum[2][AU_ROWS];
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint8_t* queries = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* ring_tiles = queries + 2 * Plan::TILE_BYTES;
     if (threadIdx.x == 0) {
+        s_queue.init(14);
         for (int i = 0; i < Plan::SLOTS; ++i) { ptx::mbar_init(&s_full[i], 1); ptx::mbar_init(&s_empty[i], 1); }
         for (int x = 0; x < 2; ++x) {
             ptx::mbar_init(&s_qfull[x], 1);
             ptx::mbar_init(&s_qempty[x], 1);
             ptx::mbar_init(&s_scores[x], 1);
-            ptx::mbar_init(&s_probs[x], 4);
+            ptx::mbar_init(&s_probs[x][0], 4);
+            ptx::mbar_init(&s_probs[x][1], 4);
             ptx::mbar_init(&s_done[x], 1);
+            ptx::mbar_init(&s_sums[x], 4);
+            ptx::mbar_init(&s_free[x], 4);
         }
         ptx::mbar_init(&s_tail, 1);
         s_abort = 0;
@@ -210,94 +357,154 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
     volatile int* abort_flag = &s_abort;
     grid_dependency_wait();
     bool ok = true;
+    ItemReader reader = {&s_queue, abort_flag};
+    Item item;
 
-    if (warp >= 8) {
-      ptx::registers_down<AU_OTHER_REGS>();
-      if (warp == AU_TMA_WARP) {
-        TileRing ring = {ring_tiles, s_full, s_empty, &s_tail, abort_flag, Plan::SLOTS, 0, 0, 0, 0, false};
-        uint32_t q_phase[2] = {0, 0};
-        for (int w = blockIdx.x; w < works && ok; w += gridDim.x) {
-            int item, h;
-            order.at(w, item, h);
-            const Tile t = find_tile<AF_QUERIES>(a.s, item);
-            if (!t.any) continue;
-            const int n0 = af_key_tiles(t, a.causal, 0), n1 = af_key_tiles(t, a.causal, 1), n = max(n0, n1);
-            const bool clear = t.first + t.len < a.s.seq;
-            for (int x = 0; x < 2 && ok; ++x) {
-                if ((x ? n1 : n0) == 0) continue;
-                ok = warp_wait(&s_qempty[x], q_phase[x] ^ 1u, abort_flag);
+    if (warp >= AU_TMA_WARP) {
+        ptx::registers_down<AU_OTHER_REGS>();
+        if (warp == AU_ITEMS_WARP) {
+            ok = au_find_items<AF_QUERIES>(s_queue, a.s, order, works, abort_flag);
+        } else if (warp == AU_TMA_WARP) {
+            TileRing ring = {ring_tiles, s_full, s_empty, &s_tail, abort_flag, Plan::SLOTS, 0, 0, 0, 0, false};
+            uint32_t q_phase[2] = {0, 0};
+            while (reader.next(item, ok)) {
+                const Tile& t = item.t;
+                const int n0 = au_key_tiles(t, a.causal, 0), n1 = au_key_tiles(t, a.causal, 1), n = max(n0, n1), hk = item.head / a.group;
+                const bool clear = t.first + t.len < a.s.seq;
+                // the second tile's queries come behind the first keys: their place is free later
+                for (int j = 0; j < n && ok; ++j) {
+                    for (int x = 0; x < 2 && ok; ++x) {
+                        if (j == 0 && (x ? n1 : n0) > 0) {
+                            ok = warp_wait(&s_qempty[x], q_phase[x] ^ 1u, abort_flag);
+                            if (!ok) break;
+                            q_phase[x] ^= 1u;
+                            if (ptx::elect_one()) {
+                                ptx::mbar_arrive_expect_tx(&s_qfull[x], Plan::TILE_BYTES);
+                                au_load<DP>(queries + x * Plan::TILE_BYTES, &m.q, t, item.head, t.at + x * AU_ROWS, &s_qfull[x]);
+                            }
+                            __syncwarp();
+                        }
+                        ok = x == 0 ? au_produce<DP>(ring, &m.k, t, hk, j * AU_ROWS, false) : au_produce<DP>(ring, &m.v, t, hk, j * AU_ROWS, clear);
+                    }
+                }
                 if (!ok) break;
-                q_phase[x] ^= 1u;
-                if (ptx::elect_one()) {
-                    ptx::mbar_arrive_expect_tx(&s_qfull[x], Plan::TILE_BYTES);
-                    au_load<DP>(queries + x * Plan::TILE_BYTES, &m.q, t, h, t.at + x * AU_ROWS, &s_qfull[x]);
-                }
-                __syncwarp();
             }
-            for (int j = 0; j < n && ok; ++j)
-                ok = au_produce<DP>(ring, &m.k, t, h / a.group, j * AU_ROWS, false) && au_produce<DP>(ring, &m.v, t, h / a.group, j * AU_ROWS, clear);
-        }
-        if (!ok) {
-            au_drain(ring);
-            int never = 0;
-            for (int x = 0; x < 2; ++x) ptx::mbar_wait(&s_qfull[x], q_phase[x] ^ 1u, &never, 1u << 14);
-        }
-      } else if (warp == AU_MMA_WARP) {
-        const uint32_t idesc_s = ptx::umma_idesc_bf16(AU_ROWS, AU_ROWS);
-        const uint32_t idesc_o = ptx::umma_idesc_bf16(AU_ROWS, (uint32_t)((a.d + 15) / 16 * 16)) | (1u << 16);      // B MN-major
-        const int steps = (a.d + 15) / 16;
-        const uint32_t q_addr = ptx::smem_u32(queries), ring_addr = ptx::smem_u32(ring_tiles);
-        uint32_t q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
-        uint32_t count = 0;                     // ring tiles of earlier items
-        const auto slot_of = [&](uint32_t i) { return i % Plan::SLOTS; };
-        const auto tile_ready = [&](uint32_t i) { return warp_wait(&s_full[slot_of(i)], (i / Plan::SLOTS) & 1u, abort_flag); };
-        for (int w = blockIdx.x; w < works && ok; w += gridDim.x) {
-            int item, h;
-            order.at(w, item, h);
-            const Tile t = find_tile<AF_QUERIES>(a.s, item);
-            if (!t.any) continue;
-            const int n0 = af_key_tiles(t, a.causal, 0), n1 = af_key_tiles(t, a.causal, 1), n = max(n0, n1);
-            // S of tile x and key tile j; the last use of key tile j frees its slot
-            const auto scores = [&](int x, int j) {
-                if (ptx::elect_one()) {
-                    au_scores(tmem + x * 128, q_addr + x * Plan::TILE_BYTES, ring_addr + slot_of(count + 2 * j) * Plan::TILE_BYTES, steps, idesc_s);
-                    ptx::umma_commit(&s_scores[x]);
-                    if (j == (x ? n1 : n0) - 1) ptx::umma_commit(&s_qempty[x]);
-                    if (x == 1 || j >= n1) ptx::umma_commit(&s_empty[slot_of(count + 2 * j)]);
+            if (!ok) {
+                au_drain(ring);
+                int never = 0;
+                for (int x = 0; x < 2; ++x) ptx::mbar_wait(&s_qfull[x], q_phase[x] ^ 1u, &never, 1u << 14);
+            }
+        } else if (warp == AU_MMA_WARP && ptx::elect_one()) {
+            const uint32_t idesc_s = ptx::umma_idesc_bf16(AU_ROWS, AU_ROWS);
+            const uint32_t idesc_o = ptx::umma_idesc_bf16(AU_ROWS, (uint32_t)((a.d + 15) / 16 * 16)) | (1u << 16);      // B MN-major
+            const int steps = (a.d + 15) / 16;
+            const uint32_t q_addr = ptx::smem_u32(queries), ring_addr = ptx::smem_u32(ring_tiles);
+            uint32_t q_phase[2] = {0, 0}, p_phase[2] = {0, 0}, f_phase[2] = {1, 1};
+            uint32_t count = 0;                                     // ring tiles before the next item
+            RingPlace<Plan::SLOTS> keys[2], values[2];              // of the tiles that x takes next
+            const auto wait = [&](uint64_t& bar, uint32_t parity) { return ptx::mbar_wait(&bar, parity, abort_flag); };
+            // S of tile x and its next key tile; `free`: the tile's last use
+            const auto scores = [&](int x, bool first, bool last, bool free) {
+                RingPlace<Plan::SLOTS>& k = keys[x];
+                if (first) {
+                    if (!wait(s_qfull[x], q_phase[x])) return false;
+                    q_phase[x] ^= 1u;
                 }
-                __syncwarp();
-            };
-            for (int x = 0; x < 2 && ok; ++x) {
-                if ((x ? n1 : n0) == 0) continue;
-                ok = warp_wait(&s_qfull[x], q_phase[x], abort_flag) && tile_ready(count);
-                q_phase[x] ^= 1u;
+                if (!wait(s_full[k.slot], k.phase)) return false;
                 ptx::tc_fence_after_sync();
-                if (ok) scores(x, 0);
+                au_scores<DP>(tmem + x * 128, q_addr + x * Plan::TILE_BYTES, ring_addr + k.slot * Plan::TILE_BYTES, steps, idesc_s);
+                ptx::umma_commit(&s_scores[x]);
+                if (last) ptx::umma_commit(&s_qempty[x]);
+                if (free) ptx::umma_commit(&s_empty[k.slot]);
+                k.move(2);
+                return true;
+            };
+            const auto weighted = [&](int x, bool first, bool last, bool free) {
+                RingPlace<Plan::SLOTS>& v = values[x];
+                if (!wait(s_full[v.slot], v.phase)) return false;
+                if (first) {
+                    if (!wait(s_free[x], f_phase[x])) return false;
+                    f_phase[x] ^= 1u;
+                }
+#pragma unroll
+                for (int half = 1; half >= 0; --half) {
+                    if (!wait(s_probs[x][half], p_phase[x])) return false;
+                    ptx::tc_fence_after_sync();
+                    au_weighted_half(tmem + 256 + x * 128, tmem + x * 128, ring_addr + v.slot * Plan::TILE_BYTES, half, idesc_o, !first || half == 0);
+                }
+                p_phase[x] ^= 1u;
+                if (last) ptx::umma_commit(&s_done[x]);
+                if (free) ptx::umma_commit(&s_empty[v.slot]);
+                v.move(2);
+                return true;
+            };
+            // the places of an item whose ring tiles begin at `count`
+            const auto begin = [&](int x) { keys[x].to(count); };
+            bool more = reader.next_alone(item, ok);
+            int n0 = 0, n1 = 0;
+            if (more) {
+                n0 = au_key_tiles(item.t, a.causal, 0), n1 = au_key_tiles(item.t, a.causal, 1);
+                if (n0 > 0) ok = scores(0, true, n0 == 1, n1 == 0);
+                if (ok && n1 > 0) ok = scores(1, true, n1 == 1, true);
             }
-            for (int j = 0; j < n && ok; ++j) {
+            while (more && ok) {
+                const int n = max(n0, n1);
+                values[0].to(count + 1);
+                values[1].to(count + 1);
+                count += 2 * n;
+                int m0 = 0, m1 = 0;                                 // the next item's tiles
+                more = reader.next_alone(item, ok);
+                if (!ok) break;
+                if (more) m0 = au_key_tiles(item.t, a.causal, 0), m1 = au_key_tiles(item.t, a.causal, 1);
+                bool begun[2] = {false, false};
+                for (int j = 0; j < n && ok; ++j) {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const int mine = x ? n1 : n0, next = x ? m1 : m0;
+                        if (j >= mine || !ok) continue;
+                        ok = weighted(x, j == 0, j == mine - 1, x == 1 || j >= n1);
+                        if (!ok) continue;
+                        if (j + 1 < mine) {
+                            ok = scores(x, false, j + 2 == mine, x == 1 || j + 1 >= n1);
+                        } else if (next > 0 && (x == 0 || begun[0])) {
+                            begin(x);
+                            ok = scores(x, true, next == 1, x == 1 || m1 == 0);
+                            begun[x] = true;
+                        }
+                    }
+                }
                 for (int x = 0; x < 2 && ok; ++x) {
-                    const int mine = x ? n1 : n0;
-                    if (j >= mine) continue;
-                    ok = tile_ready(count + 2 * j + 1) && warp_wait(&s_probs[x], p_phase[x], abort_flag);
-                    p_phase[x] ^= 1u;
+                    if ((x ? m1 : m0) == 0 || begun[x]) continue;
+                    begin(x);
+                    ok = scores(x, true, (x ? m1 : m0) == 1, x == 1 || m1 == 0);
+                }
+                n0 = m0;
+                n1 = m1;
+            }
+        }
+    } else if (warp >= AU_FINISH_WARP) {
+        ptx::registers_down<AU_OTHER_REGS>();
+        const int row = (warp & 3) * 32 + lane;
+        const uint32_t lanes = ((uint32_t)(warp & 3) * 32) << 16;
+        uint32_t phase[2] = {0, 0};
+        while (reader.next(item, ok)) {
+            const Tile& t = item.t;
+            for (int x = 0; x < 2 && ok; ++x) {
+                const int me = t.at + x * AU_ROWS + row, n = au_key_tiles(t, a.causal, x);
+                if (t.at + x * AU_ROWS >= t.rows) continue;
+                float sum = 1.f;
+                if (n > 0) {
+                    ok = warp_wait(&s_sums[x], phase[x], abort_flag) && warp_wait(&s_done[x], phase[x], abort_flag);
+                    phase[x] ^= 1u;
                     if (!ok) break;
                     ptx::tc_fence_after_sync();
-                    if (ptx::elect_one()) {
-                        au_weighted(tmem + 256 + x * 128, tmem + x * 128, ring_addr + slot_of(count + 2 * j + 1) * Plan::TILE_BYTES, idesc_o, j > 0);
-                        if (j == mine - 1) ptx::umma_commit(&s_done[x]);
-                        if (x == 1 || j >= n1) ptx::umma_commit(&s_empty[slot_of(count + 2 * j + 1)]);
-                    }
-                    __syncwarp();
-                    if (j + 1 < mine) {
-                        ok = tile_ready(count + 2 * j + 2);
-                        ptx::tc_fence_after_sync();
-                        if (ok) scores(x, j + 1);
-                    }
+                    sum = s_sum[x][row];
                 }
+                const bool valid = me < t.len, written = me < t.rows;
+                au_store(tmem + 256 + x * 128 + lanes, a.o.at<__nv_bfloat16>(t.b, t.first + me, item.head), a.d, 1.f / sum, n > 0, valid, written, a.wide, &s_free[x]);
             }
-            count += 2 * n;
+            if (!ok) break;
         }
-      }
     } else {
         ptx::registers_up<AU_ROW_REGS>();
         const int x = warp >> 2;
@@ -305,13 +512,10 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
         const uint32_t lanes = ((uint32_t)(warp & 3) * 32) << 16;
         const uint32_t t_s = tmem + x * 128 + lanes, t_o = tmem + 256 + x * 128 + lanes;
         const float c = a.scale * LOG2E;
-        uint32_t s_phase = 0, d_phase = 0;
-        for (int w = blockIdx.x; w < works && ok; w += gridDim.x) {
-            int item, h;
-            order.at(w, item, h);
-            const Tile t = find_tile<AF_QUERIES>(a.s, item);
-            if (!t.any) continue;
-            const int n = af_key_tiles(t, a.causal, x), me = t.at + x * AU_ROWS + row;
+        uint32_t s_phase = 0, f_phase = 1;
+        while (reader.next(item, ok)) {
+            const Tile& t = item.t;
+            const int n = au_key_tiles(t, a.causal, x), me = t.at + x * AU_ROWS + row;
             const int last = a.causal ? min(me, t.len - 1) : t.len - 1;       // the last key that the row sees
             float top = -INFINITY, sum = 0.f;
             for (int j = 0; j < n; ++j) {
@@ -328,18 +532,9 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
                 const int limit = last - j * AU_ROWS;
                 if (__any_sync(0xffffffffu, limit < AU_ROWS - 1)) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) s[i][e] = 32 * i + e <= limit ? s[i][e] : 0xFF800000u;
+                    for (int i = 0; i < 4; ++i) mask_behind(s[i], limit - 32 * i, 0xFF800000u);
                 }
-                float best[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    best[i] = __uint_as_float(s[i][0]);
-#pragma unroll
-                    for (int e = 1; e < 32; ++e) best[i] = fmaxf(best[i], __uint_as_float(s[i][e]));
-                }
-                const float seen = fmaxf(top, fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3])));
+                const float seen = fmaxf(max_of(s[0], top), fmaxf(max_of(s[1], top), fmaxf(max_of(s[2], top), max_of(s[3], top))));
                 if (j == 0) {
                     top = seen;
                 } else if (__any_sync(0xffffffffu, (seen - top) * c > AF_RISE)) {
@@ -348,71 +543,54 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
                     top = seen;
                     sum *= keep;
 #pragma unroll 1
-                    for (int i = 0; i < DP; i += 32) {
-                        uint32_t o[32];
-                        ptx::tmem_ld_32x32(t_o + i, o);
-                        ptx::tmem_ld_wait();
-                        ptx::tmem_ld_tie(o);
+                    for (int i = 0; i < DP; i += 8) {
+                        uint32_t o[8];
+                        ptx::tmem_ld_32x8(t_o + i, o);
+                        ptx::tmem_ld_wait(o);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
-                        ptx::tmem_st_32x32(t_o + i, o);
+                        for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
+                        ptx::tmem_st_32x8(t_o + i, o);
                     }
                 }
                 const float less = top == -INFINITY ? 0.f : -top * c;         // a row that has seen no finite score
                 float2 part[2] = {twice(0.f), twice(0.f)};
                 const float2 cc = twice(c), ll = twice(less);
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    uint32_t p[32];
+                for (int half = 1; half >= 0; --half) {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        const uint32_t *from = &s[2 * i + e / 16][2 * (e % 16)];
-                        const float2 f = fma2(make_float2(__uint_as_float(from[0]), __uint_as_float(from[1])), cc, ll);
-                        const float2 y = make_float2(exp2_approx(f.x), exp2_approx(f.y));
-                        part[e & 1] = add2(part[e & 1], y);
-                        p[e] = round_bf16x2(y.x, y.y);
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t p[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const uint32_t* from = &s[2 * half + i][2 * e];
+                            const float2 f = fma2(make_float2(__uint_as_float(from[0]), __uint_as_float(from[1])), cc, ll);
+                            const float2 y = make_float2(exp2_approx(f.x), exp2_approx(f.y));
+                            part[e & 1] = add2(part[e & 1], y);
+                            p[e] = round_bf16x2(y.x, y.y);
+                        }
+                        ptx::tmem_st_32x16(t_s + 64 * half + 16 * i, p);
                     }
-                    ptx::tmem_st_32x32(t_s + 32 * i, p);
+                    ptx::tmem_st_wait();
+                    ptx::tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(&s_probs[x][half]);
                 }
                 sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
-                ptx::tmem_st_wait();
-                ptx::tc_fence_before_sync();
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(&s_probs[x]);
             }
             if (!ok) break;
+            if (a.lse && me < t.rows) a.lse[a.row_number(t, item.head) + me] = me < t.len ? fmaf(top, a.scale, logf(sum)) : -INFINITY;
             if (n > 0) {
-                ok = warp_wait(&s_done[x], d_phase, abort_flag);
+                ok = warp_wait(&s_free[x], f_phase, abort_flag);       // the item before has left, and its sums have been read
                 if (!ok) break;
-                d_phase ^= 1u;
-                ptx::tc_fence_after_sync();
+                f_phase ^= 1u;
+                s_sum[x][row] = sum;
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&s_sums[x]);
             }
-            if (t.at + x * AU_ROWS >= t.rows) continue;
-            const bool valid = me < t.len, written = me < t.rows;
-            const float factor = 1.f / sum;
-            __nv_bfloat16* out = a.o.at<__nv_bfloat16>(t.b, t.first + me, h);
-#pragma unroll 1
-            for (int i = 0; i < a.d; i += 32) {
-                uint32_t o[32];
-                if (n > 0) {
-                    ptx::tmem_ld_32x32(t_o + i, o);
-                    ptx::tmem_ld_wait();
-                    ptx::tmem_ld_tie(o);
-                }
-#pragma unroll
-                for (int e = 0; e < 32; e += 8) {
-                    uint32_t v[4];
-#pragma unroll
-                    for (int u = 0; u < 4; ++u)
-                        v[u] = valid ? round_bf16x2(__uint_as_float(o[e + 2 * u]) * factor, __uint_as_float(o[e + 2 * u + 1]) * factor) : 0u;
-                    if (written && i + e < a.d) st16(out + i + e, make_uint4(v[0], v[1], v[2], v[3]));
-                }
-            }
-            if (written && a.lse) a.lse[a.row_number(t, h) + me] = valid ? fmaf(top, a.scale, logf(sum)) : -INFINITY;
-            ptx::tc_fence_before_sync();       // O has been read before the next item's first probabilities are announced
         }
     }
-    if (!ok && lane == 0) raise_status(DEV_TIMEOUT);
+    if (!ok) raise_status(DEV_TIMEOUT);
+    __syncwarp();
     ptx::tc_fence_before_sync();
     __syncthreads();
     if (warp == AU_MMA_WARP) {

@@ -924,9 +924,9 @@ bool heads_view(const pamm_heads* t, const AttentionShape& g, int64_t heads, siz
     return !output || ((g.batch == 1 || out.batch != 0) && (g.seq == 1 || out.token != 0) && (heads == 1 || out.head != 0));
 }
 // Whole 16-byte vectors on memory's grid in every row.
-bool heads_aligned(const HeadsView& t, size_t es) {
-    const auto on = [&](int64_t stride) { return stride * (int64_t)es % 16 == 0; };
-    return aligned(t.p, 16) && on(t.batch) && on(t.token) && on(t.head);
+bool heads_aligned(const HeadsView& t, size_t es, int64_t to = 16) {
+    const auto on = [&](int64_t stride) { return stride * (int64_t)es % to == 0; };
+    return aligned(t.p, (size_t)to) && on(t.batch) && on(t.token) && on(t.head);
 }
 
 pamm_status check_attention(const AttentionShape& g, pamm_dtype dt, float scale, const void* lengths, const void* starts,
@@ -981,27 +981,27 @@ pamm_status run_attention_generic(const AttentionArgs& a, bool back, cudaStream_
 
 template <int DP>
 pamm_status launch_attention_forward(AttentionArgs a, const AttentionMaps& m, cudaStream_t st) {
-    using Plan = ForwardPlan<DP>;
+    using Plan = AttentionPlan<DP>;
     if (!ensure_dynamic_smem((const void*)attention_forward_kernel<DP>, Plan::SMEM)) return PAMM_ERR_CUDA;
     a.s.items = tiles_of(a.s, AF_QUERIES);
     const int works = a.s.items * a.heads, blocks = std::min(works, sm_count());
-    launch(attention_forward_kernel<DP>, dim3((unsigned)blocks), dim3(AF_THREADS), Plan::SMEM, st, true, a, m,
+    launch(attention_forward_kernel<DP>, dim3((unsigned)blocks), dim3(AU_THREADS), Plan::SMEM, st, true, a, m,
            attention_order(a.s, a.heads, AF_QUERIES, blocks, a.causal), works);
     return launch_result("attention_forward_kernel launch");
 }
 
 template <int DP>
 pamm_status launch_attention_backward(AttentionArgs a, const AttentionMaps& m, cudaStream_t st) {
-    using Plan = BackwardPlan<DP>;
+    using Plan = AttentionPlan<DP>;
     if (!ensure_dynamic_smem((const void*)attention_queries_backward_kernel<DP>, Plan::SMEM) ||
         !ensure_dynamic_smem((const void*)attention_keys_backward_kernel<DP>, Plan::SMEM))
         return PAMM_ERR_CUDA;
     a.s.items = tiles_of(a.s, AU_ROWS);
     const int kv = a.heads / a.group, rows = a.s.items * a.heads, keys = a.s.items * kv, sms = sm_count();
     const int row_blocks = std::min(rows, sms), key_blocks = std::min(keys, sms);
-    launch(attention_queries_backward_kernel<DP>, dim3((unsigned)row_blocks), dim3(AB_THREADS), Plan::SMEM, st, true, a, m,
+    launch(attention_queries_backward_kernel<DP>, dim3((unsigned)row_blocks), dim3(AU_THREADS), Plan::SMEM, st, true, a, m,
            attention_order(a.s, a.heads, AU_ROWS, row_blocks, a.causal), rows);
-    launch(attention_keys_backward_kernel<DP>, dim3((unsigned)key_blocks), dim3(AB_THREADS), Plan::SMEM, st, true, a, m,
+    launch(attention_keys_backward_kernel<DP>, dim3((unsigned)key_blocks), dim3(AU_THREADS), Plan::SMEM, st, true, a, m,
            attention_order(a.s, kv, AU_ROWS, key_blocks, false), keys);
     return launch_result("attention_keys_backward_kernel launch");
 }
@@ -1070,6 +1070,7 @@ pamm_status pamm_attention_forward(const pamm_heads* Q, const pamm_heads* K, con
     a.heads = (int)heads; a.group = (int)(heads / kv_heads); a.d = (int)head_dim;
     a.scale = scale; a.causal = causal != 0;
     a.vectors = head_dim * (int64_t)es % 16 == 0 && heads_aligned(a.q, es) && heads_aligned(a.k, es) && heads_aligned(a.v, es) && heads_aligned(a.o, es);
+    a.wide = head_dim * (int64_t)es % 32 == 0 && heads_aligned(a.o, es, 32);
     return run_attention(a, dt, false, (cudaStream_t)stream);
 }
 
@@ -1095,6 +1096,7 @@ pamm_status pamm_attention_backward(const pamm_heads* dO, const pamm_heads* Q, c
     a.scale = scale; a.causal = causal != 0;
     a.vectors = head_dim * (int64_t)es % 16 == 0;
     for (const HeadsView* t : {&a.q, &a.k, &a.v, &a.o, &a.d_o, &a.dq, &a.dk, &a.dv}) a.vectors = a.vectors && heads_aligned(*t, es);
+    a.wide = head_dim * (int64_t)es % 32 == 0 && heads_aligned(a.dq, es, 32) && heads_aligned(a.dk, es, 32) && heads_aligned(a.dv, es, 32);
     return run_attention(a, dt, true, (cudaStream_t)stream);
 }
 
