@@ -55,8 +55,7 @@ __device__ __forceinline__ void ab_drain(const TileRing& ring, uint64_t* full) {
     for (int x = 0; x < 4; ++x) ptx::mbar_wait(&full[x & 1], (uint32_t)x >> 1, &never, 1u << 14);
 }
 
-// Rows of queries: dQ and delta.  Tensor memory: two buffers of S (dS takes their place), dP, dQ.  One warp sums dO O of the next
-// item's rows ahead of time.
+// Rows of queries: dQ and delta.  Tensor memory: two buffers of S (dS takes their place), dP, dQ.
 template <int DP>
 __global__ void __launch_bounds__(AU_THREADS, 1)
 attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const __grid_constant__ AttentionMaps m, const __grid_constant__ AttentionOrder order,
@@ -73,7 +72,7 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
     uint8_t* fixed = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* ring_tiles = fixed + 2 * Plan::TILE_BYTES;
     if (threadIdx.x == 0) {
-        s_queue.init(15);
+        s_queue.init(14);
         for (int i = 0; i < Plan::SLOTS; ++i) { ptx::mbar_init(&s_full[i], 1); ptx::mbar_init(&s_empty[i], 1); }
         for (int x = 0; x < 2; ++x) {
             ptx::mbar_init(&s_ffull[x], 1);
@@ -85,7 +84,7 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
         ptx::mbar_init(&s_read, 8);
         ptx::mbar_init(&s_done, 1);
         ptx::mbar_init(&s_free, 4);
-        ptx::mbar_init(&s_rows, 1);
+        ptx::mbar_init(&s_rows, 4);
         ptx::mbar_init(&s_rows_free, 8);
         ptx::mbar_init(&s_tail, 1);
         s_abort = 0;
@@ -190,76 +189,73 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
                 one = two;
             }
           }
-        } else {
-            // delta and the log-sums of the item's rows, half a row of 16-byte pieces a thread
-            uint32_t phase = 1;
-            while (reader.next(item, ok)) {
+        }
+    } else if (warp >= AU_FINISH_WARP) {
+        // An item's deltas and log-sums before its first step, while the item before is computed; then the gradients of that one.
+        ptx::registers_down<AU_OTHER_REGS>();
+        const int quarter = (warp & 3) * 32, row = quarter + lane;
+        const uint32_t lanes = (uint32_t)quarter << 16;
+        uint32_t done_phase = 0, rows_phase = 1;
+        Item before;
+        bool any = false, more = true;
+        while (more || any) {
+            more = more && reader.next(item, ok);
+            if (!ok) break;
+            if (more && au_key_tiles(item.t, a.causal, 0) > 0) {
                 const Tile& t = item.t;
-                if (au_key_tiles(t, a.causal, 0) == 0) continue;
-                const int64_t number = a.row_number(t, item.head) + t.at;
-                const int pieces = a.d / 8, piece = lane & 15, valid = min(AU_ROWS, t.len - t.at);
-                const bool mine = piece < pieces;
-                const __nv_bfloat16 *o = a.o.at<__nv_bfloat16>(t.b, t.first + t.at, item.head) + piece * 8;
-                const __nv_bfloat16 *g = a.d_o.at<__nv_bfloat16>(t.b, t.first + t.at, item.head) + piece * 8;
-                float less[4], delta[4];
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    less[u] = u * 32 + lane < valid ? -a.lse_in[number + u * 32 + lane] * LOG2E : 0.f;
-                    delta[u] = 0.f;
+                const int pieces = a.d / 8, piece = lane & 15, valid = t.len - t.at - quarter;      // of 16 bytes, 16 lanes a row
+                const int64_t number = a.row_number(t, item.head) + t.at + quarter;
+                const __nv_bfloat16 *o = a.o.at<__nv_bfloat16>(t.b, t.first + t.at + quarter, item.head) + piece * 8;
+                const __nv_bfloat16 *g = a.d_o.at<__nv_bfloat16>(t.b, t.first + t.at + quarter, item.head) + piece * 8;
+                const float less = lane < valid ? -a.lse_in[number + lane] * LOG2E : 0.f;
+                float delta = 0.f;
 #pragma unroll 1
-                    for (int r = 0; r < 32; r += 8) {       // 16 lanes a row, eight rows of loads in flight
-                        uint4 x[4], y[4];
+                for (int r = 0; r < 32; r += 8) {       // eight rows of loads in flight
+                    uint4 x[4], y[4];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int row = u * 32 + r + 2 * i + (lane >> 4);
-                            x[i] = y[i] = make_uint4(0, 0, 0, 0);
-                            if (mine && row < valid) {
-                                x[i] = *reinterpret_cast<const uint4*>(o + row * a.o.token);
-                                y[i] = *reinterpret_cast<const uint4*>(g + row * a.d_o.token);
-                            }
-                        }
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            float p[8], q[8], part = 0.f;
-                            unpack_vec<__nv_bfloat16>(x[i], p);
-                            unpack_vec<__nv_bfloat16>(y[i], q);
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) part = fmaf(p[e], q[e], part);
-                            part = warp_sum<16>(part);
-                            const float both[2] = {__shfl_sync(0xffffffffu, part, 0), __shfl_sync(0xffffffffu, part, 16)};
-                            if (lane == r + 2 * i) delta[u] = both[0];
-                            if (lane == r + 2 * i + 1) delta[u] = both[1];
+                    for (int i = 0; i < 4; ++i) {
+                        const int at = r + 2 * i + (lane >> 4);
+                        x[i] = y[i] = make_uint4(0, 0, 0, 0);
+                        if (piece < pieces && at < valid) {
+                            x[i] = *reinterpret_cast<const uint4*>(o + at * a.o.token);
+                            y[i] = *reinterpret_cast<const uint4*>(g + at * a.d_o.token);
                         }
                     }
-                    if (u * 32 + lane < valid) a.delta[number + u * 32 + lane] = delta[u];
-                }
-                ok = warp_wait(&s_rows_free, phase, abort_flag);
-                if (!ok) break;
-                phase ^= 1u;
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    s_less[u * 32 + lane] = less[u];
-                    s_delta[u * 32 + lane] = delta[u];
+                    for (int i = 0; i < 4; ++i) {
+                        float p[8], q[8], part = 0.f;
+                        unpack_vec<__nv_bfloat16>(x[i], p);
+                        unpack_vec<__nv_bfloat16>(y[i], q);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) part = fmaf(p[e], q[e], part);
+                        part = warp_sum<16>(part);
+                        const float mine = __shfl_sync(0xffffffffu, part, (lane & 1) * 16);
+                        if ((lane >> 1) == (r >> 1) + i) delta = mine;
+                    }
                 }
+                if (lane < valid) a.delta[number + lane] = delta;
+                ok = warp_wait(&s_rows_free, rows_phase, abort_flag);
+                if (!ok) break;
+                rows_phase ^= 1u;
+                s_less[row] = less;
+                s_delta[row] = delta;
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(&s_rows);
             }
-        }
-    } else if (warp >= AU_FINISH_WARP) {
-        ptx::registers_down<AU_OTHER_REGS>();
-        const int row = (warp & 3) * 32 + lane;
-        const uint32_t lanes = ((uint32_t)(warp & 3) * 32) << 16;
-        uint32_t phase = 0;
-        while (reader.next(item, ok)) {
-            const Tile& t = item.t;
-            const int n = au_key_tiles(t, a.causal, 0), me = t.at + row;
-            if (n > 0) {
-                ok = warp_wait(&s_done, phase, abort_flag);
-                if (!ok) break;
-                phase ^= 1u;
-                ptx::tc_fence_after_sync();
+            if (any) {
+                const Tile& t = before.t;
+                const int n = au_key_tiles(t, a.causal, 0), me = t.at + row;
+                if (n > 0) {
+                    ok = warp_wait(&s_done, done_phase, abort_flag);
+                    if (!ok) break;
+                    done_phase ^= 1u;
+                    ptx::tc_fence_after_sync();
+                }
+                au_store(tmem + 384 + lanes, a.dq.at<__nv_bfloat16>(t.b, t.first + me, before.head), a.d, a.scale, n > 0, me < t.len, me < t.rows, a.wide,
+                         &s_free);
             }
-            au_store(tmem + 384 + lanes, a.dq.at<__nv_bfloat16>(t.b, t.first + me, item.head), a.d, a.scale, n > 0, me < t.len, me < t.rows, a.wide, &s_free);
+            before = item;
+            any = more;
         }
     } else {
         ptx::registers_up<AU_ROW_REGS>();
