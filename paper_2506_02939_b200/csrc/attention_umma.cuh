@@ -13,8 +13,11 @@ namespace pamm {
 constexpr int AU_ROWS = 128, AU_BLOCK_BYTES = AU_ROWS * 128;       // of a tile, and of 64 of its columns
 
 // The 16 warps of a block: eight own rows of scores, four take accumulators out of tensor memory (a warp reaches the 32
-// lanes of its number modulo 4 only), and one each copies tiles in, issues the products, fetches numbers of rows and finds the
-// next items.  Registers: 128 a thread at the launch; the rows' warps take what the others give back.
+// lanes of its number modulo 4 only), one copies tiles in, one or two issue products, one brings
+// numbers of rows (backward, keys) and one finds the next items.  A thread's wait gets its answer only when the thread's own
+// products before it have been taken by the tensor cores (165 clocks a wait that is long over, where products follow
+// each other without a gap otherwise); where products wait for different warps, a second thread's fill that time.
+// Registers: 128 a thread at the launch; the rows' warps take what the others give back.
 constexpr int AU_THREADS = 512, AU_FINISH_WARP = 8, AU_TMA_WARP = 12, AU_MMA_WARP = 13, AU_STATS_WARP = 14, AU_ITEMS_WARP = 15;
 constexpr int AU_ROW_REGS = 168, AU_OTHER_REGS = 88;
 static_assert(256 * AU_ROW_REGS + 256 * AU_OTHER_REGS <= 65536, "what is taken has to have been given back");
@@ -103,22 +106,6 @@ struct ItemReader {
         ptx::mbar_arrive(&q->empty[slot]);
         ++count;
         return item.t.rows >= 0;
-    }
-};
-// A place in the ring of a thread that goes through it.
-template <int SLOTS>
-struct RingPlace {
-    uint32_t slot = 0, phase = 0;
-    __device__ __forceinline__ void move(uint32_t by) {      // by at most SLOTS
-        slot += by;
-        if (slot >= SLOTS) {
-            slot -= SLOTS;
-            phase ^= 1u;
-        }
-    }
-    __device__ __forceinline__ void to(uint32_t tile) {
-        slot = tile % SLOTS;
-        phase = (tile / SLOTS) & 1u;
     }
 };
 // The warp that finds them.
@@ -328,8 +315,8 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
     uint8_t* queries = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* ring_tiles = queries + 2 * Plan::TILE_BYTES;
     if (threadIdx.x == 0) {
-        s_queue.init(14);
-        for (int i = 0; i < Plan::SLOTS; ++i) { ptx::mbar_init(&s_full[i], 1); ptx::mbar_init(&s_empty[i], 1); }
+        s_queue.init(15);
+        for (int i = 0; i < Plan::SLOTS; ++i) { ptx::mbar_init(&s_full[i], 1); ptx::mbar_init(&s_empty[i], 2); }
         for (int x = 0; x < 2; ++x) {
             ptx::mbar_init(&s_qfull[x], 1);
             ptx::mbar_init(&s_qempty[x], 1);
@@ -394,92 +381,61 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
                 int never = 0;
                 for (int x = 0; x < 2; ++x) ptx::mbar_wait(&s_qfull[x], q_phase[x] ^ 1u, &never, 1u << 14);
             }
-        } else if (warp == AU_MMA_WARP && ptx::elect_one()) {
+        } else if (ptx::elect_one()) {
+            // The products of tile x.  Both threads go through all ring tiles, so that each tile is given back twice.
+            const int x = warp - AU_MMA_WARP;
             const uint32_t idesc_s = ptx::umma_idesc_bf16(AU_ROWS, AU_ROWS);
             const uint32_t idesc_o = ptx::umma_idesc_bf16(AU_ROWS, (uint32_t)((a.d + 15) / 16 * 16)) | (1u << 16);      // B MN-major
             const int steps = (a.d + 15) / 16;
-            const uint32_t q_addr = ptx::smem_u32(queries), ring_addr = ptx::smem_u32(ring_tiles);
-            uint32_t q_phase[2] = {0, 0}, p_phase[2] = {0, 0}, f_phase[2] = {1, 1};
-            uint32_t count = 0;                                     // ring tiles before the next item
-            RingPlace<Plan::SLOTS> keys[2], values[2];              // of the tiles that x takes next
-            const auto wait = [&](uint64_t& bar, uint32_t parity) { return ptx::mbar_wait(&bar, parity, abort_flag); };
-            // S of tile x and its next key tile; `free`: the tile's last use
-            const auto scores = [&](int x, bool first, bool last, bool free) {
-                RingPlace<Plan::SLOTS>& k = keys[x];
-                if (first) {
-                    if (!wait(s_qfull[x], q_phase[x])) return false;
-                    q_phase[x] ^= 1u;
-                }
-                if (!wait(s_full[k.slot], k.phase)) return false;
-                ptx::tc_fence_after_sync();
-                au_scores<DP>(tmem + x * 128, q_addr + x * Plan::TILE_BYTES, ring_addr + k.slot * Plan::TILE_BYTES, steps, idesc_s);
-                ptx::umma_commit(&s_scores[x]);
-                if (last) ptx::umma_commit(&s_qempty[x]);
-                if (free) ptx::umma_commit(&s_empty[k.slot]);
-                k.move(2);
-                return true;
-            };
-            const auto weighted = [&](int x, bool first, bool last, bool free) {
-                RingPlace<Plan::SLOTS>& v = values[x];
-                if (!wait(s_full[v.slot], v.phase)) return false;
-                if (first) {
-                    if (!wait(s_free[x], f_phase[x])) return false;
-                    f_phase[x] ^= 1u;
-                }
-#pragma unroll
-                for (int half = 1; half >= 0; --half) {
-                    if (!wait(s_probs[x][half], p_phase[x])) return false;
-                    ptx::tc_fence_after_sync();
-                    au_weighted_half(tmem + 256 + x * 128, tmem + x * 128, ring_addr + v.slot * Plan::TILE_BYTES, half, idesc_o, !first || half == 0);
-                }
-                p_phase[x] ^= 1u;
-                if (last) ptx::umma_commit(&s_done[x]);
-                if (free) ptx::umma_commit(&s_empty[v.slot]);
-                v.move(2);
-                return true;
-            };
-            // the places of an item whose ring tiles begin at `count`
-            const auto begin = [&](int x) { keys[x].to(count); };
-            bool more = reader.next_alone(item, ok);
-            int n0 = 0, n1 = 0;
-            if (more) {
-                n0 = au_key_tiles(item.t, a.causal, 0), n1 = au_key_tiles(item.t, a.causal, 1);
-                if (n0 > 0) ok = scores(0, true, n0 == 1, n1 == 0);
-                if (ok && n1 > 0) ok = scores(1, true, n1 == 1, true);
-            }
-            while (more && ok) {
-                const int n = max(n0, n1);
-                values[0].to(count + 1);
-                values[1].to(count + 1);
-                count += 2 * n;
-                int m0 = 0, m1 = 0;                                 // the next item's tiles
-                more = reader.next_alone(item, ok);
-                if (!ok) break;
-                if (more) m0 = au_key_tiles(item.t, a.causal, 0), m1 = au_key_tiles(item.t, a.causal, 1);
-                bool begun[2] = {false, false};
-                for (int j = 0; j < n && ok; ++j) {
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const int mine = x ? n1 : n0, next = x ? m1 : m0;
-                        if (j >= mine || !ok) continue;
-                        ok = weighted(x, j == 0, j == mine - 1, x == 1 || j >= n1);
-                        if (!ok) continue;
-                        if (j + 1 < mine) {
-                            ok = scores(x, false, j + 2 == mine, x == 1 || j + 1 >= n1);
-                        } else if (next > 0 && (x == 0 || begun[0])) {
-                            begin(x);
-                            ok = scores(x, true, next == 1, x == 1 || m1 == 0);
-                            begun[x] = true;
+            const uint32_t q_addr = ptx::smem_u32(queries) + x * Plan::TILE_BYTES, ring_addr = ptx::smem_u32(ring_tiles);
+            const uint32_t t_s = tmem + x * 128, t_o = tmem + 256 + x * 128;
+            uint32_t q_phase = 0, p_phase = 0, f_phase = 1, base = 0;        // base: ring tiles before the item
+            const auto wait = [&](uint64_t& bar, uint32_t parity) { return ptx::mbar_wait(&bar, parity & 1u, abort_flag); };
+            while (reader.next_alone(item, ok)) {
+                const int n0 = au_key_tiles(item.t, a.causal, 0), n1 = au_key_tiles(item.t, a.causal, 1), n = max(n0, n1), mine = x ? n1 : n0;
+#pragma unroll 1
+                for (int j = -1; j < n; ++j) {
+                    if (j >= 0) {
+                        const uint32_t tile = base + 2 * j + 1, slot = tile % Plan::SLOTS;
+                        if (!(ok = wait(s_full[slot], tile / Plan::SLOTS))) break;
+                        if (j < mine) {
+                            if (j == 0) {
+                                if (!(ok = wait(s_free[x], f_phase))) break;
+                                f_phase ^= 1u;
+                            }
+#pragma unroll 1
+                            for (int half = 1; half >= 0; --half) {
+                                if (!(ok = wait(s_probs[x][half], p_phase))) break;
+                                ptx::tc_fence_after_sync();
+                                au_weighted_half(t_o, t_s, ring_addr + slot * Plan::TILE_BYTES, half, idesc_o, j > 0 || half == 0);
+                            }
+                            if (!ok) break;
+                            p_phase ^= 1u;
+                            ptx::umma_commit(&s_empty[slot]);
+                            if (j == mine - 1) ptx::umma_commit(&s_done[x]);
+                        } else {
+                            ptx::mbar_arrive(&s_empty[slot]);
                         }
                     }
+                    if (j + 1 == n) break;
+                    const uint32_t tile = base + 2 * (j + 1), slot = tile % Plan::SLOTS;
+                    if (j < 0 && mine > 0) {
+                        if (!(ok = wait(s_qfull[x], q_phase))) break;
+                        q_phase ^= 1u;
+                    }
+                    if (!(ok = wait(s_full[slot], tile / Plan::SLOTS))) break;
+                    if (j + 1 < mine) {
+                        ptx::tc_fence_after_sync();
+                        au_scores<DP>(t_s, q_addr, ring_addr + slot * Plan::TILE_BYTES, steps, idesc_s);
+                        ptx::umma_commit(&s_scores[x]);
+                        ptx::umma_commit(&s_empty[slot]);
+                        if (j + 2 == mine) ptx::umma_commit(&s_qempty[x]);
+                    } else {
+                        ptx::mbar_arrive(&s_empty[slot]);
+                    }
                 }
-                for (int x = 0; x < 2 && ok; ++x) {
-                    if ((x ? m1 : m0) == 0 || begun[x]) continue;
-                    begin(x);
-                    ok = scores(x, true, (x ? m1 : m0) == 1, x == 1 || m1 == 0);
-                }
-                n0 = m0;
-                n1 = m1;
+                if (!ok) break;
+                base += 2 * n;
             }
         }
     } else if (warp >= AU_FINISH_WARP) {
@@ -523,18 +479,22 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
                 if (!ok) break;
                 s_phase ^= 1u;
                 ptx::tc_fence_after_sync();
-                uint32_t s[4][32];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) ptx::tmem_ld_32x32(t_s + 32 * i, s[i]);
-                ptx::tmem_ld_wait();
-#pragma unroll
-                for (int i = 0; i < 4; ++i) ptx::tmem_ld_tie(s[i]);
                 const int limit = last - j * AU_ROWS;
-                if (__any_sync(0xffffffffu, limit < AU_ROWS - 1)) {
+                const bool masked = __any_sync(0xffffffffu, limit < AU_ROWS - 1);
+                float seen = top;
+                {
+                    uint32_t s[4][32];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) mask_behind(s[i], limit - 32 * i, 0xFF800000u);
+                    for (int i = 0; i < 4; ++i) ptx::tmem_ld_32x32(t_s + 32 * i, s[i]);
+                    ptx::tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) ptx::tmem_ld_tie(s[i]);
+                    if (masked) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) mask_behind(s[i], limit - 32 * i, 0xFF800000u);
+                    }
+                    seen = fmaxf(max_of(s[0], top), fmaxf(max_of(s[1], top), fmaxf(max_of(s[2], top), max_of(s[3], top))));
                 }
-                const float seen = fmaxf(max_of(s[0], top), fmaxf(max_of(s[1], top), fmaxf(max_of(s[2], top), max_of(s[3], top))));
                 if (j == 0) {
                     top = seen;
                 } else if (__any_sync(0xffffffffu, (seen - top) * c > AF_RISE)) {
@@ -555,15 +515,25 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
                 const float less = top == -INFINITY ? 0.f : -top * c;         // a row that has seen no finite score
                 float2 part[2] = {twice(0.f), twice(0.f)};
                 const float2 cc = twice(c), ll = twice(less);
-#pragma unroll
+                // The scores are read a second time, by halves: the loop's code stays small, and no register holds what the other half needs.
+#pragma unroll 1
                 for (int half = 1; half >= 0; --half) {
+                    uint32_t s[2][32];
+                    ptx::tmem_ld_32x32(t_s + 64 * half, s[0]);
+                    ptx::tmem_ld_32x32(t_s + 64 * half + 32, s[1]);
+                    ptx::tmem_ld_wait();
+                    ptx::tmem_ld_tie(s[0]);
+                    ptx::tmem_ld_tie(s[1]);
+                    if (masked) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) mask_behind(s[i], limit - 64 * half - 32 * i, 0xFF800000u);
+                    }
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         uint32_t p[16];
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
-                            const uint32_t* from = &s[2 * half + i][2 * e];
-                            const float2 f = fma2(make_float2(__uint_as_float(from[0]), __uint_as_float(from[1])), cc, ll);
+                            const float2 f = fma2(make_float2(__uint_as_float(s[i][2 * e]), __uint_as_float(s[i][2 * e + 1])), cc, ll);
                             const float2 y = make_float2(exp2_approx(f.x), exp2_approx(f.y));
                             part[e & 1] = add2(part[e & 1], y);
                             p[e] = round_bf16x2(y.x, y.y);

@@ -72,7 +72,7 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
     uint8_t* fixed = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* ring_tiles = fixed + 2 * Plan::TILE_BYTES;
     if (threadIdx.x == 0) {
-        s_queue.init(14);
+        s_queue.init(15);
         for (int i = 0; i < Plan::SLOTS; ++i) { ptx::mbar_init(&s_full[i], 1); ptx::mbar_init(&s_empty[i], 1); }
         for (int x = 0; x < 2; ++x) {
             ptx::mbar_init(&s_ffull[x], 1);
@@ -127,68 +127,74 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
                 if (n > 0) f_phase ^= 1u;
             }
             if (!ok) ab_drain(ring, s_ffull);
-        } else if (warp == AU_MMA_WARP) {
-          if (ptx::elect_one()) {
+        } else if (warp == AU_MMA_WARP && ptx::elect_one()) {
+            // S two steps ahead of dQ, whose dS takes the place of the scores it came from
             const uint32_t idesc_s = ptx::umma_idesc_bf16(AU_ROWS, AU_ROWS);
             const uint32_t idesc_g = ptx::umma_idesc_bf16(AU_ROWS, (uint32_t)((a.d + 15) / 16 * 16)) | (1u << 16);      // B MN-major
             const int steps = (a.d + 15) / 16;
             const uint32_t f_addr = ptx::smem_u32(fixed), ring_addr = ptx::smem_u32(ring_tiles);
-            uint32_t q_phase = 0, g_phase = 0, free_phase = 1, step = 0;
-            RingPlace<Plan::SLOTS> k_scores, v_grads, k_weighted;       // the next tile of each kind of product
-            v_grads.move(1);
-            const auto wait = [&](uint64_t& bar, uint32_t parity) { return ptx::mbar_wait(&bar, parity, abort_flag); };
-            const auto scores = [&](const Step& s, uint32_t buffer) {
-                if (s.first) {
-                    if (!wait(s_ffull[0], q_phase)) return false;
-                    q_phase ^= 1u;
-                }
-                if (!wait(s_full[k_scores.slot], k_scores.phase)) return false;
-                ptx::tc_fence_after_sync();
-                au_scores<DP>(tmem + buffer * 128, f_addr, ring_addr + k_scores.slot * Plan::TILE_BYTES, steps, idesc_s);
-                ptx::umma_commit(&s_scores[buffer]);
-                if (s.last) ptx::umma_commit(&s_fempty[0]);
-                k_scores.move(2);
-                return true;
-            };
-            const auto grads = [&](const Step& s) {
-                if (s.first) {
-                    if (!wait(s_ffull[1], g_phase)) return false;
-                    g_phase ^= 1u;
-                }
-                if (!wait(s_full[v_grads.slot], v_grads.phase)) return false;
-                ptx::tc_fence_after_sync();
-                au_scores<DP>(tmem + 256, f_addr + Plan::TILE_BYTES, ring_addr + v_grads.slot * Plan::TILE_BYTES, steps, idesc_s);
-                ptx::umma_commit(&s_grads);
-                ptx::umma_commit(&s_empty[v_grads.slot]);
-                if (s.last) ptx::umma_commit(&s_fempty[1]);
-                v_grads.move(2);
-                return true;
-            };
+            uint32_t q_phase = 0, free_phase = 1, scored = 0, taken = 0;        // the next ring tile of each kind of product
+            const auto wait = [&](uint64_t& bar, uint32_t parity) { return ptx::mbar_wait(&bar, parity & 1u, abort_flag); };
             StepReader<false> ahead = {reader};
-            const auto next = [&] { return ahead.next(a.causal, a.group, ok); };
-            Step now = next();
-            if (now.any) ok = scores(now, 0) && grads(now);
-            Step one = now.any && ok ? next() : now;
-            if (one.any && ok) ok = scores(one, 1);
-            for (; now.any && ok; ++step) {
-                const Step two = one.any ? next() : one;
-                if (!ok) break;
-                ok = wait(s_read, step & 1u) && (!one.any || grads(one)) && wait(s_ds[step & 1u], (step >> 1) & 1u);
-                if (ok && now.first) {
-                    ok = wait(s_free, free_phase);
-                    free_phase ^= 1u;
+            Step now = {}, one = {};
+#pragma unroll 1
+            for (int step = -2; ok; ++step) {
+                const Step two = ahead.next(a.causal, a.group, ok);
+                if (!ok || !(now.any || one.any || two.any)) break;
+                const uint32_t buffer = tmem + (step & 1) * 128;
+                if (now.any) {
+                    if (!(ok = wait(s_ds[step & 1], (uint32_t)step >> 1))) break;
+                    if (now.first) {
+                        if (!(ok = wait(s_free, free_phase))) break;
+                        free_phase ^= 1u;
+                    }
+                    const uint32_t slot = taken % Plan::SLOTS;
+                    taken += 2;
+                    ptx::tc_fence_after_sync();
+                    au_weighted(tmem + 384, buffer, ring_addr + slot * Plan::TILE_BYTES, idesc_g, !now.first);
+                    ptx::umma_commit(&s_empty[slot]);
+                    if (now.last) ptx::umma_commit(&s_done);
                 }
-                if (!ok) break;
-                ptx::tc_fence_after_sync();
-                au_weighted(tmem + 384, tmem + (step & 1u) * 128, ring_addr + k_weighted.slot * Plan::TILE_BYTES, idesc_g, !now.first);
-                ptx::umma_commit(&s_empty[k_weighted.slot]);
-                if (now.last) ptx::umma_commit(&s_done);
-                k_weighted.move(2);
-                if (two.any) ok = scores(two, step & 1u);
+                if (two.any) {
+                    if (two.first) {
+                        if (!(ok = wait(s_ffull[0], q_phase))) break;
+                        q_phase ^= 1u;
+                    }
+                    const uint32_t slot = scored % Plan::SLOTS;
+                    if (!(ok = wait(s_full[slot], scored / Plan::SLOTS))) break;
+                    scored += 2;
+                    ptx::tc_fence_after_sync();
+                    au_scores<DP>(buffer, f_addr, ring_addr + slot * Plan::TILE_BYTES, steps, idesc_s);
+                    ptx::umma_commit(&s_scores[step & 1]);
+                    if (two.last) ptx::umma_commit(&s_fempty[0]);
+                }
                 now = one;
                 one = two;
             }
-          }
+        } else if (warp == AU_MMA_WARP + 1 && ptx::elect_one()) {
+            // dP, as soon as the last one has been read
+            const uint32_t idesc_s = ptx::umma_idesc_bf16(AU_ROWS, AU_ROWS);
+            const int steps = (a.d + 15) / 16;
+            const uint32_t f_addr = ptx::smem_u32(fixed) + Plan::TILE_BYTES, ring_addr = ptx::smem_u32(ring_tiles);
+            uint32_t g_phase = 0, tile = 1;
+            const auto wait = [&](uint64_t& bar, uint32_t parity) { return ptx::mbar_wait(&bar, parity & 1u, abort_flag); };
+            StepReader<false> ahead = {reader};
+#pragma unroll 1
+            for (uint32_t step = 0; ok; ++step, tile += 2) {
+                const Step now = ahead.next(a.causal, a.group, ok);
+                if (!ok || !now.any) break;
+                if (now.first) {
+                    if (!(ok = wait(s_ffull[1], g_phase))) break;
+                    g_phase ^= 1u;
+                }
+                const uint32_t slot = tile % Plan::SLOTS;
+                if (!(ok = wait(s_full[slot], tile / Plan::SLOTS) && wait(s_read, step + 1))) break;      // the first finds it free
+                ptx::tc_fence_after_sync();
+                au_scores<DP>(tmem + 256, f_addr, ring_addr + slot * Plan::TILE_BYTES, steps, idesc_s);
+                ptx::umma_commit(&s_grads);
+                ptx::umma_commit(&s_empty[slot]);
+                if (now.last) ptx::umma_commit(&s_fempty[1]);
+            }
         }
     } else if (warp >= AU_FINISH_WARP) {
         // An item's deltas and log-sums before its first step, while the item before is computed; then the gradients of that one.
@@ -348,8 +354,8 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
     using Plan = AttentionPlan<DP>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ ItemQueue s_queue;
-    __shared__ uint64_t s_full[Plan::SLOTS], s_empty[Plan::SLOTS], s_ffull[2], s_fempty[2], s_scores, s_probs, s_grads, s_ds, s_done[2], s_free[2], s_stats[2],
-        s_tail;
+    __shared__ uint64_t s_full[Plan::SLOTS], s_empty[Plan::SLOTS], s_ffull[2], s_fempty[2], s_scores[2], s_weights[2], s_done[2], s_free[2], s_stats[2],
+        s_tail;      // [0]: S, P, dV, log-sums; [1]: dP, dS, dK, deltas
     __shared__ __align__(16) float s_less[AU_ROWS], s_delta[AU_ROWS];
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort;
@@ -363,13 +369,11 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
             ptx::mbar_init(&s_ffull[x], 1);
             ptx::mbar_init(&s_fempty[x], 1);
             ptx::mbar_init(&s_stats[x], 1);
+            ptx::mbar_init(&s_scores[x], 1);
+            ptx::mbar_init(&s_weights[x], 8);
             ptx::mbar_init(&s_done[x], 1);
             ptx::mbar_init(&s_free[x], 4);
         }
-        ptx::mbar_init(&s_scores, 1);
-        ptx::mbar_init(&s_probs, 8);
-        ptx::mbar_init(&s_grads, 1);
-        ptx::mbar_init(&s_ds, 8);
         ptx::mbar_init(&s_tail, 1);
         s_abort = 0;
         ptx::fence_barrier_init();
@@ -415,49 +419,52 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
             if (!ok) ab_drain(ring, s_ffull);
         } else if (warp == AU_MMA_WARP) {
           if (ptx::elect_one()) {
+            // dV += P^T dO and the next S^T = K Q^T (what = 0), then dK += dS^T Q and the next dP^T = V dO^T (1): the scores that the rows'
+            // warps wait for go first.  (Two threads, one a kind, had their products run between each other: 18% slower.)
             const uint32_t idesc_s = ptx::umma_idesc_bf16(AU_ROWS, AU_ROWS);
             const uint32_t idesc_g = ptx::umma_idesc_bf16(AU_ROWS, (uint32_t)((a.d + 15) / 16 * 16)) | (1u << 16);
             const int steps = (a.d + 15) / 16;
             const uint32_t f_addr = ptx::smem_u32(fixed), ring_addr = ptx::smem_u32(ring_tiles);
-            uint32_t f_phase[2] = {0, 0}, free_phase = 1, phase = 0;
-            RingPlace<Plan::SLOTS> scored[2], taken[2];       // the next tile of Q (0) and dO (1) for the scores, and as the weighted operand
-            scored[1].move(1);
-            taken[1].move(1);
-            const auto wait = [&](uint64_t& bar, uint32_t parity) { return ptx::mbar_wait(&bar, parity, abort_flag); };
-            // what = 0: S^T from K and Q; 1: dP^T from V and dO
-            const auto scores = [&](int what, const Step& s) {
-                RingPlace<Plan::SLOTS>& r = scored[what];
-                if (s.first) {
-                    if (!wait(s_ffull[what], f_phase[what])) return false;
-                    f_phase[what] ^= 1u;
-                }
-                if (!wait(s_full[r.slot], r.phase)) return false;
-                ptx::tc_fence_after_sync();
-                au_scores<DP>(tmem + what * 128, f_addr + what * Plan::TILE_BYTES, ring_addr + r.slot * Plan::TILE_BYTES, steps, idesc_s);
-                ptx::umma_commit(what ? &s_grads : &s_scores);
-                if (s.last) ptx::umma_commit(&s_fempty[what]);
-                r.move(2);
-                return true;
-            };
-            // dV += P^T dO (what = 0), dK += dS^T Q (1): the last uses of their ring tiles
-            const auto weighted = [&](int what, const Step& s) {
-                RingPlace<Plan::SLOTS>& r = taken[1 - what];
-                if (s.first && !wait(s_free[what], free_phase)) return false;
-                ptx::tc_fence_after_sync();
-                au_weighted(tmem + 256 + what * 128, tmem + what * 128, ring_addr + r.slot * Plan::TILE_BYTES, idesc_g, !s.first);
-                ptx::umma_commit(&s_empty[r.slot]);
-                if (s.last) ptx::umma_commit(&s_done[what]);
-                r.move(2);
-                return true;
-            };
+            uint32_t f_phase = 0, free_phase = 3, phase = 0;        // bit `what`
+            uint32_t scored = 0, taken = 0;         // ring tiles before the pair that the scores, and the weighted operands, take next
+            const auto wait = [&](uint64_t& bar, uint32_t parity) { return ptx::mbar_wait(&bar, parity & 1u, abort_flag); };
             StepReader<true> ahead = {reader};
-            Step now = ahead.next(a.causal, a.group, ok);
-            if (now.any) ok = scores(0, now) && scores(1, now);
-            for (; now.any && ok; phase ^= 1u) {
+            Step now = {};
+            for (bool begun = false; ok; begun = true) {
                 const Step one = ahead.next(a.causal, a.group, ok);
-                ok = ok && wait(s_probs, phase) && weighted(0, now) && (!one.any || scores(0, one)) && wait(s_ds, phase) && weighted(1, now) &&
-                     (!one.any || scores(1, one));
-                if (now.first) free_phase ^= 1u;
+                if (!ok || !(now.any || one.any)) break;
+#pragma unroll 1
+                for (int what = 0; what < 2; ++what) {
+                    if (now.any) {
+                        if (!(ok = wait(s_weights[what], phase))) break;
+                        if (now.first) {
+                            if (!(ok = wait(s_free[what], free_phase >> what))) break;
+                            free_phase ^= 1u << what;
+                        }
+                        const uint32_t slot = (taken + 1 - what) % Plan::SLOTS;
+                        ptx::tc_fence_after_sync();
+                        au_weighted(tmem + 256 + what * 128, tmem + what * 128, ring_addr + slot * Plan::TILE_BYTES, idesc_g, !now.first);
+                        ptx::umma_commit(&s_empty[slot]);
+                        if (now.last) ptx::umma_commit(&s_done[what]);
+                    }
+                    if (one.any) {
+                        if (one.first) {
+                            if (!(ok = wait(s_ffull[what], f_phase >> what))) break;
+                            f_phase ^= 1u << what;
+                        }
+                        const uint32_t tile = scored + what, slot = tile % Plan::SLOTS;
+                        if (!(ok = wait(s_full[slot], tile / Plan::SLOTS))) break;
+                        ptx::tc_fence_after_sync();
+                        au_scores<DP>(tmem + what * 128, f_addr + what * Plan::TILE_BYTES, ring_addr + slot * Plan::TILE_BYTES, steps, idesc_s);
+                        ptx::umma_commit(&s_scores[what]);
+                        if (one.last) ptx::umma_commit(&s_fempty[what]);
+                    }
+                }
+                scored += 2;
+                if (begun) {
+                    taken += 2;
+                    phase ^= 1u;
+                }
                 now = one;
             }
           }
@@ -477,13 +484,13 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
                         less[u] = valid ? -a.lse_in[number + q] * LOG2E : -INFINITY;
                         delta[u] = valid ? -a.delta[number + q] : 0.f;
                     }
-                    ok = warp_wait(&s_probs, phase, abort_flag);
+                    ok = warp_wait(&s_weights[0], phase, abort_flag);
                     if (!ok) break;
 #pragma unroll
                     for (int u = 0; u < 4; ++u) s_less[lane + 32 * u] = less[u];
                     __syncwarp();
                     if (lane == 0) ptx::mbar_arrive(&s_stats[0]);
-                    ok = warp_wait(&s_ds, phase, abort_flag);
+                    ok = warp_wait(&s_weights[1], phase, abort_flag);
                     if (!ok) break;
 #pragma unroll
                     for (int u = 0; u < 4; ++u) s_delta[lane + 32 * u] = delta[u];
@@ -523,7 +530,7 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
         while (reader.next(item, ok)) {
             const int n = ab_query_tiles(item.t, a.causal, a.group, from, per);
             for (int j = 0; j < n; ++j, phase ^= 1u) {
-                ok = warp_wait(&s_stats[0], phase, abort_flag) && warp_wait(&s_scores, phase, abort_flag);
+                ok = warp_wait(&s_stats[0], phase, abort_flag) && warp_wait(&s_scores[0], phase, abort_flag);
                 if (!ok) break;
                 ptx::tc_fence_after_sync();
                 uint32_t s[2][32];
@@ -561,8 +568,8 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
                 ptx::tmem_st_wait();
                 ptx::tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(&s_probs);
-                ok = warp_wait(&s_stats[1], phase, abort_flag) && warp_wait(&s_grads, phase, abort_flag);
+                if (lane == 0) ptx::mbar_arrive(&s_weights[0]);
+                ok = warp_wait(&s_stats[1], phase, abort_flag) && warp_wait(&s_scores[1], phase, abort_flag);
                 if (!ok) break;
                 ptx::tc_fence_after_sync();
 #pragma unroll
@@ -587,7 +594,7 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
                 ptx::tmem_st_wait();
                 ptx::tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(&s_ds);
+                if (lane == 0) ptx::mbar_arrive(&s_weights[1]);
             }
             if (!ok) break;
         }
