@@ -112,12 +112,17 @@ struct ItemReader {
 template <int SIZE>
 __device__ __forceinline__ bool au_find_items(ItemQueue& q, const Sequences& s, const AttentionOrder& order, int works, volatile int* abort_flag) {
     uint32_t count = 0;
-    for (int w = blockIdx.x;; w += gridDim.x) {
+    // there and back: the first block of a round is the last of the next, so that blocks get as much where items shrink along the order
+    // (the largest share of 2 x 8192 causal tokens of 8 key heads is 2% over the mean so, and 14% with equal rounds)
+    for (int64_t round = 0;; ++round) {
+        const bool end = round * gridDim.x >= works;
+        const int64_t w = round * gridDim.x + (round & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
         Item item;
         item.t.rows = -1;
-        if (w < works) {
+        if (!end) {
+            if (w >= works) continue;
             int number;
-            order.at(w, number, item.head);
+            order.at((int)w, number, item.head);
             item.t = find_tile<SIZE>(s, number);
             if (!item.t.any) continue;
         }
@@ -129,7 +134,7 @@ __device__ __forceinline__ bool au_find_items(ItemQueue& q, const Sequences& s, 
         }
         __syncwarp();
         ++count;
-        if (w >= works) return true;
+        if (end) return true;
     }
 }
 // The producer's ring of tiles.  Called by the whole warp.
@@ -189,7 +194,7 @@ __device__ __forceinline__ void au_drain(const TileRing& r) {
 }
 
 // The products.  One thread.  A product is issued only shortly before it runs, so what this thread computes between two of them counts.
-// D = A B^T over the heads' columns, both tiles K-major: steps of 16 columns.
+// D = A B^T over the heads' columns, both tiles K-major: steps of 16 columns.  (N, and from which row of B on, is the caller's.)
 template <int DP>
 __device__ __forceinline__ void au_scores(uint32_t d_tmem, uint32_t a, uint32_t b, int steps, uint32_t idesc) {
     const uint32_t la = ptx::umma_desc_lower_k(a), lb = ptx::umma_desc_lower_k(b);
@@ -255,14 +260,17 @@ inline bool attention_map(CUtensorMap* tm, const HeadsView& t, const Sequences& 
 }
 
 // ---- forward ------------------------------------------------------------------------------------------------------------
-// A block works on 256 rows of one query head at a time: two tiles, each with four warps whose threads own a row.  Per tile of 128
-// keys: S = Q K^T into tensor memory; the row's thread takes its 128 scores, its maximum and exponentials and puts P back as bf16 over
-// S; O += P V with P as the operand in tensor memory, the second half of the keys first, as soon as it is there.  While one tile's
-// warps are at their exponentials the tensor cores work for the other.  O stays in tensor memory; it is scaled down only where
-// a row's maximum has risen by more than 2^8 since the reference that its exponentials are taken from (exact: the sum l and O share
-// the reference, and p <= 2^8 keeps its relative rounding).  The rounding of P to bf16 is the operand's; l is taken before it.
-// An item's first scores are computed as soon as the last product of the item before is issued, and O leaves through warps
-// of its own, so that short rows of tiles follow each other without a gap.
+// A block works on 256 rows of one query head at a time: two tiles, each with four warps whose threads own a row and one thread that
+// issues its products.  Per 64 keys: S = Q K^T into tensor memory; the row's thread takes its 64 scores and their exponentials
+// and puts P back as bf16 over S; O += P V with P as the operand in tensor memory.  Two such halves of a tile of keys are under way
+// at a time, so that the scores of the one come while the exponentials of the other are taken.  (Whole tiles, S of 128 columns: the
+// chain from P to the next scores, 1500 clocks, was exposed, 4000 clocks for both query tiles against 2900 that
+// products of 64 columns take, whose other operand is read from shared memory more often.)
+// The exponentials are taken from a reference that the row's maximum had before, without waiting for the new one; where that has risen
+// by more than 2^8, O and the sum l are scaled down and the half is taken again (exact: O and l share the reference, and p <= 2^8
+// keeps its relative rounding).  The rounding of P to bf16 is the operand's; l is taken before it.
+// An item's first scores follow the last product of the item before, and O leaves through warps of its own.
+// (Exponentials on the multiply-add units, one pair of four, of eight: 2 to 5% slower; the special-function unit is half busy.)
 constexpr int AF_QUERIES = 2 * AU_ROWS;
 constexpr float AF_RISE = 8.f;
 
@@ -273,13 +281,14 @@ struct AttentionPlan {
     static constexpr size_t SMEM = 1024 + (size_t)(2 + SLOTS) * TILE_BYTES;        // two fixed tiles and the ring
 };
 
-// Tiles of keys that query tile x of the item meets.
-__device__ __forceinline__ int au_key_tiles(const Tile& t, bool causal, int x) {
+// Groups of `size` keys that query tile x of the item meets, and tiles of them.
+__device__ __forceinline__ int au_key_groups(const Tile& t, bool causal, int x, int size) {
     const int at = t.at + x * AU_ROWS;
     if (at >= t.len) return 0;
     const int end = causal ? min(t.len, at + AU_ROWS) : t.len;
-    return (end + AU_ROWS - 1) / AU_ROWS;
+    return (end + size - 1) / size;
 }
+__device__ __forceinline__ int au_key_tiles(const Tile& t, bool causal, int x) { return au_key_groups(t, causal, x, AU_ROWS); }
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float y;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
@@ -307,7 +316,7 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
     using Plan = AttentionPlan<DP>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ ItemQueue s_queue;
-    __shared__ uint64_t s_full[Plan::SLOTS], s_empty[Plan::SLOTS], s_qfull[2], s_qempty[2], s_scores[2], s_probs[2][2], s_done[2], s_sums[2], s_free[2], s_tail;
+    __shared__ uint64_t s_full[Plan::SLOTS], s_empty[Plan::SLOTS], s_qfull[2], s_qempty[2], s_scores[2][2], s_probs[2][2], s_added[2], s_done[2], s_sums[2], s_free[2], s_tail;
     __shared__ float s_sum[2][AU_ROWS];
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort;
@@ -320,9 +329,11 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
         for (int x = 0; x < 2; ++x) {
             ptx::mbar_init(&s_qfull[x], 1);
             ptx::mbar_init(&s_qempty[x], 1);
-            ptx::mbar_init(&s_scores[x], 1);
-            ptx::mbar_init(&s_probs[x][0], 4);
-            ptx::mbar_init(&s_probs[x][1], 4);
+            for (int half = 0; half < 2; ++half) {
+                ptx::mbar_init(&s_scores[x][half], 1);
+                ptx::mbar_init(&s_probs[x][half], 4);
+            }
+            ptx::mbar_init(&s_added[x], 1);
             ptx::mbar_init(&s_done[x], 1);
             ptx::mbar_init(&s_sums[x], 4);
             ptx::mbar_init(&s_free[x], 4);
@@ -384,55 +395,53 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
         } else if (ptx::elect_one()) {
             // The products of tile x.  Both threads go through all ring tiles, so that each tile is given back twice.
             const int x = warp - AU_MMA_WARP;
-            const uint32_t idesc_s = ptx::umma_idesc_bf16(AU_ROWS, AU_ROWS);
+            const uint32_t idesc_s = ptx::umma_idesc_bf16(AU_ROWS, 64);
             const uint32_t idesc_o = ptx::umma_idesc_bf16(AU_ROWS, (uint32_t)((a.d + 15) / 16 * 16)) | (1u << 16);      // B MN-major
             const int steps = (a.d + 15) / 16;
             const uint32_t q_addr = ptx::smem_u32(queries) + x * Plan::TILE_BYTES, ring_addr = ptx::smem_u32(ring_tiles);
             const uint32_t t_s = tmem + x * 128, t_o = tmem + 256 + x * 128;
-            uint32_t q_phase = 0, p_phase = 0, f_phase = 1, base = 0;        // base: ring tiles before the item
+            uint32_t q_phase = 0, p_phase = 0, f_phase = 1, base = 0;        // p_phase: bit `half`; base: ring tiles before the item
             const auto wait = [&](uint64_t& bar, uint32_t parity) { return ptx::mbar_wait(&bar, parity & 1u, abort_flag); };
             while (reader.next_alone(item, ok)) {
-                const int n0 = au_key_tiles(item.t, a.causal, 0), n1 = au_key_tiles(item.t, a.causal, 1), n = max(n0, n1), mine = x ? n1 : n0;
+                const int n = max(au_key_tiles(item.t, a.causal, 0), au_key_tiles(item.t, a.causal, 1)), mine = au_key_groups(item.t, a.causal, x, 64);
+                if (mine > 0) {
+                    if (!(ok = wait(s_qfull[x], q_phase))) break;
+                    q_phase ^= 1u;
+                }
+                // step i: O += P V of group i, then the scores of group i + 2, which take its place
 #pragma unroll 1
-                for (int j = -1; j < n; ++j) {
-                    if (j >= 0) {
-                        const uint32_t tile = base + 2 * j + 1, slot = tile % Plan::SLOTS;
+                for (int i = -2; i < mine; ++i) {
+                    const int half = i & 1, next = i + 2;
+                    if (i >= 0) {
+                        const uint32_t tile = base + (i | 1), slot = tile % Plan::SLOTS;
                         if (!(ok = wait(s_full[slot], tile / Plan::SLOTS))) break;
-                        if (j < mine) {
-                            if (j == 0) {
-                                if (!(ok = wait(s_free[x], f_phase))) break;
-                                f_phase ^= 1u;
-                            }
-#pragma unroll 1
-                            for (int half = 1; half >= 0; --half) {
-                                if (!(ok = wait(s_probs[x][half], p_phase))) break;
-                                ptx::tc_fence_after_sync();
-                                au_weighted_half(t_o, t_s, ring_addr + slot * Plan::TILE_BYTES, half, idesc_o, j > 0 || half == 0);
-                            }
-                            if (!ok) break;
-                            p_phase ^= 1u;
-                            ptx::umma_commit(&s_empty[slot]);
-                            if (j == mine - 1) ptx::umma_commit(&s_done[x]);
-                        } else {
-                            ptx::mbar_arrive(&s_empty[slot]);
+                        if (i == 0) {
+                            if (!(ok = wait(s_free[x], f_phase))) break;
+                            f_phase ^= 1u;
                         }
-                    }
-                    if (j + 1 == n) break;
-                    const uint32_t tile = base + 2 * (j + 1), slot = tile % Plan::SLOTS;
-                    if (j < 0 && mine > 0) {
-                        if (!(ok = wait(s_qfull[x], q_phase))) break;
-                        q_phase ^= 1u;
-                    }
-                    if (!(ok = wait(s_full[slot], tile / Plan::SLOTS))) break;
-                    if (j + 1 < mine) {
+                        if (!(ok = wait(s_probs[x][half], p_phase >> half))) break;
+                        p_phase ^= 1u << half;
                         ptx::tc_fence_after_sync();
-                        au_scores<DP>(t_s, q_addr, ring_addr + slot * Plan::TILE_BYTES, steps, idesc_s);
-                        ptx::umma_commit(&s_scores[x]);
-                        ptx::umma_commit(&s_empty[slot]);
-                        if (j + 2 == mine) ptx::umma_commit(&s_qempty[x]);
-                    } else {
-                        ptx::mbar_arrive(&s_empty[slot]);
+                        au_weighted_half(t_o, t_s, ring_addr + slot * Plan::TILE_BYTES, half, idesc_o, i > 0);
+                        ptx::umma_commit(&s_added[x]);
+                        if (half || i == mine - 1) ptx::umma_commit(&s_empty[slot]);
+                        if (i == mine - 1) ptx::umma_commit(&s_done[x]);
                     }
+                    if (next < mine) {
+                        const uint32_t tile = base + (next & ~1), slot = tile % Plan::SLOTS;
+                        if (!(ok = wait(s_full[slot], tile / Plan::SLOTS))) break;
+                        ptx::tc_fence_after_sync();
+                        au_scores<DP>(t_s + 64 * half, q_addr, ring_addr + slot * Plan::TILE_BYTES + half * 64 * 128, steps, idesc_s);
+                        ptx::umma_commit(&s_scores[x][half]);
+                        if (half || next == mine - 1) ptx::umma_commit(&s_empty[slot]);
+                        if (next == mine - 1) ptx::umma_commit(&s_qempty[x]);
+                    }
+                }
+                if (!ok) break;
+                for (uint32_t tile = base + (uint32_t)((mine + 1) & ~1); tile < base + 2 * n; ++tile) {      // tiles of the other's only
+                    const uint32_t slot = tile % Plan::SLOTS;
+                    if (!(ok = wait(s_full[slot], tile / Plan::SLOTS))) break;
+                    ptx::mbar_arrive(&s_empty[slot]);
                 }
                 if (!ok) break;
                 base += 2 * n;
@@ -468,37 +477,54 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
         const uint32_t lanes = ((uint32_t)(warp & 3) * 32) << 16;
         const uint32_t t_s = tmem + x * 128 + lanes, t_o = tmem + 256 + x * 128 + lanes;
         const float c = a.scale * LOG2E;
-        uint32_t s_phase = 0, f_phase = 1;
+        uint32_t s_phase = 0, f_phase = 1, total = 0;      // s_phase: bit `half`; total: groups so far
         while (reader.next(item, ok)) {
             const Tile& t = item.t;
-            const int n = au_key_tiles(t, a.causal, x), me = t.at + x * AU_ROWS + row;
+            const int n = au_key_groups(t, a.causal, x, 64), me = t.at + x * AU_ROWS + row;
             const int last = a.causal ? min(me, t.len - 1) : t.len - 1;       // the last key that the row sees
             float top = -INFINITY, sum = 0.f;
-            for (int j = 0; j < n; ++j) {
-                ok = warp_wait(&s_scores[x], s_phase, abort_flag);
+#pragma unroll 1
+            for (int g = 0; g < n; ++g, ++total) {
+                const int half = g & 1;
+                const uint32_t t_g = t_s + 64 * half;
+                ok = warp_wait(&s_scores[x][half], s_phase >> half & 1u, abort_flag);
                 if (!ok) break;
-                s_phase ^= 1u;
+                s_phase ^= 1u << half;
                 ptx::tc_fence_after_sync();
-                const int limit = last - j * AU_ROWS;
-                const bool masked = __any_sync(0xffffffffu, limit < AU_ROWS - 1);
-                float seen = top;
-                {
-                    uint32_t s[4][32];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) ptx::tmem_ld_32x32(t_s + 32 * i, s[i]);
-                    ptx::tmem_ld_wait();
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) ptx::tmem_ld_tie(s[i]);
-                    if (masked) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) mask_behind(s[i], limit - 32 * i, 0xFF800000u);
-                    }
-                    seen = fmaxf(max_of(s[0], top), fmaxf(max_of(s[1], top), fmaxf(max_of(s[2], top), max_of(s[3], top))));
+                uint32_t s[2][32];
+                ptx::tmem_ld_32x32(t_g, s[0]);
+                ptx::tmem_ld_32x32(t_g + 32, s[1]);
+                ptx::tmem_ld_wait();
+                ptx::tmem_ld_tie(s[0]);
+                ptx::tmem_ld_tie(s[1]);
+                const int limit = last - g * 64;
+                if (__any_sync(0xffffffffu, limit < 63)) {
+                    mask_behind(s[0], limit, 0xFF800000u);
+                    mask_behind(s[1], limit - 32, 0xFF800000u);
                 }
-                if (j == 0) {
-                    top = seen;
-                } else if (__any_sync(0xffffffffu, (seen - top) * c > AF_RISE)) {
-                    // the scores' arrival means that the product before, the last to add to O, is done
+                if (g == 0) top = fmaxf(max_of(s[0], top), max_of(s[1], top));
+                const float2 cc = twice(c);
+                float2 part[2];
+                uint32_t p[32];
+#pragma unroll 1
+                for (int pass = 0;; ++pass) {
+                    const float2 less = twice(top == -INFINITY ? 0.f : -top * c);         // or the row has seen no finite score
+                    part[0] = part[1] = twice(0.f);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        const uint32_t* from = &s[e / 16][2 * (e % 16)];
+                        const float2 f = fma2(make_float2(__uint_as_float(from[0]), __uint_as_float(from[1])), cc, less);
+                        const float2 y = make_float2(exp2_approx(f.x), exp2_approx(f.y));
+                        part[e & 1] = add2(part[e & 1], y);
+                        p[e] = round_bf16x2(y.x, y.y);
+                    }
+                    if (g == 0 || pass > 0) break;
+                    const float seen = fmaxf(max_of(s[0], top), max_of(s[1], top));
+                    if (!__any_sync(0xffffffffu, (seen - top) * c > AF_RISE)) break;
+                    // O is at rest once the last product handed over has been added to it
+                    ok = warp_wait(&s_added[x], total - 1 & 1u, abort_flag);
+                    if (!ok) break;
+                    ptx::tc_fence_after_sync();
                     const float keep = seen == top ? 1.f : exp2_approx((top - seen) * c);
                     top = seen;
                     sum *= keep;
@@ -512,40 +538,13 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
                         ptx::tmem_st_32x8(t_o + i, o);
                     }
                 }
-                const float less = top == -INFINITY ? 0.f : -top * c;         // a row that has seen no finite score
-                float2 part[2] = {twice(0.f), twice(0.f)};
-                const float2 cc = twice(c), ll = twice(less);
-                // The scores are read a second time, by halves: the loop's code stays small, and no register holds what the other half needs.
-#pragma unroll 1
-                for (int half = 1; half >= 0; --half) {
-                    uint32_t s[2][32];
-                    ptx::tmem_ld_32x32(t_s + 64 * half, s[0]);
-                    ptx::tmem_ld_32x32(t_s + 64 * half + 32, s[1]);
-                    ptx::tmem_ld_wait();
-                    ptx::tmem_ld_tie(s[0]);
-                    ptx::tmem_ld_tie(s[1]);
-                    if (masked) {
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) mask_behind(s[i], limit - 64 * half - 32 * i, 0xFF800000u);
-                    }
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        uint32_t p[16];
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const float2 f = fma2(make_float2(__uint_as_float(s[i][2 * e]), __uint_as_float(s[i][2 * e + 1])), cc, ll);
-                            const float2 y = make_float2(exp2_approx(f.x), exp2_approx(f.y));
-                            part[e & 1] = add2(part[e & 1], y);
-                            p[e] = round_bf16x2(y.x, y.y);
-                        }
-                        ptx::tmem_st_32x16(t_s + 64 * half + 16 * i, p);
-                    }
-                    ptx::tmem_st_wait();
-                    ptx::tc_fence_before_sync();
-                    __syncwarp();
-                    if (lane == 0) ptx::mbar_arrive(&s_probs[x][half]);
-                }
+                if (!ok) break;
+                ptx::tmem_st_32x32(t_g, p);
                 sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
+                ptx::tmem_st_wait();
+                ptx::tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&s_probs[x][half]);
             }
             if (!ok) break;
             if (a.lse && me < t.rows) a.lse[a.row_number(t, item.head) + me] = me < t.len ? fmaf(top, a.scale, logf(sum)) : -INFINITY;
