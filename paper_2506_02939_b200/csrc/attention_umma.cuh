@@ -412,9 +412,11 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
 #pragma unroll 1
                 for (int i = -2; i < mine; ++i) {
                     const int half = i & 1, next = i + 2;
+                    // what is there long before is waited for first, so that nothing stands between P's arrival and the products
+                    const uint32_t v_tile = base + (i | 1), v_slot = v_tile % Plan::SLOTS, k_tile = base + (next & ~1), k_slot = k_tile % Plan::SLOTS;
+                    if (next < mine && !half && !(ok = wait(s_full[k_slot], k_tile / Plan::SLOTS))) break;
                     if (i >= 0) {
-                        const uint32_t tile = base + (i | 1), slot = tile % Plan::SLOTS;
-                        if (!(ok = wait(s_full[slot], tile / Plan::SLOTS))) break;
+                        if (!half && !(ok = wait(s_full[v_slot], v_tile / Plan::SLOTS))) break;
                         if (i == 0) {
                             if (!(ok = wait(s_free[x], f_phase))) break;
                             f_phase ^= 1u;
@@ -422,18 +424,16 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
                         if (!(ok = wait(s_probs[x][half], p_phase >> half))) break;
                         p_phase ^= 1u << half;
                         ptx::tc_fence_after_sync();
-                        au_weighted_half(t_o, t_s, ring_addr + slot * Plan::TILE_BYTES, half, idesc_o, i > 0);
+                        au_weighted_half(t_o, t_s, ring_addr + v_slot * Plan::TILE_BYTES, half, idesc_o, i > 0);
                         ptx::umma_commit(&s_added[x]);
-                        if (half || i == mine - 1) ptx::umma_commit(&s_empty[slot]);
+                        if (half || i == mine - 1) ptx::umma_commit(&s_empty[v_slot]);
                         if (i == mine - 1) ptx::umma_commit(&s_done[x]);
                     }
                     if (next < mine) {
-                        const uint32_t tile = base + (next & ~1), slot = tile % Plan::SLOTS;
-                        if (!(ok = wait(s_full[slot], tile / Plan::SLOTS))) break;
                         ptx::tc_fence_after_sync();
-                        au_scores<DP>(t_s + 64 * half, q_addr, ring_addr + slot * Plan::TILE_BYTES + half * 64 * 128, steps, idesc_s);
+                        au_scores<DP>(t_s + 64 * half, q_addr, ring_addr + k_slot * Plan::TILE_BYTES + half * 64 * 128, steps, idesc_s);
                         ptx::umma_commit(&s_scores[x][half]);
-                        if (half || next == mine - 1) ptx::umma_commit(&s_empty[slot]);
+                        if (half || next == mine - 1) ptx::umma_commit(&s_empty[k_slot]);
                         if (next == mine - 1) ptx::umma_commit(&s_qempty[x]);
                     }
                 }
@@ -503,18 +503,16 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
                     mask_behind(s[1], limit - 32, 0xFF800000u);
                 }
                 if (g == 0) top = fmaxf(max_of(s[0], top), max_of(s[1], top));
-                const float2 cc = twice(c);
                 float2 part[2];
                 uint32_t p[32];
 #pragma unroll 1
                 for (int pass = 0;; ++pass) {
-                    const float2 less = twice(top == -INFINITY ? 0.f : -top * c);         // or the row has seen no finite score
+                    const float less = top == -INFINITY ? 0.f : -top * c;         // or the row has seen no finite score
                     part[0] = part[1] = twice(0.f);
 #pragma unroll
                     for (int e = 0; e < 32; ++e) {
                         const uint32_t* from = &s[e / 16][2 * (e % 16)];
-                        const float2 f = fma2(make_float2(__uint_as_float(from[0]), __uint_as_float(from[1])), cc, less);
-                        const float2 y = make_float2(exp2_approx(f.x), exp2_approx(f.y));
+                        const float2 y = make_float2(exp2_approx(fmaf(__uint_as_float(from[0]), c, less)), exp2_approx(fmaf(__uint_as_float(from[1]), c, less)));
                         part[e & 1] = add2(part[e & 1], y);
                         p[e] = round_bf16x2(y.x, y.y);
                     }

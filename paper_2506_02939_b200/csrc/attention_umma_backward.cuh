@@ -61,10 +61,11 @@ __global__ void __launch_bounds__(AU_THREADS, 1)
 attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const __grid_constant__ AttentionMaps m, const __grid_constant__ AttentionOrder order,
                                   const int works) {
     using Plan = AttentionPlan<DP>;
+    constexpr int K_SLOTS = (Plan::SLOTS + 1) / 2, V_SLOTS = Plan::SLOTS / 2;      // K stays for two products: rings of their own
     extern __shared__ uint8_t smem_raw[];
     __shared__ ItemQueue s_queue;
     __shared__ uint64_t s_full[Plan::SLOTS], s_empty[Plan::SLOTS], s_ffull[2], s_fempty[2], s_scores[2], s_grads, s_read, s_ds[2], s_done, s_free, s_rows,
-        s_rows_free, s_tail;
+        s_rows_free, s_tail[2];
     __shared__ float s_less[AU_ROWS], s_delta[AU_ROWS];
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort;
@@ -86,7 +87,8 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
         ptx::mbar_init(&s_free, 4);
         ptx::mbar_init(&s_rows, 4);
         ptx::mbar_init(&s_rows_free, 8);
-        ptx::mbar_init(&s_tail, 1);
+        ptx::mbar_init(&s_tail[0], 1);
+        ptx::mbar_init(&s_tail[1], 1);
         s_abort = 0;
         ptx::fence_barrier_init();
         ptx::fence_proxy_async();
@@ -111,7 +113,8 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
         if (warp == AU_ITEMS_WARP) {
             ok = au_find_items<AU_ROWS>(s_queue, a.s, order, works, abort_flag);
         } else if (warp == AU_TMA_WARP) {
-            TileRing ring = {ring_tiles, s_full, s_empty, &s_tail, abort_flag, Plan::SLOTS, 0, 0, 0, 0, false};
+            TileRing keys = {ring_tiles, s_full, s_empty, &s_tail[0], abort_flag, K_SLOTS, 0, 0, 0, 0, false};
+            TileRing values = {ring_tiles + K_SLOTS * Plan::TILE_BYTES, s_full + K_SLOTS, s_empty + K_SLOTS, &s_tail[1], abort_flag, V_SLOTS, 0, 0, 0, 0, false};
             uint32_t f_phase = 0;
             while (reader.next(item, ok)) {
                 const Tile& t = item.t;
@@ -119,21 +122,24 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
                 const bool clear = t.first + t.len < a.s.seq;
                 for (int j = 0; j < n && ok; ++j) {
                     ok = (j > 0 || ab_load_fixed<DP>(fixed, &m.q, item, &s_ffull[0], &s_fempty[0], f_phase, abort_flag)) &&
-                         au_produce<DP>(ring, &m.k, t, hk, j * AU_ROWS, clear) &&
+                         au_produce<DP>(keys, &m.k, t, hk, j * AU_ROWS, clear) &&
                          (j > 0 || ab_load_fixed<DP>(fixed + Plan::TILE_BYTES, &m.d_o, item, &s_ffull[1], &s_fempty[1], f_phase, abort_flag)) &&
-                         au_produce<DP>(ring, &m.v, t, hk, j * AU_ROWS, clear);
+                         au_produce<DP>(values, &m.v, t, hk, j * AU_ROWS, clear);
                 }
                 if (!ok) break;
                 if (n > 0) f_phase ^= 1u;
             }
-            if (!ok) ab_drain(ring, s_ffull);
+            if (!ok) {
+                ab_drain(keys, s_ffull);
+                au_drain(values);
+            }
         } else if (warp == AU_MMA_WARP && ptx::elect_one()) {
             // S two steps ahead of dQ, whose dS takes the place of the scores it came from
             const uint32_t idesc_s = ptx::umma_idesc_bf16(AU_ROWS, AU_ROWS);
             const uint32_t idesc_g = ptx::umma_idesc_bf16(AU_ROWS, (uint32_t)((a.d + 15) / 16 * 16)) | (1u << 16);      // B MN-major
             const int steps = (a.d + 15) / 16;
             const uint32_t f_addr = ptx::smem_u32(fixed), ring_addr = ptx::smem_u32(ring_tiles);
-            uint32_t q_phase = 0, free_phase = 1, scored = 0, taken = 0;        // the next ring tile of each kind of product
+            uint32_t q_phase = 0, free_phase = 1, scored = 0, taken = 0;        // the next tile of each kind of product
             const auto wait = [&](uint64_t& bar, uint32_t parity) { return ptx::mbar_wait(&bar, parity & 1u, abort_flag); };
             StepReader<false> ahead = {reader};
             Step now = {}, one = {};
@@ -148,8 +154,7 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
                         if (!(ok = wait(s_free, free_phase))) break;
                         free_phase ^= 1u;
                     }
-                    const uint32_t slot = taken % Plan::SLOTS;
-                    taken += 2;
+                    const uint32_t slot = taken++ % K_SLOTS;
                     ptx::tc_fence_after_sync();
                     au_weighted(tmem + 384, buffer, ring_addr + slot * Plan::TILE_BYTES, idesc_g, !now.first);
                     ptx::umma_commit(&s_empty[slot]);
@@ -160,9 +165,9 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
                         if (!(ok = wait(s_ffull[0], q_phase))) break;
                         q_phase ^= 1u;
                     }
-                    const uint32_t slot = scored % Plan::SLOTS;
-                    if (!(ok = wait(s_full[slot], scored / Plan::SLOTS))) break;
-                    scored += 2;
+                    const uint32_t slot = scored % K_SLOTS;
+                    if (!(ok = wait(s_full[slot], scored / K_SLOTS))) break;
+                    ++scored;
                     ptx::tc_fence_after_sync();
                     au_scores<DP>(buffer, f_addr, ring_addr + slot * Plan::TILE_BYTES, steps, idesc_s);
                     ptx::umma_commit(&s_scores[step & 1]);
@@ -176,19 +181,19 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
             const uint32_t idesc_s = ptx::umma_idesc_bf16(AU_ROWS, AU_ROWS);
             const int steps = (a.d + 15) / 16;
             const uint32_t f_addr = ptx::smem_u32(fixed) + Plan::TILE_BYTES, ring_addr = ptx::smem_u32(ring_tiles);
-            uint32_t g_phase = 0, tile = 1;
+            uint32_t g_phase = 0;
             const auto wait = [&](uint64_t& bar, uint32_t parity) { return ptx::mbar_wait(&bar, parity & 1u, abort_flag); };
             StepReader<false> ahead = {reader};
 #pragma unroll 1
-            for (uint32_t step = 0; ok; ++step, tile += 2) {
+            for (uint32_t step = 0; ok; ++step) {
                 const Step now = ahead.next(a.causal, a.group, ok);
                 if (!ok || !now.any) break;
                 if (now.first) {
                     if (!(ok = wait(s_ffull[1], g_phase))) break;
                     g_phase ^= 1u;
                 }
-                const uint32_t slot = tile % Plan::SLOTS;
-                if (!(ok = wait(s_full[slot], tile / Plan::SLOTS) && wait(s_read, step + 1))) break;      // the first finds it free
+                const uint32_t slot = K_SLOTS + step % V_SLOTS;
+                if (!(ok = wait(s_full[slot], step / V_SLOTS) && wait(s_read, step + 1))) break;      // the first finds it free
                 ptx::tc_fence_after_sync();
                 au_scores<DP>(tmem + 256, f_addr, ring_addr + slot * Plan::TILE_BYTES, steps, idesc_s);
                 ptx::umma_commit(&s_grads);
@@ -278,7 +283,7 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
             ok = warp_wait(&s_rows, phase, abort_flag);
             if (!ok) break;
             phase ^= 1u;
-            const float2 cc = twice(c), ll = twice(s_less[row]), dd = twice(-s_delta[row]);
+            const float less = s_less[row], delta = s_delta[row];
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(&s_rows_free);
             for (int j = 0; j < n; ++j, ++step) {
@@ -297,9 +302,8 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
                     for (int e = 0; e < 32; e += 2) {
-                        const float2 f = fma2(make_float2(__uint_as_float(s[i][e]), __uint_as_float(s[i][e + 1])), cc, ll);
-                        s[i][e] = __float_as_uint(exp2_approx(f.x));
-                        s[i][e + 1] = __float_as_uint(exp2_approx(f.y));
+                        s[i][e] = __float_as_uint(exp2_approx(fmaf(__uint_as_float(s[i][e]), c, less)));
+                        s[i][e + 1] = __float_as_uint(exp2_approx(fmaf(__uint_as_float(s[i][e + 1]), c, less)));
                     }
                 if (__any_sync(0xffffffffu, limit < 63)) {
                     mask_behind(s[0], limit, 0u);
@@ -321,9 +325,8 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
                     }
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        const float2 x = mul2(make_float2(__uint_as_float(s[i][2 * e]), __uint_as_float(s[i][2 * e + 1])),
-                                              add2(make_float2(__uint_as_float(g[2 * e]), __uint_as_float(g[2 * e + 1])), dd));
-                        p[e] = round_bf16x2(x.x, x.y);
+                        p[e] = round_bf16x2(__uint_as_float(s[i][2 * e]) * (__uint_as_float(g[2 * e]) - delta),
+                                            __uint_as_float(s[i][2 * e + 1]) * (__uint_as_float(g[2 * e + 1]) - delta));
                     }
                     ptx::tmem_st_32x16(t_s + 16 * i, p);
                 }
@@ -525,7 +528,7 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
         const int half = warp >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = ((uint32_t)(warp & 3) * 32) << 16;
         const uint32_t t_s = tmem + half * 64 + lanes, t_g = t_s + 128;
-        const float2 cc = twice(a.scale * LOG2E);
+        const float c = a.scale * LOG2E;
         uint32_t phase = 0;        // one phase a tile for all barriers of the tile
         while (reader.next(item, ok)) {
             const int n = ab_query_tiles(item.t, a.causal, a.group, from, per);
@@ -544,12 +547,10 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
 #pragma unroll
                     for (int e = 0; e < 32; e += 4) {
                         const float4 less = *reinterpret_cast<const float4*>(s_less + half * 64 + 32 * u + e);
-                        const float2 f = fma2(make_float2(__uint_as_float(s[u][e]), __uint_as_float(s[u][e + 1])), cc, make_float2(less.x, less.y));
-                        const float2 g = fma2(make_float2(__uint_as_float(s[u][e + 2]), __uint_as_float(s[u][e + 3])), cc, make_float2(less.z, less.w));
-                        s[u][e] = __float_as_uint(exp2_approx(f.x));
-                        s[u][e + 1] = __float_as_uint(exp2_approx(f.y));
-                        s[u][e + 2] = __float_as_uint(exp2_approx(g.x));
-                        s[u][e + 3] = __float_as_uint(exp2_approx(g.y));
+                        s[u][e] = __float_as_uint(exp2_approx(fmaf(__uint_as_float(s[u][e]), c, less.x)));
+                        s[u][e + 1] = __float_as_uint(exp2_approx(fmaf(__uint_as_float(s[u][e + 1]), c, less.y)));
+                        s[u][e + 2] = __float_as_uint(exp2_approx(fmaf(__uint_as_float(s[u][e + 2]), c, less.z)));
+                        s[u][e + 3] = __float_as_uint(exp2_approx(fmaf(__uint_as_float(s[u][e + 3]), c, less.w)));
                     }
                 if (a.causal && j % per == 0) {      // the tile on the diagonal: queries before the key do not see it
                     const int first = row - half * 64;
@@ -581,12 +582,10 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
 #pragma unroll
                     for (int e = 0; e < 16; e += 2) {
                         const float4 d = *reinterpret_cast<const float4*>(s_delta + half * 64 + 32 * u + 2 * e);
-                        const float2 x = mul2(make_float2(__uint_as_float(s[u][2 * e]), __uint_as_float(s[u][2 * e + 1])),
-                                              add2(make_float2(__uint_as_float(g[2 * e]), __uint_as_float(g[2 * e + 1])), make_float2(d.x, d.y)));
-                        const float2 y = mul2(make_float2(__uint_as_float(s[u][2 * e + 2]), __uint_as_float(s[u][2 * e + 3])),
-                                              add2(make_float2(__uint_as_float(g[2 * e + 2]), __uint_as_float(g[2 * e + 3])), make_float2(d.z, d.w)));
-                        p[e] = round_bf16x2(x.x, x.y);
-                        p[e + 1] = round_bf16x2(y.x, y.y);
+                        p[e] = round_bf16x2(__uint_as_float(s[u][2 * e]) * (__uint_as_float(g[2 * e]) + d.x),
+                                            __uint_as_float(s[u][2 * e + 1]) * (__uint_as_float(g[2 * e + 1]) + d.y));
+                        p[e + 1] = round_bf16x2(__uint_as_float(s[u][2 * e + 2]) * (__uint_as_float(g[2 * e + 2]) + d.z),
+                                                __uint_as_float(s[u][2 * e + 3]) * (__uint_as_float(g[2 * e + 3]) + d.w));
                     }
                     // the second half's gradients are still to be read: dS stays inside what the first half left
                     ptx::tmem_st_32x16(t_g + 16 * u, p);
