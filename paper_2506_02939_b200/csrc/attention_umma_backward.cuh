@@ -218,6 +218,13 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
                 const int64_t number = a.row_number(t, item.head) + t.at + quarter;
                 const __nv_bfloat16 *o = a.o.at<__nv_bfloat16>(t.b, t.first + t.at + quarter, item.head) + piece * 8;
                 const __nv_bfloat16 *g = a.d_o.at<__nv_bfloat16>(t.b, t.first + t.at + quarter, item.head) + piece * 8;
+                if (lane < valid) {       // all rows are on their way to L2 before the first is waited for
+                    const __nv_bfloat16 *o_row = o - piece * 8 + lane * a.o.token, *g_row = g - piece * 8 + lane * a.d_o.token;
+                    for (int e = 0; e < a.d; e += 64) {
+                        asm volatile("prefetch.global.L2 [%0];" ::"l"(o_row + e));
+                        asm volatile("prefetch.global.L2 [%0];" ::"l"(g_row + e));
+                    }
+                }
                 const float less = lane < valid ? -a.lse_in[number + lane] * LOG2E : 0.f;
                 float delta = 0.f;
 #pragma unroll 1

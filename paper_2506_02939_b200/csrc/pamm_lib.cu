@@ -1117,8 +1117,10 @@ pamm_status pamm_dropout(const void* X, int64_t ldx, const void* R, int64_t ldr,
     }
     DropoutArgs a = {};
     a.x = X; a.r = R; a.y = Y; a.rows = b; a.n = n; a.ldx = ldx; a.ldr = ldr; a.ldy = ldy; a.total = b * n;
-    a.counter = counter; a.seed = seed; a.offset = offset;
-    a.threshold = (uint64_t)(p * 4294967296.0);
+    a.counter = counter; a.offset = offset;
+    dropout_keys(seed, a.keys);
+    a.none = p == 1.0;
+    a.threshold = a.none ? 0 : (uint32_t)(p * 4294967296.0);       // floor; below 2^32, p being the nearest double to 1 at most
     a.factor = p < 1.0 ? (float)(1.0 / (1.0 - p)) : 0.f;
     return dt == PAMM_F32 ? run_dropout<float>(a, (cudaStream_t)stream) : run_dropout<__nv_bfloat16>(a, (cudaStream_t)stream);
 }
