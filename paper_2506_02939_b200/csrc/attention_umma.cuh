@@ -74,14 +74,17 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volati
     return __all_sync(0xffffffffu, ptx::mbar_wait(bar, parity, abort_flag));
 }
 // The block's items, found ahead by one warp and read by all others (`readers` warps: each gives an entry back as soon as it has it in
-// registers).  An entry with rows < 0 is the end.
-constexpr int AU_ITEMS = 4;
+// registers).  An entry with rows < 0 is the end.  Every item has a block in the grid; a block that is through with its own takes over
+// the next one that has not started, so that no block is left with more than the others whatever the sequences' lengths are.
+constexpr int AU_ITEMS = 2;
 struct Item { Tile t; int head; };
 struct ItemQueue {
+    uint4 response;
     Item items[AU_ITEMS];
-    uint64_t full[AU_ITEMS], empty[AU_ITEMS];
+    uint64_t full[AU_ITEMS], empty[AU_ITEMS], answered;
     __device__ __forceinline__ void init(int readers) {
         for (int i = 0; i < AU_ITEMS; ++i) { ptx::mbar_init(&full[i], 1); ptx::mbar_init(&empty[i], readers); }
+        ptx::mbar_init(&answered, 1);
     }
 };
 struct ItemReader {
@@ -110,31 +113,38 @@ struct ItemReader {
 };
 // The warp that finds them.
 template <int SIZE>
-__device__ __forceinline__ bool au_find_items(ItemQueue& q, const Sequences& s, const AttentionOrder& order, int works, volatile int* abort_flag) {
-    uint32_t count = 0;
-    // there and back: the first block of a round is the last of the next, so that blocks get as much where items shrink along the order
-    // (the largest share of 2 x 8192 causal tokens of 8 key heads is 2% over the mean so, and 14% with equal rounds)
-    for (int64_t round = 0;; ++round) {
-        const bool end = round * gridDim.x >= works;
-        const int64_t w = round * gridDim.x + (round & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+__device__ __forceinline__ bool au_find_items(ItemQueue& q, const Sequences& s, const AttentionOrder& order, volatile int* abort_flag) {
+    uint32_t count = 0, phase = 0;
+    int w = (int)blockIdx.x;
+    while (true) {
         Item item;
         item.t.rows = -1;
-        if (!end) {
-            if (w >= works) continue;
+        if (w >= 0) {
             int number;
-            order.at((int)w, number, item.head);
+            order.at(w, number, item.head);
             item.t = find_tile<SIZE>(s, number);
-            if (!item.t.any) continue;
         }
-        const uint32_t slot = count % AU_ITEMS;
-        if (!warp_wait(&q.empty[slot], ((count / AU_ITEMS) & 1u) ^ 1u, abort_flag)) return false;
+        if (w < 0 || item.t.any) {
+            const uint32_t slot = count % AU_ITEMS;
+            if (!warp_wait(&q.empty[slot], ((count / AU_ITEMS) & 1u) ^ 1u, abort_flag)) return false;
+            if ((threadIdx.x & 31) == 0) {
+                q.items[slot] = item;
+                ptx::mbar_arrive(&q.full[slot]);
+            }
+            __syncwarp();
+            ++count;
+            if (w < 0) return true;
+        }
         if ((threadIdx.x & 31) == 0) {
-            q.items[slot] = item;
-            ptx::mbar_arrive(&q.full[slot]);
+            ptx::fence_proxy_async();          // the last answer has been read
+            ptx::mbar_arrive_expect_tx(&q.answered, 16);
+            ptx::take_next_block(&q.response, &q.answered);
         }
         __syncwarp();
-        ++count;
-        if (end) return true;
+        if (!warp_wait(&q.answered, phase, abort_flag)) return false;
+        phase ^= 1u;
+        w = ptx::taken_block(&q.response);
+        __syncwarp();
     }
 }
 // The producer's ring of tiles.  Called by the whole warp.
@@ -311,11 +321,10 @@ __device__ __forceinline__ void mask_behind(uint32_t (&s)[32], int limit, uint32
 
 template <int DP>
 __global__ void __launch_bounds__(AU_THREADS, 1)
-attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_constant__ AttentionMaps m, const __grid_constant__ AttentionOrder order,
-                         const int works) {
+attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_constant__ AttentionMaps m, const __grid_constant__ AttentionOrder order) {
     using Plan = AttentionPlan<DP>;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ ItemQueue s_queue;
+    __shared__ __align__(16) ItemQueue s_queue;
     __shared__ uint64_t s_full[Plan::SLOTS], s_empty[Plan::SLOTS], s_qfull[2], s_qempty[2], s_scores[2][2], s_probs[2][2], s_added[2], s_done[2], s_sums[2], s_free[2], s_tail;
     __shared__ float s_sum[2][AU_ROWS];
     __shared__ uint32_t s_tmem;
@@ -361,7 +370,7 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
     if (warp >= AU_TMA_WARP) {
         ptx::registers_down<AU_OTHER_REGS>();
         if (warp == AU_ITEMS_WARP) {
-            ok = au_find_items<AF_QUERIES>(s_queue, a.s, order, works, abort_flag);
+            ok = au_find_items<AF_QUERIES>(s_queue, a.s, order, abort_flag);
         } else if (warp == AU_TMA_WARP) {
             TileRing ring = {ring_tiles, s_full, s_empty, &s_tail, abort_flag, Plan::SLOTS, 0, 0, 0, 0, false};
             uint32_t q_phase[2] = {0, 0};

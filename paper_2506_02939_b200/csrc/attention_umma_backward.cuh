@@ -58,12 +58,11 @@ __device__ __forceinline__ void ab_drain(const TileRing& ring, uint64_t* full) {
 // Rows of queries: dQ and delta.  Tensor memory: two buffers of S (dS takes their place), dP, dQ.
 template <int DP>
 __global__ void __launch_bounds__(AU_THREADS, 1)
-attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const __grid_constant__ AttentionMaps m, const __grid_constant__ AttentionOrder order,
-                                  const int works) {
+attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const __grid_constant__ AttentionMaps m, const __grid_constant__ AttentionOrder order) {
     using Plan = AttentionPlan<DP>;
     constexpr int K_SLOTS = (Plan::SLOTS + 1) / 2, V_SLOTS = Plan::SLOTS / 2;      // K stays for two products: rings of their own
     extern __shared__ uint8_t smem_raw[];
-    __shared__ ItemQueue s_queue;
+    __shared__ __align__(16) ItemQueue s_queue;
     __shared__ uint64_t s_full[Plan::SLOTS], s_empty[Plan::SLOTS], s_ffull[2], s_fempty[2], s_scores[2], s_grads, s_read, s_ds[2], s_done, s_free, s_rows,
         s_rows_free, s_tail[2];
     __shared__ float s_less[AU_ROWS], s_delta[AU_ROWS];
@@ -111,7 +110,7 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
     if (warp >= AU_TMA_WARP) {
         ptx::registers_down<AU_OTHER_REGS>();
         if (warp == AU_ITEMS_WARP) {
-            ok = au_find_items<AU_ROWS>(s_queue, a.s, order, works, abort_flag);
+            ok = au_find_items<AU_ROWS>(s_queue, a.s, order, abort_flag);
         } else if (warp == AU_TMA_WARP) {
             TileRing keys = {ring_tiles, s_full, s_empty, &s_tail[0], abort_flag, K_SLOTS, 0, 0, 0, 0, false};
             TileRing values = {ring_tiles + K_SLOTS * Plan::TILE_BYTES, s_full + K_SLOTS, s_empty + K_SLOTS, &s_tail[1], abort_flag, V_SLOTS, 0, 0, 0, 0, false};
@@ -359,11 +358,10 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
 // queries, which are its columns, are brought to shared memory by a warp of their own, the next tile's as soon as the last use is over.
 template <int DP>
 __global__ void __launch_bounds__(AU_THREADS, 1)
-attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __grid_constant__ AttentionMaps m, const __grid_constant__ AttentionOrder order,
-                               const int works) {
+attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __grid_constant__ AttentionMaps m, const __grid_constant__ AttentionOrder order) {
     using Plan = AttentionPlan<DP>;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ ItemQueue s_queue;
+    __shared__ __align__(16) ItemQueue s_queue;
     __shared__ uint64_t s_full[Plan::SLOTS], s_empty[Plan::SLOTS], s_ffull[2], s_fempty[2], s_scores[2], s_weights[2], s_done[2], s_free[2], s_stats[2],
         s_tail;      // [0]: S, P, dV, log-sums; [1]: dP, dS, dK, deltas
     __shared__ __align__(16) float s_less[AU_ROWS], s_delta[AU_ROWS];
@@ -408,7 +406,7 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
     if (warp >= AU_TMA_WARP) {
         ptx::registers_down<AU_OTHER_REGS>();
         if (warp == AU_ITEMS_WARP) {
-            ok = au_find_items<AU_ROWS>(s_queue, a.s, order, works, abort_flag);
+            ok = au_find_items<AU_ROWS>(s_queue, a.s, order, abort_flag);
         } else if (warp == AU_TMA_WARP) {
             TileRing ring = {ring_tiles, s_full, s_empty, &s_tail, abort_flag, Plan::SLOTS, 0, 0, 0, 0, false};
             uint32_t f_phase = 0;

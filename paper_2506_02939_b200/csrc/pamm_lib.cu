@@ -984,9 +984,8 @@ pamm_status launch_attention_forward(AttentionArgs a, const AttentionMaps& m, cu
     using Plan = AttentionPlan<DP>;
     if (!ensure_dynamic_smem((const void*)attention_forward_kernel<DP>, Plan::SMEM)) return PAMM_ERR_CUDA;
     a.s.items = tiles_of(a.s, AF_QUERIES);
-    const int works = a.s.items * a.heads, blocks = std::min(works, sm_count());
-    launch(attention_forward_kernel<DP>, dim3((unsigned)blocks), dim3(AU_THREADS), Plan::SMEM, st, true, a, m,
-           attention_order(a.s, a.heads, AF_QUERIES, blocks, a.causal), works);
+    launch(attention_forward_kernel<DP>, dim3((unsigned)(a.s.items * a.heads)), dim3(AU_THREADS), Plan::SMEM, st, true, a, m,
+           attention_order(a.s, a.heads, AF_QUERIES, sm_count(), a.causal));
     return launch_result("attention_forward_kernel launch");
 }
 
@@ -997,12 +996,11 @@ pamm_status launch_attention_backward(AttentionArgs a, const AttentionMaps& m, c
         !ensure_dynamic_smem((const void*)attention_keys_backward_kernel<DP>, Plan::SMEM))
         return PAMM_ERR_CUDA;
     a.s.items = tiles_of(a.s, AU_ROWS);
-    const int kv = a.heads / a.group, rows = a.s.items * a.heads, keys = a.s.items * kv, sms = sm_count();
-    const int row_blocks = std::min(rows, sms), key_blocks = std::min(keys, sms);
-    launch(attention_queries_backward_kernel<DP>, dim3((unsigned)row_blocks), dim3(AU_THREADS), Plan::SMEM, st, true, a, m,
-           attention_order(a.s, a.heads, AU_ROWS, row_blocks, a.causal), rows);
-    launch(attention_keys_backward_kernel<DP>, dim3((unsigned)key_blocks), dim3(AU_THREADS), Plan::SMEM, st, true, a, m,
-           attention_order(a.s, kv, AU_ROWS, key_blocks, false), keys);
+    const int kv = a.heads / a.group;
+    launch(attention_queries_backward_kernel<DP>, dim3((unsigned)(a.s.items * a.heads)), dim3(AU_THREADS), Plan::SMEM, st, true, a, m,
+           attention_order(a.s, a.heads, AU_ROWS, sm_count(), a.causal));
+    launch(attention_keys_backward_kernel<DP>, dim3((unsigned)(a.s.items * kv)), dim3(AU_THREADS), Plan::SMEM, st, true, a, m,
+           attention_order(a.s, kv, AU_ROWS, sm_count(), false));
     return launch_result("attention_keys_backward_kernel launch");
 }
 

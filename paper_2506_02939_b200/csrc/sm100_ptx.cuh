@@ -161,6 +161,26 @@ __device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.
 template <int N>
 __device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 
+// Asks for the grid's next block that has not started, which then never starts: its work is this block's.  The answer, 16 bytes at
+// `response`, is counted on `bar`.  After an answer without a block there are no more.  One thread.
+__device__ __forceinline__ void take_next_block(void* response, uint64_t* bar) {
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];"
+                 ::"r"(smem_u32(response)), "r"(smem_u32(bar)) : "memory");
+}
+// Its number along x, or -1.
+__device__ __forceinline__ int taken_block(const void* response) {
+    uint32_t x, any;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b128 r;\n\t"
+        "ld.shared.b128 r, [%2];\n\t"
+        "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
+        "selp.u32 %1, 1, 0, p;\n\t"
+        "mov.u32 %0, 0;\n\t"
+        "@p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%0, _, _, _}, r;\n\t}"
+        : "=r"(x), "=r"(any) : "r"(smem_u32(response)) : "memory");
+    return any ? (int)x : -1;
+}
+
 // ---- tensor memory ----------------------------------------------------------------
 // Warp-wide.  ncols: power of two in [32, 512].  The base address lands in *dst_smem.
 __device__ __forceinline__ void tmem_alloc(uint32_t* dst_smem, uint32_t ncols) {
