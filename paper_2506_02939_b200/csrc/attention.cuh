@@ -10,6 +10,8 @@
 #include "pamm_common.cuh"
 #include "row_io.cuh"
 
+#include <algorithm>
+
 namespace pamm {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
@@ -91,6 +93,40 @@ __device__ __forceinline__ Tile find_tile(const Sequences& s, int item) {
     return t;
 }
 
+// The order of work.  Whole and padded batches: (batch, head) pairs in groups of about one per block, in a group the tiles of every pair
+// from the last to the first -- the long ones first where causal -- so that a pair's keys are read again while they
+// are in L2.  Packed sequences: by tile, all heads of a tile one after another.
+struct AttentionOrder {
+    int pairs, tiles, groups, per_group, owners;       // owners: heads of the rows that a tile owns
+    bool packed, descending;
+    __device__ __forceinline__ void at(int w, int& item, int& head) const {
+        if (packed) {
+            item = w / owners;
+            head = w - item * owners;
+            return;
+        }
+        const int full = per_group * tiles;
+        int g = w / full;
+        if (g > groups - 1) g = groups - 1;
+        const int members = g == groups - 1 ? pairs - g * per_group : per_group;
+        const int local = w - g * full, level = local / members, pair = g * per_group + (local - level * members);
+        const int b = pair / owners;
+        head = pair - b * owners;
+        item = b * tiles + (descending ? tiles - 1 - level : level);
+    }
+};
+inline AttentionOrder attention_order(const Sequences& s, int owners, int tile, int blocks, bool descending) {
+    AttentionOrder o = {};
+    o.owners = owners;
+    o.packed = s.starts != nullptr;
+    o.descending = descending;
+    o.tiles = (int)((s.seq + tile - 1) / tile);
+    o.pairs = s.batch * owners;
+    o.groups = o.packed ? 1 : std::max(1, (int)(((int64_t)o.pairs + blocks / 2) / blocks));
+    o.per_group = o.groups > 1 ? blocks : o.pairs;
+    return o;
+}
+
 struct AttentionArgs {
     HeadsView q, k, v, o, d_o, dq, dk, dv;
     const float* lse_in;
@@ -110,29 +146,60 @@ constexpr int AG_TILE = 64, AG_THREADS = 256, AG_P_LD = AG_TILE + 4;
 
 template <int DP>
 __host__ __device__ constexpr size_t ag_smem(int tiles) { return ((size_t)tiles * AG_TILE * (DP + 4) + AG_TILE * AG_P_LD + 2 * AG_TILE) * 4; }
+// Whether the two streamed tiles have a place each, so that the one is on its way while the other is worked on.  Forward: with heads
+// of up to 64 two blocks an SM fit all the same.
+template <int DP, bool BACK>
+constexpr bool ag_split = BACK ? DP <= 128 : DP <= 64;
+template <int DP, bool BACK>
+constexpr int ag_tiles = (BACK ? 3 : 2) + (ag_split<DP, BACK> ? 1 : 0);
 
-// Rows `at` .. of the sequence into a tile: rows from `valid` on and columns from d on are zero.
+// 16 bytes to shared memory without passing through registers, or zeros.
+__device__ __forceinline__ void ag_copy16(float* dst, const void* src, bool any) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "r"(any ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void ag_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void ag_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Rows `at` .. of the sequence into a tile, as one group of copies: rows from `valid` on and columns from d on are zero.  fp32 in vectors
+// goes asynchronously; other forms are there when the call returns.
 template <typename T, int DP>
 __device__ __forceinline__ void ag_load(float* tile, const HeadsView& x, const Tile& t, int64_t head, int at, int valid, int d, bool vectors) {
-    constexpr int V = 16 / (int)sizeof(T), LD = DP + 4;
+    constexpr int V = 16 / (int)sizeof(T), LD = DP + 4, PER = DP / V, EACH = AG_TILE * PER / AG_THREADS;
     const T* base = x.at<T>(t.b, t.first + at, head);
     if (vectors) {
-        constexpr int PER = DP / V;
-        for (int i = threadIdx.x; i < AG_TILE * PER; i += AG_THREADS) {
-            const int row = i / PER, col = (i % PER) * V;
-            float f[V];
+        if constexpr (sizeof(T) == 4) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) f[e] = 0.f;
-            if (at + row < valid && col < d) Piece<T, V>::unpack(Piece<T, V>::load(base + row * x.token + col), f);
+            for (int i = 0; i < EACH; ++i) {
+                const int at_i = threadIdx.x + i * AG_THREADS, row = at_i / PER, col = (at_i % PER) * V;
+                const bool any = at + row < valid && col < d;
+                ag_copy16(tile + row * LD + col, any ? base + row * x.token + col : base, any);
+            }
+        } else {
+            typename Piece<T, V>::Raw raw[EACH];       // all of a thread's loads are in flight before the first is waited for
 #pragma unroll
-            for (int e = 0; e < V; e += 4) *reinterpret_cast<float4*>(tile + row * LD + col + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+            for (int i = 0; i < EACH; ++i) {
+                const int at_i = threadIdx.x + i * AG_THREADS, row = at_i / PER, col = (at_i % PER) * V;
+                raw[i] = Piece<T, V>::zero();
+                if (at + row < valid && col < d) raw[i] = Piece<T, V>::load(base + row * x.token + col);
+            }
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) {
+                const int at_i = threadIdx.x + i * AG_THREADS, row = at_i / PER, col = (at_i % PER) * V;
+                float f[V];
+                Piece<T, V>::unpack(raw[i], f);
+#pragma unroll
+                for (int e = 0; e < V; e += 4) *reinterpret_cast<float4*>(tile + row * LD + col + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+            }
         }
     } else {
+#pragma unroll 4
         for (int i = threadIdx.x; i < AG_TILE * DP; i += AG_THREADS) {
             const int row = i / DP, col = i % DP;
             tile[row * LD + col] = at + row < valid && col < d ? to_float(base[row * x.token + col]) : 0.f;
         }
     }
+    ag_commit();
 }
 
 // c[r][j] = row (4 ty + r) of A times row (tx + 16 j) of B
@@ -211,16 +278,20 @@ __device__ __forceinline__ void ag_store(const HeadsView& y, const Tile& t, int6
     }
 }
 
-// One block: 64 rows of one query head, over all tiles of keys with the running maximum and sum of the softmax.
+// One block: 64 rows of one query head, over all tiles of keys with the running maximum and sum of the softmax.  Rows of P are written
+// and read by the same half of a warp.
 template <typename T, int DP>
 __global__ void __launch_bounds__(AG_THREADS, DP <= 128 ? 2 : 1)
-attention_forward_generic_kernel(const __grid_constant__ AttentionArgs a) {
+attention_forward_generic_kernel(const __grid_constant__ AttentionArgs a, const __grid_constant__ AttentionOrder order) {
+    constexpr bool SPLIT = ag_split<DP, false>;
+    constexpr int TILE = AG_TILE * (DP + 4);
     extern __shared__ __align__(16) float ag_shared[];
-    float *Q = ag_shared, *X = Q + AG_TILE * (DP + 4), *P = X + AG_TILE * (DP + 4);
+    float *Q = ag_shared, *K = Q + TILE, *V = SPLIT ? K + TILE : K, *P = V + TILE;
     grid_dependency_wait();
     grid_launch_dependents();
-    const int h = (int)(blockIdx.x / a.s.items);
-    const Tile t = find_tile<AG_TILE>(a.s, (int)(blockIdx.x - (unsigned)h * a.s.items));
+    int h, item;
+    order.at((int)blockIdx.x, item, h);
+    const Tile t = find_tile<AG_TILE>(a.s, item);
     if (!t.any) return;
     const int tx = threadIdx.x % 16, row0 = t.at + (threadIdx.x / 16) * 4;
     const float c = a.scale * LOG2E;
@@ -232,16 +303,24 @@ attention_forward_generic_kernel(const __grid_constant__ AttentionArgs a) {
 #pragma unroll
         for (int e = 0; e < DP / 16; ++e) acc[r][e] = 0.f;
     }
-    if (t.at < t.len) ag_load<T, DP>(Q, a.q, t, h, t.at, t.len, a.d, a.vectors);
     const int end = t.at < t.len ? (a.causal ? min(t.len, t.at + AG_TILE) : t.len) : 0;
+    const auto load = [&](float* to, const HeadsView& x, int k0) { ag_load<T, DP>(to, x, t, h / a.group, k0, t.len, a.d, a.vectors); };
+    if (end > 0) {
+        ag_load<T, DP>(Q, a.q, t, h, t.at, t.len, a.d, a.vectors);
+        load(K, a.k, 0);
+        if (SPLIT) load(V, a.v, 0);
+    }
     for (int k0 = 0; k0 < end; k0 += AG_TILE) {
-        __syncthreads();
-        ag_load<T, DP>(X, a.k, t, h / a.group, k0, t.len, a.d, a.vectors);
+        const bool more = k0 + AG_TILE < end;
+        if (SPLIT) ag_wait<1>();
+        else ag_wait<0>();
         __syncthreads();
         float s[4][4];
-        ag_scores<DP>(Q, X, a.d, s);
+        ag_scores<DP>(Q, K, a.d, s);
         __syncthreads();
-        ag_load<T, DP>(X, a.v, t, h / a.group, k0, t.len, a.d, a.vectors);
+        if (!SPLIT) load(V, a.v, k0);
+        else if (more) load(K, a.k, k0 + AG_TILE);
+        else ag_commit();                                       // as many groups, so that V's is the last but one
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int last = a.causal ? min(row0 + r, t.len - 1) : t.len - 1;
@@ -266,8 +345,15 @@ attention_forward_generic_kernel(const __grid_constant__ AttentionArgs a) {
             top[r] = m;
         }
         ag_store_scores(P, s);
+        if (SPLIT) ag_wait<1>();
+        else ag_wait<0>();
         __syncthreads();
-        ag_accumulate<DP>(P, X, min(AG_TILE, (end - k0 + 3) & ~3), acc);
+        ag_accumulate<DP>(P, V, min(AG_TILE, (end - k0 + 3) & ~3), acc);
+        if (more) {
+            __syncthreads();
+            if (SPLIT) load(V, a.v, k0 + AG_TILE);
+            else load(K, a.k, k0 + AG_TILE);
+        }
     }
     float factor[4];
 #pragma unroll
@@ -285,15 +371,17 @@ attention_forward_generic_kernel(const __grid_constant__ AttentionArgs a) {
 // One block: 64 rows of the queries (KEYS false: A0 = Q, A1 = dO against X0 = K, X1 = V; dq, and delta on the way) or of the
 // keys (A0 = K, A1 = V against X0 = Q, X1 = dO of every head of the group; dk and dv).
 template <typename T, int DP, bool KEYS>
-__global__ void __launch_bounds__(AG_THREADS, 1)
-attention_backward_generic_kernel(const __grid_constant__ AttentionArgs a) {
+__global__ void __launch_bounds__(AG_THREADS, DP <= 64 ? 2 : 1)
+attention_backward_generic_kernel(const __grid_constant__ AttentionArgs a, const __grid_constant__ AttentionOrder order) {
+    constexpr bool SPLIT = ag_split<DP, true>;
     constexpr int TILE = AG_TILE * (DP + 4);
     extern __shared__ __align__(16) float ag_shared[];
-    float *A0 = ag_shared, *A1 = A0 + TILE, *X = A1 + TILE, *P = X + TILE, *lse = P + AG_TILE * AG_P_LD, *delta = lse + AG_TILE;
+    float *A0 = ag_shared, *A1 = A0 + TILE, *X0 = A1 + TILE, *X1 = SPLIT ? X0 + TILE : X0, *P = X1 + TILE, *lse = P + AG_TILE * AG_P_LD, *delta = lse + AG_TILE;
     grid_dependency_wait();
     grid_launch_dependents();
-    const int owner = (int)(blockIdx.x / a.s.items);          // query head or key head
-    const Tile t = find_tile<AG_TILE>(a.s, (int)(blockIdx.x - (unsigned)owner * a.s.items));
+    int owner, item;                                          // query head or key head
+    order.at((int)blockIdx.x, item, owner);
+    const Tile t = find_tile<AG_TILE>(a.s, item);
     if (!t.any) return;
     const int tx = threadIdx.x % 16, ty = threadIdx.x / 16, row0 = t.at + ty * 4;
     const float c = a.scale * LOG2E;
@@ -306,12 +394,33 @@ attention_backward_generic_kernel(const __grid_constant__ AttentionArgs a) {
             if (KEYS) acc1[r][KEYS ? e : 0] = 0.f;
         }
     }
-    if (t.at < t.len) {
+    // step i of n: tile i % per of the streamed rows, of head i / per of those that share the keys
+    const int begin = KEYS && a.causal ? t.at : 0;
+    const int end = t.at >= t.len ? begin : !KEYS && a.causal ? min(t.len, t.at + AG_TILE) : t.len;
+    const int per = (end - begin + AG_TILE - 1) / AG_TILE, n = per * (KEYS ? a.group : 1);
+    const auto head_of = [&](int i) { return KEYS ? owner * a.group + i / per : owner / a.group; };
+    const auto at_of = [&](int i) { return begin + i % per * AG_TILE; };
+    const auto load0 = [&](int i) { ag_load<T, DP>(X0, KEYS ? a.q : a.k, t, head_of(i), at_of(i), t.len, a.d, a.vectors); };
+    const auto load1 = [&](int i) { ag_load<T, DP>(X1, KEYS ? a.d_o : a.v, t, head_of(i), at_of(i), t.len, a.d, a.vectors); };
+    float next_lse = 0.f, next_delta = 0.f;                   // of the next step's columns, on their way
+    const auto numbers = [&](int i) {
+        const int row = at_of(i) + (int)threadIdx.x;
+        if (!KEYS || threadIdx.x >= AG_TILE) return;
+        const int64_t number = a.row_number(t, head_of(i)) + row;
+        next_lse = row < t.len ? a.lse_in[number] * LOG2E : 0.f;
+        next_delta = row < t.len ? a.delta[number] : 0.f;
+    };
+    if (n > 0) {
         ag_load<T, DP>(A0, KEYS ? a.k : a.q, t, owner, t.at, t.len, a.d, a.vectors);
         ag_load<T, DP>(A1, KEYS ? a.v : a.d_o, t, owner, t.at, t.len, a.d, a.vectors);
+        numbers(0);
+        load0(0);
+        if (SPLIT) load1(0);
     }
     if (!KEYS) {
         const int64_t number = a.row_number(t, owner);
+        if (SPLIT) ag_wait<2>();
+        else ag_wait<1>();
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
@@ -327,48 +436,59 @@ attention_backward_generic_kernel(const __grid_constant__ AttentionArgs a) {
             if (tx == 0 && row0 + r < t.rows) a.delta[number + row0 + r] = sum;
         }
     }
-    const int begin = KEYS && a.causal ? t.at : 0;
-    const int end = t.at >= t.len ? begin : !KEYS && a.causal ? min(t.len, t.at + AG_TILE) : t.len;
-    const int others = KEYS ? a.group : 1;
-    for (int g = 0; g < others; ++g) {
-        const int h0 = KEYS ? owner * a.group + g : owner / a.group;
-        for (int x0 = begin; x0 < end; x0 += AG_TILE) {
-            __syncthreads();
-            ag_load<T, DP>(X, KEYS ? a.q : a.k, t, h0, x0, t.len, a.d, a.vectors);
-            if (KEYS && threadIdx.x < AG_TILE) {
-                const int64_t number = a.row_number(t, h0) + x0 + threadIdx.x;
-                const bool valid = x0 + (int)threadIdx.x < t.len;
-                lse[threadIdx.x] = valid ? a.lse_in[number] * LOG2E : 0.f;
-                delta[threadIdx.x] = valid ? a.delta[number] : 0.f;
+    for (int i = 0; i < n; ++i) {
+        const bool more = i + 1 < n;
+        const int x0 = at_of(i);
+        if (KEYS && threadIdx.x < AG_TILE) {
+            lse[threadIdx.x] = next_lse;
+            delta[threadIdx.x] = next_delta;
+        }
+        if (SPLIT) ag_wait<1>();
+        else ag_wait<0>();
+        __syncthreads();
+        if (more) numbers(i + 1);
+        float p[4][4], dp[4][4];
+        ag_scores<DP>(A0, X0, a.d, p);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int row = row0 + r, col = x0 + tx + 16 * j;
+                const bool sees = col < t.len && (!a.causal || (KEYS ? col >= row : col <= row));
+                p[r][j] = sees ? exp2f(fmaf(p[r][j], c, -(KEYS ? lse[tx + 16 * j] : row_lse[r]))) : 0.f;
             }
+        if (!SPLIT) {
             __syncthreads();
-            float p[4][4], dp[4][4];
-            ag_scores<DP>(A0, X, a.d, p);
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int row = row0 + r, col = x0 + tx + 16 * j;
-                    const bool sees = col < t.len && (!a.causal || (KEYS ? col >= row : col <= row));
-                    p[r][j] = sees ? exp2f(fmaf(p[r][j], c, -(KEYS ? lse[tx + 16 * j] : row_lse[r]))) : 0.f;
-                }
-            __syncthreads();
-            ag_load<T, DP>(X, KEYS ? a.d_o : a.v, t, h0, x0, t.len, a.d, a.vectors);
-            if (KEYS) ag_store_scores(P, p);
-            __syncthreads();
-            ag_scores<DP>(A1, X, a.d, dp);
-            const int used = min(AG_TILE, (end - x0 + 3) & ~3);
-            if constexpr (KEYS) ag_accumulate<DP>(P, X, used, acc1);
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)      // a masked place stays 0 whatever dp is there
-                    p[r][j] = p[r][j] == 0.f ? 0.f : p[r][j] * (dp[r][j] - (KEYS ? delta[tx + 16 * j] : row_delta[r]));
-            __syncthreads();
-            ag_load<T, DP>(X, KEYS ? a.q : a.k, t, h0, x0, t.len, a.d, a.vectors);
+            load1(i);
+        }
+        ag_wait<0>();
+        __syncthreads();
+        ag_scores<DP>(A1, X1, a.d, dp);
+        const int used = min(AG_TILE, (end - x0 + 3) & ~3);
+        if constexpr (KEYS) {
             ag_store_scores(P, p);
+            __syncwarp();
+            ag_accumulate<DP>(P, X1, used, acc1);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)      // a masked place stays 0 whatever dp is there
+                p[r][j] = p[r][j] == 0.f ? 0.f : p[r][j] * (dp[r][j] - (KEYS ? delta[tx + 16 * j] : row_delta[r]));
+        if (!SPLIT) {
             __syncthreads();
-            ag_accumulate<DP>(P, X, used, acc0);
+            load0(i);
+            ag_wait<0>();
+            __syncthreads();
+        }
+        __syncwarp();
+        ag_store_scores(P, p);
+        __syncwarp();
+        ag_accumulate<DP>(P, X0, used, acc0);
+        if (more) {
+            __syncthreads();
+            load0(i + 1);
+            if (SPLIT) load1(i + 1);
         }
     }
     const float factor[4] = {a.scale, a.scale, a.scale, a.scale}, one[4] = {1.f, 1.f, 1.f, 1.f};

@@ -22,40 +22,6 @@ constexpr int AU_THREADS = 512, AU_FINISH_WARP = 8, AU_TMA_WARP = 12, AU_MMA_WAR
 constexpr int AU_ROW_REGS = 168, AU_OTHER_REGS = 88;
 static_assert(256 * AU_ROW_REGS + 256 * AU_OTHER_REGS <= 65536, "what is taken has to have been given back");
 
-// The order of work.  Whole and padded batches: (batch, head) pairs in groups of about one per block, in a group the tiles of every pair
-// from the last to the first -- the long ones first where causal -- so that a pair's keys are read again while they
-// are in L2.  Packed sequences: by tile, all heads of a tile one after another.
-struct AttentionOrder {
-    int pairs, tiles, groups, per_group, owners;       // owners: heads of the rows that a tile owns
-    bool packed, descending;
-    __device__ __forceinline__ void at(int w, int& item, int& head) const {
-        if (packed) {
-            item = w / owners;
-            head = w - item * owners;
-            return;
-        }
-        const int full = per_group * tiles;
-        int g = w / full;
-        if (g > groups - 1) g = groups - 1;
-        const int members = g == groups - 1 ? pairs - g * per_group : per_group;
-        const int local = w - g * full, level = local / members, pair = g * per_group + (local - level * members);
-        const int b = pair / owners;
-        head = pair - b * owners;
-        item = b * tiles + (descending ? tiles - 1 - level : level);
-    }
-};
-inline AttentionOrder attention_order(const Sequences& s, int owners, int tile, int blocks, bool descending) {
-    AttentionOrder o = {};
-    o.owners = owners;
-    o.packed = s.starts != nullptr;
-    o.descending = descending;
-    o.tiles = (int)((s.seq + tile - 1) / tile);
-    o.pairs = s.batch * owners;
-    o.groups = o.packed ? 1 : std::max(1, (int)(((int64_t)o.pairs + blocks / 2) / blocks));
-    o.per_group = o.groups > 1 ? blocks : o.pairs;
-    return o;
-}
-
 __device__ __forceinline__ float exp2_approx(float x) {       // 2 units, results below 2^-126 are 0
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -955,21 +955,25 @@ Sequences sequences_of(const AttentionShape& g, const void* lengths, const void*
 
 template <typename T, int DP>
 pamm_status launch_attention_forward_generic(AttentionArgs a, cudaStream_t st) {
-    const size_t smem = ag_smem<DP>(2);
+    const size_t smem = ag_smem<DP>(ag_tiles<DP, false>);
     if (!ensure_dynamic_smem((const void*)attention_forward_generic_kernel<T, DP>, smem)) return PAMM_ERR_CUDA;
     a.s.items = tiles_of(a.s, AG_TILE);
-    launch(attention_forward_generic_kernel<T, DP>, dim3((unsigned)a.s.items * a.heads), dim3(AG_THREADS), smem, st, true, a);
+    launch(attention_forward_generic_kernel<T, DP>, dim3((unsigned)a.s.items * a.heads), dim3(AG_THREADS), smem, st, true, a,
+           attention_order(a.s, a.heads, AG_TILE, sm_count(), a.causal));
     return launch_result("attention_forward_generic_kernel launch");
 }
 template <typename T, int DP>
 pamm_status launch_attention_backward_generic(AttentionArgs a, cudaStream_t st) {
-    const size_t smem = ag_smem<DP>(3);
+    const size_t smem = ag_smem<DP>(ag_tiles<DP, true>);
     if (!ensure_dynamic_smem((const void*)attention_backward_generic_kernel<T, DP, false>, smem) ||
         !ensure_dynamic_smem((const void*)attention_backward_generic_kernel<T, DP, true>, smem))
         return PAMM_ERR_CUDA;
     a.s.items = tiles_of(a.s, AG_TILE);
-    launch(attention_backward_generic_kernel<T, DP, false>, dim3((unsigned)a.s.items * a.heads), dim3(AG_THREADS), smem, st, true, a);
-    launch(attention_backward_generic_kernel<T, DP, true>, dim3((unsigned)a.s.items * (a.heads / a.group)), dim3(AG_THREADS), smem, st, true, a);
+    const int kv = a.heads / a.group, sms = sm_count();
+    launch(attention_backward_generic_kernel<T, DP, false>, dim3((unsigned)a.s.items * a.heads), dim3(AG_THREADS), smem, st, true, a,
+           attention_order(a.s, a.heads, AG_TILE, sms, a.causal));
+    launch(attention_backward_generic_kernel<T, DP, true>, dim3((unsigned)a.s.items * kv), dim3(AG_THREADS), smem, st, true, a,
+           attention_order(a.s, kv, AG_TILE, sms, false));
     return launch_result("attention_backward_generic_kernel launch");
 }
 template <typename T>
