@@ -139,19 +139,19 @@ struct AttentionArgs {
 };
 
 // ---- kernels for every type, size and order ---------------------------------------------------------------------
-// Products in fp32 by fused multiply-adds: tiles of 64 x 64 scores, 16 a thread in 4 rows, whose operands come out of shared
+// Products in fp32 by fused multiply-adds: tiles of 32 x 64 scores, 16 a thread in 4 rows, whose operands come out of shared
 // memory as vectors along the head (rows 4 words past a multiple of 32 apart: no bank conflicts).  They serve fp32, heads
-// that are not multiples of 8 or wider than 128, and rows off the 16-byte grid.
-constexpr int AG_TILE = 64, AG_THREADS = 256, AG_P_LD = AG_TILE + 4;
+// that are not multiples of 8 or wider than 128, and rows off the 16-byte grid.  Bound by instructions and reads of shared memory.
+// (Blocks of 64 rows and 256 threads: 2 an SM, unevenly loaded in small batches; 8 x 256 tokens of 8 heads of 64 causal took
+// 33 us forward and 113 us backward.)
+constexpr int AG_ROWS = 32, AG_TILE = 64, AG_THREADS = 4 * AG_ROWS, AG_P_LD = AG_TILE + 4;       // owned rows, streamed rows
 
+// Whether the two streamed tiles have a place each, so that the one is on its way while the other is worked on.
 template <int DP>
-__host__ __device__ constexpr size_t ag_smem(int tiles) { return ((size_t)tiles * AG_TILE * (DP + 4) + AG_TILE * AG_P_LD + 2 * AG_TILE) * 4; }
-// Whether the two streamed tiles have a place each, so that the one is on its way while the other is worked on.  Forward: with heads
-// of up to 64 two blocks an SM fit all the same.
+constexpr bool ag_split = DP <= 128;
+// Owned tiles (Q, or two), streamed ones, P, and two numbers a streamed row.
 template <int DP, bool BACK>
-constexpr bool ag_split = BACK ? DP <= 128 : DP <= 64;
-template <int DP, bool BACK>
-constexpr int ag_tiles = (BACK ? 3 : 2) + (ag_split<DP, BACK> ? 1 : 0);
+constexpr size_t ag_smem = (size_t)(((BACK ? 2 : 1) * AG_ROWS + (ag_split<DP> ? 2 : 1) * AG_TILE) * (DP + 4) + AG_ROWS * AG_P_LD + 2 * AG_TILE) * 4;
 
 // 16 bytes to shared memory without passing through registers, or zeros.
 __device__ __forceinline__ void ag_copy16(float* dst, const void* src, bool any) {
@@ -163,9 +163,9 @@ __device__ __forceinline__ void ag_wait() { asm volatile("cp.async.wait_group %0
 
 // Rows `at` .. of the sequence into a tile, as one group of copies: rows from `valid` on and columns from d on are zero.  fp32 in vectors
 // goes asynchronously; other forms are there when the call returns.
-template <typename T, int DP>
+template <typename T, int DP, int ROWS>
 __device__ __forceinline__ void ag_load(float* tile, const HeadsView& x, const Tile& t, int64_t head, int at, int valid, int d, bool vectors) {
-    constexpr int V = 16 / (int)sizeof(T), LD = DP + 4, PER = DP / V, EACH = AG_TILE * PER / AG_THREADS;
+    constexpr int V = 16 / (int)sizeof(T), LD = DP + 4, PER = DP / V, EACH = ROWS * PER / AG_THREADS;
     const T* base = x.at<T>(t.b, t.first + at, head);
     if (vectors) {
         if constexpr (sizeof(T) == 4) {
@@ -194,7 +194,7 @@ __device__ __forceinline__ void ag_load(float* tile, const HeadsView& x, const T
         }
     } else {
 #pragma unroll 4
-        for (int i = threadIdx.x; i < AG_TILE * DP; i += AG_THREADS) {
+        for (int i = threadIdx.x; i < ROWS * DP; i += AG_THREADS) {
             const int row = i / DP, col = i % DP;
             tile[row * LD + col] = at + row < valid && col < d ? to_float(base[row * x.token + col]) : 0.f;
         }
@@ -278,20 +278,20 @@ __device__ __forceinline__ void ag_store(const HeadsView& y, const Tile& t, int6
     }
 }
 
-// One block: 64 rows of one query head, over all tiles of keys with the running maximum and sum of the softmax.  Rows of P are written
+// One block: AG_ROWS rows of one query head, over all tiles of keys with the running maximum and sum of the softmax.  Rows of P are written
 // and read by the same half of a warp.
 template <typename T, int DP>
-__global__ void __launch_bounds__(AG_THREADS, DP <= 128 ? 2 : 1)
+__global__ void __launch_bounds__(AG_THREADS, DP <= 64 ? 4 : 2)
 attention_forward_generic_kernel(const __grid_constant__ AttentionArgs a, const __grid_constant__ AttentionOrder order) {
-    constexpr bool SPLIT = ag_split<DP, false>;
-    constexpr int TILE = AG_TILE * (DP + 4);
+    constexpr bool SPLIT = ag_split<DP>;
+    constexpr int OWNED = AG_ROWS * (DP + 4), TILE = AG_TILE * (DP + 4);
     extern __shared__ __align__(16) float ag_shared[];
-    float *Q = ag_shared, *K = Q + TILE, *V = SPLIT ? K + TILE : K, *P = V + TILE;
+    float *Q = ag_shared, *K = Q + OWNED, *V = SPLIT ? K + TILE : K, *P = V + TILE;
     grid_dependency_wait();
     grid_launch_dependents();
     int h, item;
     order.at((int)blockIdx.x, item, h);
-    const Tile t = find_tile<AG_TILE>(a.s, item);
+    const Tile t = find_tile<AG_ROWS>(a.s, item);
     if (!t.any) return;
     const int tx = threadIdx.x % 16, row0 = t.at + (threadIdx.x / 16) * 4;
     const float c = a.scale * LOG2E;
@@ -303,10 +303,10 @@ attention_forward_generic_kernel(const __grid_constant__ AttentionArgs a, const 
 #pragma unroll
         for (int e = 0; e < DP / 16; ++e) acc[r][e] = 0.f;
     }
-    const int end = t.at < t.len ? (a.causal ? min(t.len, t.at + AG_TILE) : t.len) : 0;
-    const auto load = [&](float* to, const HeadsView& x, int k0) { ag_load<T, DP>(to, x, t, h / a.group, k0, t.len, a.d, a.vectors); };
+    const int end = t.at < t.len ? (a.causal ? min(t.len, t.at + AG_ROWS) : t.len) : 0;
+    const auto load = [&](float* to, const HeadsView& x, int k0) { ag_load<T, DP, AG_TILE>(to, x, t, h / a.group, k0, t.len, a.d, a.vectors); };
     if (end > 0) {
-        ag_load<T, DP>(Q, a.q, t, h, t.at, t.len, a.d, a.vectors);
+        ag_load<T, DP, AG_ROWS>(Q, a.q, t, h, t.at, t.len, a.d, a.vectors);
         load(K, a.k, 0);
         if (SPLIT) load(V, a.v, 0);
     }
@@ -368,20 +368,20 @@ attention_forward_generic_kernel(const __grid_constant__ AttentionArgs a, const 
     ag_store<T, DP>(a.o, t, h, a.d, acc, factor);
 }
 
-// One block: 64 rows of the queries (KEYS false: A0 = Q, A1 = dO against X0 = K, X1 = V; dq, and delta on the way) or of the
+// One block: AG_ROWS rows of the queries (KEYS false: A0 = Q, A1 = dO against X0 = K, X1 = V; dq, and delta on the way) or of the
 // keys (A0 = K, A1 = V against X0 = Q, X1 = dO of every head of the group; dk and dv).
 template <typename T, int DP, bool KEYS>
-__global__ void __launch_bounds__(AG_THREADS, DP <= 64 ? 2 : 1)
+__global__ void __launch_bounds__(AG_THREADS, DP <= 64 ? 3 : DP <= 128 ? 2 : 1)
 attention_backward_generic_kernel(const __grid_constant__ AttentionArgs a, const __grid_constant__ AttentionOrder order) {
-    constexpr bool SPLIT = ag_split<DP, true>;
-    constexpr int TILE = AG_TILE * (DP + 4);
+    constexpr bool SPLIT = ag_split<DP>;
+    constexpr int OWNED = AG_ROWS * (DP + 4), TILE = AG_TILE * (DP + 4);
     extern __shared__ __align__(16) float ag_shared[];
-    float *A0 = ag_shared, *A1 = A0 + TILE, *X0 = A1 + TILE, *X1 = SPLIT ? X0 + TILE : X0, *P = X1 + TILE, *lse = P + AG_TILE * AG_P_LD, *delta = lse + AG_TILE;
+    float *A0 = ag_shared, *A1 = A0 + OWNED, *X0 = A1 + OWNED, *X1 = SPLIT ? X0 + TILE : X0, *P = X1 + TILE, *lse = P + AG_ROWS * AG_P_LD, *delta = lse + AG_TILE;
     grid_dependency_wait();
     grid_launch_dependents();
     int owner, item;                                          // query head or key head
     order.at((int)blockIdx.x, item, owner);
-    const Tile t = find_tile<AG_TILE>(a.s, item);
+    const Tile t = find_tile<AG_ROWS>(a.s, item);
     if (!t.any) return;
     const int tx = threadIdx.x % 16, ty = threadIdx.x / 16, row0 = t.at + ty * 4;
     const float c = a.scale * LOG2E;
@@ -396,12 +396,12 @@ attention_backward_generic_kernel(const __grid_constant__ AttentionArgs a, const
     }
     // step i of n: tile i % per of the streamed rows, of head i / per of those that share the keys
     const int begin = KEYS && a.causal ? t.at : 0;
-    const int end = t.at >= t.len ? begin : !KEYS && a.causal ? min(t.len, t.at + AG_TILE) : t.len;
+    const int end = t.at >= t.len ? begin : !KEYS && a.causal ? min(t.len, t.at + AG_ROWS) : t.len;
     const int per = (end - begin + AG_TILE - 1) / AG_TILE, n = per * (KEYS ? a.group : 1);
     const auto head_of = [&](int i) { return KEYS ? owner * a.group + i / per : owner / a.group; };
     const auto at_of = [&](int i) { return begin + i % per * AG_TILE; };
-    const auto load0 = [&](int i) { ag_load<T, DP>(X0, KEYS ? a.q : a.k, t, head_of(i), at_of(i), t.len, a.d, a.vectors); };
-    const auto load1 = [&](int i) { ag_load<T, DP>(X1, KEYS ? a.d_o : a.v, t, head_of(i), at_of(i), t.len, a.d, a.vectors); };
+    const auto load0 = [&](int i) { ag_load<T, DP, AG_TILE>(X0, KEYS ? a.q : a.k, t, head_of(i), at_of(i), t.len, a.d, a.vectors); };
+    const auto load1 = [&](int i) { ag_load<T, DP, AG_TILE>(X1, KEYS ? a.d_o : a.v, t, head_of(i), at_of(i), t.len, a.d, a.vectors); };
     float next_lse = 0.f, next_delta = 0.f;                   // of the next step's columns, on their way
     const auto numbers = [&](int i) {
         const int row = at_of(i) + (int)threadIdx.x;
@@ -411,8 +411,8 @@ attention_backward_generic_kernel(const __grid_constant__ AttentionArgs a, const
         next_delta = row < t.len ? a.delta[number] : 0.f;
     };
     if (n > 0) {
-        ag_load<T, DP>(A0, KEYS ? a.k : a.q, t, owner, t.at, t.len, a.d, a.vectors);
-        ag_load<T, DP>(A1, KEYS ? a.v : a.d_o, t, owner, t.at, t.len, a.d, a.vectors);
+        ag_load<T, DP, AG_ROWS>(A0, KEYS ? a.k : a.q, t, owner, t.at, t.len, a.d, a.vectors);
+        ag_load<T, DP, AG_ROWS>(A1, KEYS ? a.v : a.d_o, t, owner, t.at, t.len, a.d, a.vectors);
         numbers(0);
         load0(0);
         if (SPLIT) load1(0);

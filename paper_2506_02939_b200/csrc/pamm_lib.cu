@@ -943,7 +943,7 @@ pamm_status check_attention(const AttentionShape& g, pamm_dtype dt, float scale,
     if (g.batch == 0 || g.seq == 0 || g.heads == 0) return PAMM_OK;
     const int64_t most = 1ll << 40;
     if (g.batch > most / g.seq || g.batch * g.seq > most / g.heads) return PAMM_ERR_UNSUPPORTED;
-    const int64_t tiles = starts ? g.seq / 64 + g.sequences + 2 : g.batch * ((g.seq + 63) / 64);
+    const int64_t tiles = starts ? g.seq / AG_ROWS + g.sequences + 2 : g.batch * ((g.seq + AG_ROWS - 1) / AG_ROWS);
     return tiles > MAX_ROWS / g.heads ? PAMM_ERR_UNSUPPORTED : PAMM_OK;
 }
 inline int tiles_of(const Sequences& s, int64_t size) {
@@ -955,25 +955,25 @@ Sequences sequences_of(const AttentionShape& g, const void* lengths, const void*
 
 template <typename T, int DP>
 pamm_status launch_attention_forward_generic(AttentionArgs a, cudaStream_t st) {
-    const size_t smem = ag_smem<DP>(ag_tiles<DP, false>);
+    const size_t smem = ag_smem<DP, false>;
     if (!ensure_dynamic_smem((const void*)attention_forward_generic_kernel<T, DP>, smem)) return PAMM_ERR_CUDA;
-    a.s.items = tiles_of(a.s, AG_TILE);
+    a.s.items = tiles_of(a.s, AG_ROWS);
     launch(attention_forward_generic_kernel<T, DP>, dim3((unsigned)a.s.items * a.heads), dim3(AG_THREADS), smem, st, true, a,
-           attention_order(a.s, a.heads, AG_TILE, sm_count(), a.causal));
+           attention_order(a.s, a.heads, AG_ROWS, sm_count(), a.causal));
     return launch_result("attention_forward_generic_kernel launch");
 }
 template <typename T, int DP>
 pamm_status launch_attention_backward_generic(AttentionArgs a, cudaStream_t st) {
-    const size_t smem = ag_smem<DP>(ag_tiles<DP, true>);
+    const size_t smem = ag_smem<DP, true>;
     if (!ensure_dynamic_smem((const void*)attention_backward_generic_kernel<T, DP, false>, smem) ||
         !ensure_dynamic_smem((const void*)attention_backward_generic_kernel<T, DP, true>, smem))
         return PAMM_ERR_CUDA;
-    a.s.items = tiles_of(a.s, AG_TILE);
+    a.s.items = tiles_of(a.s, AG_ROWS);
     const int kv = a.heads / a.group, sms = sm_count();
     launch(attention_backward_generic_kernel<T, DP, false>, dim3((unsigned)a.s.items * a.heads), dim3(AG_THREADS), smem, st, true, a,
-           attention_order(a.s, a.heads, AG_TILE, sms, a.causal));
+           attention_order(a.s, a.heads, AG_ROWS, sms, a.causal));
     launch(attention_backward_generic_kernel<T, DP, true>, dim3((unsigned)a.s.items * kv), dim3(AG_THREADS), smem, st, true, a,
-           attention_order(a.s, kv, AG_TILE, sms, false));
+           attention_order(a.s, kv, AG_ROWS, sms, false));
     return launch_result("attention_backward_generic_kernel launch");
 }
 template <typename T>
