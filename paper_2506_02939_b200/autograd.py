@@ -214,7 +214,7 @@ class AttentionFunction(torch.autograd.Function):
         Z, O, lse, lengths, starts = ctx.saved_tensors
         Zd = Z.detach()
         dO = dO.to(Zd.dtype)
-        if dO.shape[-1] > 1 and dO.stride(-1) != 1:
+        if (dO.shape[-1] > 1 and dO.stride(-1) != 1) or 0 in dO.stride():      # a broadcast gradient has no tiles to copy
             dO = dO.contiguous()
         dZ = torch.empty(Zd.shape, dtype=Zd.dtype, device=Zd.device)
         dQ, dK, dV = dZ.split(ctx.parts, -2)
