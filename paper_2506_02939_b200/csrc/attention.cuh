@@ -163,15 +163,15 @@ __device__ __forceinline__ void ag_wait() { asm volatile("cp.async.wait_group %0
 
 // Rows `at` .. of the sequence into a tile, as one group of copies: rows from `valid` on and columns from d on are zero.  fp32 in vectors
 // goes asynchronously; other forms are there when the call returns.
-template <typename T, int DP, int ROWS, int THREADS = AG_THREADS>
+template <typename T, int DP, int ROWS>
 __device__ __forceinline__ void ag_load(float* tile, const HeadsView& x, const Tile& t, int64_t head, int at, int valid, int d, bool vectors) {
-    constexpr int V = 16 / (int)sizeof(T), LD = DP + 4, PER = DP / V, EACH = ROWS * PER / THREADS;
+    constexpr int V = 16 / (int)sizeof(T), LD = DP + 4, PER = DP / V, EACH = ROWS * PER / AG_THREADS;
     const T* base = x.at<T>(t.b, t.first + at, head);
     if (vectors) {
         if constexpr (sizeof(T) == 4) {
 #pragma unroll
             for (int i = 0; i < EACH; ++i) {
-                const int at_i = threadIdx.x + i * THREADS, row = at_i / PER, col = (at_i % PER) * V;
+                const int at_i = threadIdx.x + i * AG_THREADS, row = at_i / PER, col = (at_i % PER) * V;
                 const bool any = at + row < valid && col < d;
                 ag_copy16(tile + row * LD + col, any ? base + row * x.token + col : base, any);
             }
@@ -179,13 +179,13 @@ __device__ __forceinline__ void ag_load(float* tile, const HeadsView& x, const T
             typename Piece<T, V>::Raw raw[EACH];       // all of a thread's loads are in flight before the first is waited for
 #pragma unroll
             for (int i = 0; i < EACH; ++i) {
-                const int at_i = threadIdx.x + i * THREADS, row = at_i / PER, col = (at_i % PER) * V;
+                const int at_i = threadIdx.x + i * AG_THREADS, row = at_i / PER, col = (at_i % PER) * V;
                 raw[i] = Piece<T, V>::zero();
                 if (at + row < valid && col < d) raw[i] = Piece<T, V>::load(base + row * x.token + col);
             }
 #pragma unroll
             for (int i = 0; i < EACH; ++i) {
-                const int at_i = threadIdx.x + i * THREADS, row = at_i / PER, col = (at_i % PER) * V;
+                const int at_i = threadIdx.x + i * AG_THREADS, row = at_i / PER, col = (at_i % PER) * V;
                 float f[V];
                 Piece<T, V>::unpack(raw[i], f);
 #pragma unroll
@@ -194,7 +194,7 @@ __device__ __forceinline__ void ag_load(float* tile, const HeadsView& x, const T
         }
     } else {
 #pragma unroll 4
-        for (int i = threadIdx.x; i < ROWS * DP; i += THREADS) {
+        for (int i = threadIdx.x; i < ROWS * DP; i += AG_THREADS) {
             const int row = i / DP, col = i % DP;
             tile[row * LD + col] = at + row < valid && col < d ? to_float(base[row * x.token + col]) : 0.f;
         }

@@ -31,7 +31,6 @@
 #include "rotary.cuh"
 #include "grad_clip.cuh"
 #include "attention.cuh"
-#include "attention_tf32.cuh"
 #include "attention_umma.cuh"
 #include "attention_umma_backward.cuh"
 #include "dropout.cuh"
@@ -985,27 +984,6 @@ pamm_status run_attention_generic(const AttentionArgs& a, bool back, cudaStream_
 }
 
 template <int DP>
-pamm_status launch_attention_tf32(AttentionArgs a, bool back, cudaStream_t st) {
-    const size_t smem = tf_smem<DP, true>;
-    a.s.items = tiles_of(a.s, TF_ROWS);
-    const int kv = a.heads / a.group, sms = sm_count();
-    if (!back) {
-        if (!ensure_dynamic_smem((const void*)attention_forward_tf32_kernel<DP>, tf_smem<DP, false>)) return PAMM_ERR_CUDA;
-        launch(attention_forward_tf32_kernel<DP>, dim3((unsigned)a.s.items * a.heads), dim3(TF_THREADS), tf_smem<DP, false>, st, true, a,
-               attention_order(a.s, a.heads, TF_ROWS, sms, a.causal));
-        return launch_result("attention_forward_tf32_kernel launch");
-    }
-    if (!ensure_dynamic_smem((const void*)attention_backward_tf32_kernel<DP, false>, smem) ||
-        !ensure_dynamic_smem((const void*)attention_backward_tf32_kernel<DP, true>, smem))
-        return PAMM_ERR_CUDA;
-    launch(attention_backward_tf32_kernel<DP, false>, dim3((unsigned)a.s.items * a.heads), dim3(TF_THREADS), smem, st, true, a,
-           attention_order(a.s, a.heads, TF_ROWS, sms, a.causal));
-    launch(attention_backward_tf32_kernel<DP, true>, dim3((unsigned)a.s.items * kv), dim3(TF_THREADS), smem, st, true, a,
-           attention_order(a.s, kv, TF_ROWS, sms, false));
-    return launch_result("attention_backward_tf32_kernel launch");
-}
-
-template <int DP>
 pamm_status launch_attention_forward(AttentionArgs a, const AttentionMaps& m, cudaStream_t st) {
     using Plan = AttentionPlan<DP>;
     if (!ensure_dynamic_smem((const void*)attention_forward_kernel<DP>, Plan::SMEM)) return PAMM_ERR_CUDA;
@@ -1053,7 +1031,6 @@ pamm_status run_attention(const AttentionArgs& a, pamm_dtype dt, bool back, cuda
         }
         return a.d <= 64 ? launch_attention_forward<64>(a, m, st) : launch_attention_forward<128>(a, m, st);
     }
-    if (dt == PAMM_F32 && a.vectors && a.d <= 128) return a.d <= 64 ? launch_attention_tf32<64>(a, back, st) : launch_attention_tf32<128>(a, back, st);
     return dt == PAMM_F32 ? run_attention_generic<float>(a, back, st) : run_attention_generic<__nv_bfloat16>(a, back, st);
 }
 
