@@ -493,13 +493,14 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
                     }
                     if (g == 0 || pass > 0) break;
                     const float seen = fmaxf(max_of(s[0], top), max_of(s[1], top));
-                    if (!__any_sync(0xffffffffu, (seen - top) * c > AF_RISE)) break;
+                    const bool rises = (seen - top) * c > AF_RISE;       // each row for itself: its result does not depend on its neighbours
+                    if (!__any_sync(0xffffffffu, rises)) break;
                     // O is at rest once the last product handed over has been added to it
                     ok = warp_wait(&s_added[x], total - 1 & 1u, abort_flag);
                     if (!ok) break;
                     ptx::tc_fence_after_sync();
-                    const float keep = seen == top ? 1.f : exp2_approx((top - seen) * c);
-                    top = seen;
+                    const float keep = rises ? exp2_approx((top - seen) * c) : 1.f;
+                    if (rises) top = seen;
                     sum *= keep;
 #pragma unroll 1
                     for (int i = 0; i < DP; i += 8) {
