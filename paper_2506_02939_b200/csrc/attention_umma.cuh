@@ -77,9 +77,13 @@ struct ItemReader {
         return item.t.rows >= 0;
     }
 };
-// The warp that finds them.
-template <int SIZE>
-__device__ __forceinline__ bool au_find_items(ItemQueue& q, const Sequences& s, const AttentionOrder& order, volatile int* abort_flag) {
+// The warp that finds them.  `steps` says how long an item takes: behind one of a few steps the next is taken at once, so that its tiles
+// come in time; behind a longer one when that has begun, so that no block holds work that another could start on.
+// Items without a valid row are not handed on: this warp writes their zeros itself (`clear`).  So every item that is has at least a
+// step, and a reader that looks two steps ahead never needs more than two items ahead -- no more than the queue holds while another
+// reader waits for what the first one does with its present item.
+template <int SIZE, typename F, typename G>
+__device__ __forceinline__ bool au_find_items(ItemQueue& q, const Sequences& s, const AttentionOrder& order, volatile int* abort_flag, F steps, G clear) {
     uint32_t count = 0, phase = 0;
     int w = (int)blockIdx.x;
     while (true) {
@@ -90,7 +94,10 @@ __device__ __forceinline__ bool au_find_items(ItemQueue& q, const Sequences& s, 
             order.at(w, number, item.head);
             item.t = find_tile<SIZE>(s, number);
         }
-        if (w < 0 || item.t.any) {
+        if (w >= 0 && item.t.any && item.t.at >= item.t.len) {
+            clear(item);
+            __syncwarp();
+        } else if (w < 0 || item.t.any) {
             const uint32_t slot = count % AU_ITEMS;
             if (!warp_wait(&q.empty[slot], ((count / AU_ITEMS) & 1u) ^ 1u, abort_flag)) return false;
             if ((threadIdx.x & 31) == 0) {
@@ -98,8 +105,9 @@ __device__ __forceinline__ bool au_find_items(ItemQueue& q, const Sequences& s, 
                 ptx::mbar_arrive(&q.full[slot]);
             }
             __syncwarp();
-            ++count;
             if (w < 0) return true;
+            if (steps(item.t) >= 4 && !warp_wait(&q.empty[slot], (count / AU_ITEMS) & 1u, abort_flag)) return false;
+            ++count;
         }
         if ((threadIdx.x & 31) == 0) {
             ptx::fence_proxy_async();          // the last answer has been read
@@ -111,6 +119,14 @@ __device__ __forceinline__ bool au_find_items(ItemQueue& q, const Sequences& s, 
         phase ^= 1u;
         w = ptx::taken_block(&q.response);
         __syncwarp();
+    }
+}
+// Zeros in the rows of an item from `at` on, at most `size` of them.  A whole warp.
+__device__ __forceinline__ void au_clear(const HeadsView& y, const Item& item, int size, int d) {
+    const int end = min(size, item.t.rows - item.t.at);
+    for (int r = threadIdx.x & 31; r < end; r += 32) {
+        __nv_bfloat16* p = y.at<__nv_bfloat16>(item.t.b, item.t.first + item.t.at + r, item.head);
+        for (int c = 0; c < d; c += 8) st16(p + c, make_uint4(0, 0, 0, 0));
     }
 }
 // The producer's ring of tiles.  Called by the whole warp.
@@ -336,7 +352,10 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
     if (warp >= AU_TMA_WARP) {
         ptx::registers_down<AU_OTHER_REGS>();
         if (warp == AU_ITEMS_WARP) {
-            ok = au_find_items<AF_QUERIES>(s_queue, a.s, order, abort_flag);
+            ok = au_find_items<AF_QUERIES>(s_queue, a.s, order, abort_flag, [&](const Tile& t) { return au_key_tiles(t, a.causal, 0); }, [&](const Item& it) {
+                au_clear(a.o, it, AF_QUERIES, a.d);
+                for (int r = it.t.at + lane; a.lse && r < min(it.t.at + AF_QUERIES, it.t.rows); r += 32) a.lse[a.row_number(it.t, it.head) + r] = -INFINITY;
+            });
         } else if (warp == AU_TMA_WARP) {
             TileRing ring = {ring_tiles, s_full, s_empty, &s_tail, abort_flag, Plan::SLOTS, 0, 0, 0, 0, false};
             uint32_t q_phase[2] = {0, 0};

@@ -16,7 +16,7 @@ struct Step { bool any, first, last; };
 // The tiles of queries that see a tile of keys: `per` of each of the group's heads, from tile `from` on.
 __device__ __forceinline__ int ab_query_tiles(const Tile& t, bool causal, int group, int& from, int& per) {
     from = causal ? t.at / AU_ROWS : 0;
-    per = t.at < t.len ? (t.len + AU_ROWS - 1) / AU_ROWS - from : 0;
+    per = (t.len + AU_ROWS - 1) / AU_ROWS - from;
     return per * group;
 }
 template <bool KEYS>
@@ -25,11 +25,11 @@ struct StepReader {
     int n = 0, j = 0;
     bool end = false;
     __device__ __forceinline__ Step next(bool causal, int group, bool& ok) {
-        while (!end && j == n) {
+        if (!end && j == n) {
             Item item;
             int from, per;
             end = !reader.next_alone(item, ok);
-            n = end ? 0 : KEYS ? ab_query_tiles(item.t, causal, group, from, per) : au_key_tiles(item.t, causal, 0);
+            if (!end) n = KEYS ? ab_query_tiles(item.t, causal, group, from, per) : au_key_tiles(item.t, causal, 0);
             j = 0;
         }
         const Step s = {!end, j == 0, j == n - 1};
@@ -110,7 +110,8 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
     if (warp >= AU_TMA_WARP) {
         ptx::registers_down<AU_OTHER_REGS>();
         if (warp == AU_ITEMS_WARP) {
-            ok = au_find_items<AU_ROWS>(s_queue, a.s, order, abort_flag);
+            ok = au_find_items<AU_ROWS>(s_queue, a.s, order, abort_flag, [&](const Tile& t) { return au_key_tiles(t, a.causal, 0); },
+                                        [&](const Item& it) { au_clear(a.dq, it, AU_ROWS, a.d); });
         } else if (warp == AU_TMA_WARP) {
             TileRing keys = {ring_tiles, s_full, s_empty, &s_tail[0], abort_flag, K_SLOTS, 0, 0, 0, 0, false};
             TileRing values = {ring_tiles + K_SLOTS * Plan::TILE_BYTES, s_full + K_SLOTS, s_empty + K_SLOTS, &s_tail[1], abort_flag, V_SLOTS, 0, 0, 0, 0, false};
@@ -126,7 +127,7 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
                          au_produce<DP>(values, &m.v, t, hk, j * AU_ROWS, clear);
                 }
                 if (!ok) break;
-                if (n > 0) f_phase ^= 1u;
+                f_phase ^= 1u;
             }
             if (!ok) {
                 ab_drain(keys, s_ffull);
@@ -211,7 +212,7 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
         while (more || any) {
             more = more && reader.next(item, ok);
             if (!ok) break;
-            if (more && au_key_tiles(item.t, a.causal, 0) > 0) {
+            if (more) {
                 const Tile& t = item.t;
                 const int pieces = a.d / 8, piece = lane & 15, valid = t.len - t.at - quarter;      // of 16 bytes, 16 lanes a row
                 const int64_t number = a.row_number(t, item.head) + t.at + quarter;
@@ -261,14 +262,12 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
             }
             if (any) {
                 const Tile& t = before.t;
-                const int n = au_key_tiles(t, a.causal, 0), me = t.at + row;
-                if (n > 0) {
-                    ok = warp_wait(&s_done, done_phase, abort_flag);
-                    if (!ok) break;
-                    done_phase ^= 1u;
-                    ptx::tc_fence_after_sync();
-                }
-                au_store(tmem + 384 + lanes, a.dq.at<__nv_bfloat16>(t.b, t.first + me, before.head), a.d, a.scale, n > 0, me < t.len, me < t.rows, a.wide,
+                const int me = t.at + row;
+                ok = warp_wait(&s_done, done_phase, abort_flag);
+                if (!ok) break;
+                done_phase ^= 1u;
+                ptx::tc_fence_after_sync();
+                au_store(tmem + 384 + lanes, a.dq.at<__nv_bfloat16>(t.b, t.first + me, before.head), a.d, a.scale, true, me < t.len, me < t.rows, a.wide,
                          &s_free);
             }
             before = item;
@@ -284,7 +283,6 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
         while (reader.next(item, ok)) {
             const Tile& t = item.t;
             const int n = au_key_tiles(t, a.causal, 0), me = t.at + row;
-            if (n == 0) continue;
             const int last = a.causal ? min(me, t.len - 1) : t.len - 1;
             ok = warp_wait(&s_rows, phase, abort_flag);
             if (!ok) break;
@@ -406,7 +404,10 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
     if (warp >= AU_TMA_WARP) {
         ptx::registers_down<AU_OTHER_REGS>();
         if (warp == AU_ITEMS_WARP) {
-            ok = au_find_items<AU_ROWS>(s_queue, a.s, order, abort_flag);
+            ok = au_find_items<AU_ROWS>(s_queue, a.s, order, abort_flag, [&](const Tile& t) { return ab_query_tiles(t, a.causal, a.group, from, per); }, [&](const Item& it) {
+                au_clear(a.dk, it, AU_ROWS, a.d);
+                au_clear(a.dv, it, AU_ROWS, a.d);
+            });
         } else if (warp == AU_TMA_WARP) {
             TileRing ring = {ring_tiles, s_full, s_empty, &s_tail, abort_flag, Plan::SLOTS, 0, 0, 0, 0, false};
             uint32_t f_phase = 0;
@@ -422,7 +423,7 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
                          au_produce<DP>(ring, &m.d_o, t, h, at, clear);
                 }
                 if (!ok) break;
-                if (n > 0) f_phase ^= 1u;
+                f_phase ^= 1u;
             }
             if (!ok) ab_drain(ring, s_ffull);
         } else if (warp == AU_MMA_WARP) {
@@ -515,18 +516,16 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
         uint32_t phase = 0;
         while (reader.next(item, ok)) {
             const Tile& t = item.t;
-            const int n = ab_query_tiles(t, a.causal, a.group, from, per), me = t.at + row;
+            const int me = t.at + row;
             for (int what = 0; what < 2 && ok; ++what) {
-                if (n > 0) {
-                    ok = warp_wait(&s_done[what], phase, abort_flag);
-                    if (!ok) break;
-                    ptx::tc_fence_after_sync();
-                }
-                au_store(tmem + 256 + what * 128 + lanes, (what ? a.dk : a.dv).at<__nv_bfloat16>(t.b, t.first + me, item.head), a.d, what ? a.scale : 1.f, n > 0,
+                ok = warp_wait(&s_done[what], phase, abort_flag);
+                if (!ok) break;
+                ptx::tc_fence_after_sync();
+                au_store(tmem + 256 + what * 128 + lanes, (what ? a.dk : a.dv).at<__nv_bfloat16>(t.b, t.first + me, item.head), a.d, what ? a.scale : 1.f, true,
                          me < t.len, me < t.rows, a.wide, &s_free[what]);
             }
             if (!ok) break;
-            if (n > 0) phase ^= 1u;
+            phase ^= 1u;
         }
     } else {
         ptx::registers_up<AU_ROW_REGS>();

@@ -280,3 +280,33 @@ def test_python_refusals():
         with pytest.raises(error):
             call()
     assert torch.equal(pamm.attention_forward(Q, K, V)[0], O)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+def test_many_sequences_without_a_token(causal, d):
+    """Blocks meet long runs of tiles with nothing to compute, between short and long ones."""
+    batch, seq, heads, kv = 400, 700, 2, 1
+    lengths = [(0, 0, 0, 0, 1, 0, 0, 130, 0, 0, 0, 700)[i % 12] for i in range(batch)]
+    Q, K, V = parts((batch, seq), heads, kv, d, BF16, 21)
+    dO = normal(Q.shape, BF16, 22, 0.1)
+    O, lse = pamm.attention_forward(Q, K, V, causal=causal, lengths=index(lengths))
+    grads = pamm.attention_backward(dO, Q, K, V, O, lse, causal=causal, lengths=index(lengths))
+    assert pamm.last_device_status() == pamm.OK
+    some = [i for i, n in enumerate(lengths) if n]
+    q, k, v, g = (t[some].contiguous() for t in (Q, K, V, dO))
+    few = index([lengths[i] for i in some])
+    o, l = pamm.attention_forward(q, k, v, causal=causal, lengths=few)
+    for a, b in zip((O, lse, *grads), (o, l, *pamm.attention_backward(g, q, k, v, o, l, causal=causal, lengths=few))):
+        assert torch.equal(a[some], b)
+    none = [i for i, n in enumerate(lengths) if not n]
+    assert not any(t[none].any() for t in (O, *grads)) and (lse[none] == -math.inf).all()
+    # packed: short documents, and a tail that belongs to none of them, with many heads
+    starts = [0, 1, 2, 3, 140, 141, 900]
+    Q, K, V = parts((5000,), 24, 12, d, BF16, 23)
+    O, lse = pamm.attention_forward(Q, K, V, causal=causal, starts=index(starts))
+    grads = pamm.attention_backward(Q, Q, K, V, O, lse, causal=causal, starts=index(starts))
+    assert pamm.last_device_status() == pamm.OK
+    o, l = pamm.attention_forward(Q[:900], K[:900], V[:900], causal=causal, starts=index(starts))
+    for a, b in zip((O, *grads), (o, *pamm.attention_backward(Q[:900], Q[:900], K[:900], V[:900], o, l, causal=causal, starts=index(starts)))):
+        assert torch.equal(a[:900], b) and not a[900:].any()
