@@ -6,6 +6,7 @@
 #include <cmath>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <map>
 #include <tuple>
 #include <mutex>
@@ -923,6 +924,12 @@ bool heads_view(const pamm_heads* t, const AttentionShape& g, int64_t heads, siz
     out = {t->data, g.batch > 1 ? t->batch : 0, g.seq > 1 ? t->token : 0, heads > 1 ? t->head : 0};
     return !output || ((g.batch == 1 || out.batch != 0) && (g.seq == 1 || out.token != 0) && (heads == 1 || out.head != 0));
 }
+// No output begins where an input or another output does: that much of an overlap is seen here.
+bool begin_apart(std::initializer_list<const void*> inputs, std::initializer_list<const void*> outputs) {
+    for (auto y = outputs.begin(); y != outputs.end(); ++y)
+        if (std::find(inputs.begin(), inputs.end(), *y) != inputs.end() || std::find(outputs.begin(), y, *y) != y) return false;
+    return true;
+}
 // Whole 16-byte vectors on memory's grid in every row.
 bool heads_aligned(const HeadsView& t, size_t es, int64_t to = 16) {
     const auto on = [&](int64_t stride) { return stride * (int64_t)es % to == 0; };
@@ -1065,7 +1072,7 @@ pamm_status pamm_attention_forward(const pamm_heads* Q, const pamm_heads* K, con
     const size_t es = esize(dt);
     AttentionArgs a = {};
     if (!heads_view(Q, g, heads, es, false, a.q) || !heads_view(K, g, kv_heads, es, false, a.k) || !heads_view(V, g, kv_heads, es, false, a.v) ||
-        !heads_view(O, g, heads, es, true, a.o) || !aligned(lse, 4))
+        !heads_view(O, g, heads, es, true, a.o) || !aligned(lse, 4) || !begin_apart({Q->data, K->data, V->data, lse}, {O->data}))
         return PAMM_ERR_INVALID_ARG;
     a.lse = lse;
     a.s = sequences_of(g, lengths, starts, index_type);
@@ -1091,6 +1098,7 @@ pamm_status pamm_attention_backward(const pamm_heads* dO, const pamm_heads* Q, c
         !heads_view(dK, g, kv_heads, es, true, a.dk) || !heads_view(dV, g, kv_heads, es, true, a.dv) || !lse || !aligned(lse, 4))
         return PAMM_ERR_INVALID_ARG;
     if (!workspace || !aligned(workspace, 16) || ws_bytes < attention_backward_ws_bytes(batch * seq, heads)) return PAMM_ERR_WORKSPACE;
+    if (!begin_apart({dO->data, Q->data, K->data, V->data, O->data, lse, workspace}, {dQ->data, dK->data, dV->data})) return PAMM_ERR_INVALID_ARG;
     a.lse_in = lse;
     a.delta = static_cast<float*>(workspace);
     a.s = sequences_of(g, lengths, starts, index_type);

@@ -53,6 +53,16 @@ def test_attention_refusals(back):
         assert call(back, **kw, Q=dict(data=0), ws=NULL) == pamm.OK
 
 
+@pytest.mark.parametrize("back", [False, True])
+def test_outputs_that_begin_where_another_tensor_does(back):
+    apart = {n: dict(data=FAKE * (i + 2)) for i, n in enumerate(("dO", "Q", "K", "V", "O", "dQ", "dK", "dV"))}
+    for one in ("dQ", "dK", "dV") if back else ("O",):
+        for other in ("dO", "Q", "K", "V", "O", "dQ", "dK", "dV") if back else ("Q", "K", "V"):
+            if one != other:
+                assert call(back, **{**apart, one: apart[other]}) == BAD, (one, other)
+        assert call(back, **{**apart, one: dict(data=FAKE)}) == BAD, one             # the log-sums, and the workspace
+
+
 def test_dropout_refusals():
     def call(X=FAKE, ldx=8, R=NULL, ldr=0, b=4, n=8, dt=0, p=0.5, seed=1, offset=2, counter=NULL, Y=FAKE + 4096, ldy=8):
         return pamm._lib.pamm_dropout(X, ldx, R, ldr, b, n, dt, p, seed, offset, counter, Y, ldy, None)
