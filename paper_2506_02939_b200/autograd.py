@@ -12,6 +12,9 @@ with m = |Q| + |K| + |V|, as in the paper's notation.
 Around it: ``Norm`` (layer norm or its root-mean-square form, with the residual addition), whose
 output is the projection's input; ``rotary`` on the heads of the projection's output; ``attention`` over
 them; ``dropout`` with the residual addition; and ``clip_grad_norm_`` for the end of a training step.
+
+A step that is captured into a CUDA graph starts from parameters whose earlier autograd graphs (a loss that is still held)
+are gone: PyTorch accumulates a gradient on the stream of the first graph that it belonged to, which a capture cannot join.
 """
 from __future__ import annotations
 
@@ -199,7 +202,7 @@ class AttentionFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, Z, lengths, starts, kv_heads, causal, scale):
         Zd = Z.detach()
-        if Zd.shape[-1] > 1 and Zd.stride(-1) != 1:
+        if (Zd.shape[-1] > 1 and Zd.stride(-1) != 1) or 0 in Zd.stride():      # a broadcast row has no tiles to copy
             Zd = Zd.contiguous()
         heads = Zd.shape[-2] - 2 * kv_heads
         ctx.parts = (heads, kv_heads, kv_heads)
@@ -214,7 +217,7 @@ class AttentionFunction(torch.autograd.Function):
         Z, O, lse, lengths, starts = ctx.saved_tensors
         Zd = Z.detach()
         dO = dO.to(Zd.dtype)
-        if (dO.shape[-1] > 1 and dO.stride(-1) != 1) or 0 in dO.stride():      # a broadcast gradient has no tiles to copy
+        if (dO.shape[-1] > 1 and dO.stride(-1) != 1) or 0 in dO.stride():      # nor has a broadcast gradient
             dO = dO.contiguous()
         dZ = torch.empty(Zd.shape, dtype=Zd.dtype, device=Zd.device)
         dQ, dK, dV = dZ.split(ctx.parts, -2)
@@ -264,7 +267,10 @@ class Dropout(torch.nn.Module):
     the same ``seed``.  In evaluation mode X (+ residual) passes.  Two modules with one seed have the same masks: give each its own.
 
     ``counter``: a one-element int64 tensor on the device that numbers the calls in a captured graph (counted up by the program
-    between replays); without it a graph replays the mask that it was captured with."""
+    between replays); without it a graph replays the mask that it was captured with.
+
+    ``calls`` numbers the calls outside a graph.  Code that runs a forward pass a second time for its backward pass (activation
+    checkpointing) would draw another mask there: give ``dropout`` a seed and an offset of your own instead."""
 
     def __init__(self, p: float = 0.1, seed: int = 0, counter=None):
         super().__init__()

@@ -79,6 +79,16 @@ def test_broadcast_strided_and_packed_gradients():
         assert torch.equal(o[0], O[lo:hi]) and torch.equal(one.grad[0], P.grad[lo:hi])
 
 
+def test_a_broadcast_row():
+    one = normal((1, 90, 6, 64), BF16, 5).requires_grad_()
+    many = one.detach().repeat(3, 1, 1, 1).requires_grad_()
+    g = normal((3, 90, 2, 64), BF16, 6)
+    a, b = attention(one.expand(3, -1, -1, -1), 2), attention(many, 2)
+    a.backward(g)
+    b.backward(g)
+    assert torch.equal(a, b) and torch.equal(one.grad, many.grad.sum(0, keepdim=True))
+
+
 def test_attention_of_a_row_changed_in_place_is_refused():
     Z = normal((1, 20, 3, 64), BF16, 5).requires_grad_()
     Y = Z * 1.0
