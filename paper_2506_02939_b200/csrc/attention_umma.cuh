@@ -121,12 +121,13 @@ __device__ __forceinline__ bool au_find_items(ItemQueue& q, const Sequences& s, 
         __syncwarp();
     }
 }
-// Zeros in the rows of an item from `at` on, at most `size` of them.  A whole warp.
+// Zeros in the rows of an item from `at` on, at most `size` of them.  A whole warp, whose stores follow each other in memory.
 __device__ __forceinline__ void au_clear(const HeadsView& y, const Item& item, int size, int d) {
-    const int end = min(size, item.t.rows - item.t.at);
-    for (int r = threadIdx.x & 31; r < end; r += 32) {
-        __nv_bfloat16* p = y.at<__nv_bfloat16>(item.t.b, item.t.first + item.t.at + r, item.head);
-        for (int c = 0; c < d; c += 8) st16(p + c, make_uint4(0, 0, 0, 0));
+    const int pieces = d / 8, end = min(size, item.t.rows - item.t.at) * pieces;
+    __nv_bfloat16* p = y.at<__nv_bfloat16>(item.t.b, item.t.first + item.t.at, item.head);
+    for (int i = threadIdx.x & 31; i < end; i += 32) {
+        const int r = i / pieces;
+        st16(p + r * y.token + (i - r * pieces) * 8, make_uint4(0, 0, 0, 0));
     }
 }
 // The producer's ring of tiles.  Called by the whole warp.
