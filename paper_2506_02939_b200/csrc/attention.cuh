@@ -141,9 +141,9 @@ struct AttentionArgs {
 // ---- kernels for every type, size and order ---------------------------------------------------------------------
 // Products in fp32 by fused multiply-adds: tiles of 32 x 64 scores, 16 a thread in 4 rows, whose operands come out of shared
 // memory as vectors along the head (rows 4 words past a multiple of 32 apart: no bank conflicts).  They serve fp32, heads
-// that are not multiples of 8 or wider than 128, and rows off the 16-byte grid.  Bound by instructions and reads of shared memory.
-// (Blocks of 64 rows and 256 threads: 2 an SM, unevenly loaded in small batches; 8 x 256 tokens of 8 heads of 64 causal took
-// 33 us forward and 113 us backward.)
+// that are not multiples of 8 or wider than 128, and rows off the 16-byte grid.  Bound by multiply-adds and reads of shared memory, and
+// by their latency where an SM's last blocks are alone.  8 x 256 tokens of 8 heads of 64, causal: 29 us forward, 83 backward; 31 and 87
+// with one multiply-add an instruction; 33 and 113 in blocks of 64 rows and 256 threads, 2 an SM and unevenly loaded.
 constexpr int AG_ROWS = 32, AG_TILE = 64, AG_THREADS = 4 * AG_ROWS, AG_P_LD = AG_TILE + 4;       // owned rows, streamed rows
 
 // Whether the two streamed tiles have a place each, so that the one is on its way while the other is worked on.
@@ -208,11 +208,12 @@ __device__ __forceinline__ void ag_scores(const float* A, const float* B, int d,
     constexpr int LD = DP + 4;
     const float* a = A + (threadIdx.x / 16) * 4 * LD;
     const float* b = B + (threadIdx.x % 16) * LD;
+    float2 sums[4][4];        // over even and odd columns: two multiply-adds an instruction
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) c[r][j] = 0.f;
-#pragma unroll 4
+        for (int j = 0; j < 4; ++j) sums[r][j] = twice(0.f);
+#pragma unroll 2
     for (int e = 0; e < d; e += 4) {
         float4 x[4], y[4];
 #pragma unroll
@@ -223,8 +224,12 @@ __device__ __forceinline__ void ag_scores(const float* A, const float* B, int d,
         for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                c[r][j] = fmaf(x[r].w, y[j].w, fmaf(x[r].z, y[j].z, fmaf(x[r].y, y[j].y, fmaf(x[r].x, y[j].x, c[r][j]))));
+                sums[r][j] = fma2(make_float2(x[r].z, x[r].w), make_float2(y[j].z, y[j].w), fma2(make_float2(x[r].x, x[r].y), make_float2(y[j].x, y[j].y), sums[r][j]));
     }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c[r][j] = sums[r][j].x + sums[r][j].y;
 }
 // acc[r][.] += sum over the first `keys` entries of row (4 ty + r) of P times B's rows; a thread has columns 4 tx .. of every 64
 template <int DP>
@@ -245,10 +250,12 @@ __device__ __forceinline__ void ag_accumulate(const float* P, const float* B, in
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const float w = e == 0 ? x[r].x : e == 1 ? x[r].y : e == 2 ? x[r].z : x[r].w;
-                    acc[r][4 * c] = fmaf(w, y.x, acc[r][4 * c]);
-                    acc[r][4 * c + 1] = fmaf(w, y.y, acc[r][4 * c + 1]);
-                    acc[r][4 * c + 2] = fmaf(w, y.z, acc[r][4 * c + 2]);
-                    acc[r][4 * c + 3] = fmaf(w, y.w, acc[r][4 * c + 3]);
+                    const float2 lo = fma2(twice(w), make_float2(y.x, y.y), make_float2(acc[r][4 * c], acc[r][4 * c + 1]));
+                    const float2 hi = fma2(twice(w), make_float2(y.z, y.w), make_float2(acc[r][4 * c + 2], acc[r][4 * c + 3]));
+                    acc[r][4 * c] = lo.x;
+                    acc[r][4 * c + 1] = lo.y;
+                    acc[r][4 * c + 2] = hi.x;
+                    acc[r][4 * c + 3] = hi.y;
                 }
             }
         }
