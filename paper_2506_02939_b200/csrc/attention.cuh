@@ -14,7 +14,7 @@
 
 namespace pamm {
 
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float LOG2E = 1.4426950408889634f;
 constexpr int ATT_MAX_DIM = 256;
 
 // Element (b, s, h, d) of a tensor lies at p + b batch + s token + h head + d.

@@ -18,7 +18,7 @@ constexpr int AU_ROWS = 128, AU_BLOCK_BYTES = AU_ROWS * 128;       // of a tile,
 // products before it have been taken by the tensor cores (165 clocks a wait that is long over, where products follow
 // each other without a gap otherwise); where products wait for different warps, a second thread's fill that time.
 // Registers: 128 a thread at the launch; the rows' warps take what the others give back.
-constexpr int AU_THREADS = 512, AU_FINISH_WARP = 8, AU_TMA_WARP = 12, AU_MMA_WARP = 13, AU_STATS_WARP = 14, AU_ITEMS_WARP = 15;
+constexpr int AU_THREADS = 512, AU_FINISH_WARP = 8, AU_TMA_WARP = 12, AU_MMA_WARP = 13, AU_ITEMS_WARP = 15;
 constexpr int AU_ROW_REGS = 168, AU_OTHER_REGS = 88;
 static_assert(256 * AU_ROW_REGS + 256 * AU_OTHER_REGS <= 65536, "what is taken has to have been given back");
 
