@@ -570,6 +570,13 @@ pamm_status pamm_set_profile_events(pamm_prof_kind kind, void* start_event, void
 pamm_status pamm_selftest_bounded_wait(void* stream);
 
 /*
+ * Self-test of the attention kernels' waits, whose limit counts from the last sign of progress on: one small kernel
+ * waits eight times its limit for a warp that shows progress all the while and then arrives.  The device status
+ * stays clear.
+ */
+pamm_status pamm_selftest_progress_wait(void* stream);
+
+/*
  * Read-only streaming probes (no counterpart in the paper): what a pass that only reads a
  * matrix once can reach on this device, as the practical ceiling of the compression (reads X)
  * and of the contraction (reads dY).  `base` (device): `rows` rows of `row_bytes` bytes (a

@@ -35,9 +35,30 @@ __device__ __forceinline__ void au_load(uint8_t* dst, const CUtensorMap* tm, con
     for (int c = 0; c < DP / 64; ++c)
         ptx::tma_load_4d(dst + c * AU_BLOCK_BYTES, tm, c * 64, head, (int32_t)(t.first + at), (int32_t)t.b, bar);
 }
+// A wait for another warp's whole item lasts as long as the item, which grows with the context: a tile of keys meets (tokens / 128) x
+// (query heads that share it) steps of 1.4 us.  So polls are counted from the block's last sign of progress on: a tile that is on its way,
+// or an item that has been looked at.  Both come to an end with the work, so every wait does.  (2^22 polls of 4 us: 17 seconds without one.)
+struct Watch {
+    int abort;                      // set by a wait that ran out
+    uint32_t tiles, items;          // written by the warp that copies, and by the one that finds the items
+};
+__device__ __forceinline__ bool au_wait(uint64_t* bar, uint32_t parity, volatile Watch* watch, uint32_t polls = ptx::WAIT_POLLS) {
+    uint32_t seen = 0;
+    for (uint32_t it = 0; it < polls; ++it) {
+        if (ptx::mbar_try_wait(bar, parity)) return true;
+        if ((it & 63u) == 63u) {
+            if (watch->abort) return false;
+            const uint32_t now = watch->tiles + watch->items;
+            if (now != seen) { seen = now; it = 0; }
+            __nanosleep(64);
+        }
+    }
+    watch->abort = 1;
+    return false;
+}
 // A wait of a whole warp: the same answer in every lane.
-__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-    return __all_sync(0xffffffffu, ptx::mbar_wait(bar, parity, abort_flag));
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile Watch* watch, uint32_t polls = ptx::WAIT_POLLS) {
+    return __all_sync(0xffffffffu, au_wait(bar, parity, watch, polls));
 }
 // The block's items, found ahead by one warp and read by all others (`readers` warps: each gives an entry back as soon as it has it in
 // registers).  An entry with rows < 0 is the end.  Every item has a block in the grid; a block that is through with its own takes over
@@ -55,12 +76,12 @@ struct ItemQueue {
 };
 struct ItemReader {
     ItemQueue* q;
-    volatile int* abort_flag;
+    volatile Watch* watch;
     uint32_t count = 0;
     // False at the end and where a wait ran out (`ok`).
     __device__ __forceinline__ bool next(Item& item, bool& ok) {
         const uint32_t slot = count % AU_ITEMS;
-        if (!warp_wait(&q->full[slot], (count / AU_ITEMS) & 1u, abort_flag)) { ok = false; return false; }
+        if (!warp_wait(&q->full[slot], (count / AU_ITEMS) & 1u, watch)) { ok = false; return false; }
         item = q->items[slot];
         __syncwarp();
         if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(&q->empty[slot]);
@@ -70,7 +91,7 @@ struct ItemReader {
     // The same for a thread that reads for its warp.
     __device__ __forceinline__ bool next_alone(Item& item, bool& ok) {
         const uint32_t slot = count % AU_ITEMS;
-        if (!ptx::mbar_wait(&q->full[slot], (count / AU_ITEMS) & 1u, abort_flag)) { ok = false; return false; }
+        if (!au_wait(&q->full[slot], (count / AU_ITEMS) & 1u, watch)) { ok = false; return false; }
         item = q->items[slot];
         ptx::mbar_arrive(&q->empty[slot]);
         ++count;
@@ -83,10 +104,12 @@ struct ItemReader {
 // step, and a reader that looks two steps ahead never needs more than two items ahead -- no more than the queue holds while another
 // reader waits for what the first one does with its present item.
 template <int SIZE, typename F, typename G>
-__device__ __forceinline__ bool au_find_items(ItemQueue& q, const Sequences& s, const AttentionOrder& order, volatile int* abort_flag, F steps, G clear) {
-    uint32_t count = 0, phase = 0;
+__device__ __forceinline__ bool au_find_items(ItemQueue& q, const Sequences& s, const AttentionOrder& order, volatile Watch* watch, F steps, G clear) {
+    uint32_t count = 0, phase = 0, looked = 0;
     int w = (int)blockIdx.x;
     while (true) {
+        ++looked;
+        if ((threadIdx.x & 31) == 0) watch->items = looked;
         Item item;
         item.t.rows = -1;
         if (w >= 0) {
@@ -99,14 +122,14 @@ __device__ __forceinline__ bool au_find_items(ItemQueue& q, const Sequences& s, 
             __syncwarp();
         } else if (w < 0 || item.t.any) {
             const uint32_t slot = count % AU_ITEMS;
-            if (!warp_wait(&q.empty[slot], ((count / AU_ITEMS) & 1u) ^ 1u, abort_flag)) return false;
+            if (!warp_wait(&q.empty[slot], ((count / AU_ITEMS) & 1u) ^ 1u, watch)) return false;
             if ((threadIdx.x & 31) == 0) {
                 q.items[slot] = item;
                 ptx::mbar_arrive(&q.full[slot]);
             }
             __syncwarp();
             if (w < 0) return true;
-            if (steps(item.t) >= 4 && !warp_wait(&q.empty[slot], (count / AU_ITEMS) & 1u, abort_flag)) return false;
+            if (steps(item.t) >= 4 && !warp_wait(&q.empty[slot], (count / AU_ITEMS) & 1u, watch)) return false;
             ++count;
         }
         if ((threadIdx.x & 31) == 0) {
@@ -115,7 +138,7 @@ __device__ __forceinline__ bool au_find_items(ItemQueue& q, const Sequences& s, 
             ptx::take_next_block(&q.response, &q.answered);
         }
         __syncwarp();
-        if (!warp_wait(&q.answered, phase, abort_flag)) return false;
+        if (!warp_wait(&q.answered, phase, watch)) return false;
         phase ^= 1u;
         w = ptx::taken_block(&q.response);
         __syncwarp();
@@ -134,20 +157,21 @@ __device__ __forceinline__ void au_clear(const HeadsView& y, const Item& item, i
 struct TileRing {
     uint8_t* tiles;
     uint64_t *full, *empty, *tail;       // tail: for a tile whose last rows are cleared before it is handed on
-    volatile int* abort_flag;
+    volatile Watch* watch;
     int slots, slot;
     uint32_t phase, tail_phase, used;
     bool tail_open;
     __device__ __forceinline__ void next() {
         if (++slot == slots) { slot = 0; phase ^= 1u; }
         ++used;
+        if ((threadIdx.x & 31) == 0) watch->tiles = used;
     }
 };
 // The next tile of the ring.  `clear`: rows from the sequence's end on are set to zero, because a product with a weight of 0 would keep
 // their NaN or infinity; needed where the tensor goes on behind the end.
 template <int DP>
 __device__ __forceinline__ bool au_produce(TileRing& r, const CUtensorMap* tm, const Tile& t, int head, int at, bool clear) {
-    if (!warp_wait(&r.empty[r.slot], r.phase ^ 1u, r.abort_flag)) return false;
+    if (!warp_wait(&r.empty[r.slot], r.phase ^ 1u, r.watch)) return false;
     uint8_t* dst = r.tiles + (size_t)r.slot * (DP / 64) * AU_BLOCK_BYTES;
     const int valid = t.len - at;
     if (!clear || valid >= AU_ROWS) {
@@ -161,7 +185,7 @@ __device__ __forceinline__ bool au_produce(TileRing& r, const CUtensorMap* tm, c
             au_load<DP>(dst, tm, t, head, at, r.tail);
         }
         r.tail_open = true;
-        if (!warp_wait(r.tail, r.tail_phase, r.abort_flag)) return false;
+        if (!warp_wait(r.tail, r.tail_phase, r.watch)) return false;
         r.tail_open = false;
         r.tail_phase ^= 1u;
         for (int c = 0; c < DP / 64; ++c)
@@ -311,7 +335,7 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
     __shared__ uint64_t s_full[Plan::SLOTS], s_empty[Plan::SLOTS], s_qfull[2], s_qempty[2], s_scores[2][2], s_probs[2][2], s_added[2], s_done[2], s_sums[2], s_free[2], s_tail;
     __shared__ float s_sum[2][AU_ROWS];
     __shared__ uint32_t s_tmem;
-    __shared__ int s_abort;
+    __shared__ Watch s_watch;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint8_t* queries = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* ring_tiles = queries + 2 * Plan::TILE_BYTES;
@@ -331,7 +355,7 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
             ptx::mbar_init(&s_free[x], 4);
         }
         ptx::mbar_init(&s_tail, 1);
-        s_abort = 0;
+        s_watch = {};
         ptx::fence_barrier_init();
         ptx::fence_proxy_async();
     }
@@ -344,21 +368,21 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
     __syncthreads();
     ptx::tc_fence_after_sync();
     const uint32_t tmem = s_tmem;
-    volatile int* abort_flag = &s_abort;
+    volatile Watch* watch = &s_watch;
     grid_dependency_wait();
     bool ok = true;
-    ItemReader reader = {&s_queue, abort_flag};
+    ItemReader reader = {&s_queue, watch};
     Item item;
 
     if (warp >= AU_TMA_WARP) {
         ptx::registers_down<AU_OTHER_REGS>();
         if (warp == AU_ITEMS_WARP) {
-            ok = au_find_items<AF_QUERIES>(s_queue, a.s, order, abort_flag, [&](const Tile& t) { return au_key_tiles(t, a.causal, 0); }, [&](const Item& it) {
+            ok = au_find_items<AF_QUERIES>(s_queue, a.s, order, watch, [&](const Tile& t) { return au_key_tiles(t, a.causal, 0); }, [&](const Item& it) {
                 au_clear(a.o, it, AF_QUERIES, a.d);
                 for (int r = it.t.at + lane; a.lse && r < min(it.t.at + AF_QUERIES, it.t.rows); r += 32) a.lse[a.row_number(it.t, it.head) + r] = -INFINITY;
             });
         } else if (warp == AU_TMA_WARP) {
-            TileRing ring = {ring_tiles, s_full, s_empty, &s_tail, abort_flag, Plan::SLOTS, 0, 0, 0, 0, false};
+            TileRing ring = {ring_tiles, s_full, s_empty, &s_tail, watch, Plan::SLOTS, 0, 0, 0, 0, false};
             uint32_t q_phase[2] = {0, 0};
             while (reader.next(item, ok)) {
                 const Tile& t = item.t;
@@ -368,7 +392,7 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
                 for (int j = 0; j < n && ok; ++j) {
                     for (int x = 0; x < 2 && ok; ++x) {
                         if (j == 0 && (x ? n1 : n0) > 0) {
-                            ok = warp_wait(&s_qempty[x], q_phase[x] ^ 1u, abort_flag);
+                            ok = warp_wait(&s_qempty[x], q_phase[x] ^ 1u, watch);
                             if (!ok) break;
                             q_phase[x] ^= 1u;
                             if (ptx::elect_one()) {
@@ -396,7 +420,7 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
             const uint32_t q_addr = ptx::smem_u32(queries) + x * Plan::TILE_BYTES, ring_addr = ptx::smem_u32(ring_tiles);
             const uint32_t t_s = tmem + x * 128, t_o = tmem + 256 + x * 128;
             uint32_t q_phase = 0, p_phase = 0, f_phase = 1, base = 0;        // p_phase: bit `half`; base: ring tiles before the item
-            const auto wait = [&](uint64_t& bar, uint32_t parity) { return ptx::mbar_wait(&bar, parity & 1u, abort_flag); };
+            const auto wait = [&](uint64_t& bar, uint32_t parity) { return au_wait(&bar, parity & 1u, watch); };
             while (reader.next_alone(item, ok)) {
                 const int n = max(au_key_tiles(item.t, a.causal, 0), au_key_tiles(item.t, a.causal, 1)), mine = au_key_groups(item.t, a.causal, x, 64);
                 if (mine > 0) {
@@ -454,7 +478,7 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
                 if (t.at + x * AU_ROWS >= t.rows) continue;
                 float sum = 1.f;
                 if (n > 0) {
-                    ok = warp_wait(&s_sums[x], phase[x], abort_flag) && warp_wait(&s_done[x], phase[x], abort_flag);
+                    ok = warp_wait(&s_sums[x], phase[x], watch) && warp_wait(&s_done[x], phase[x], watch);
                     phase[x] ^= 1u;
                     if (!ok) break;
                     ptx::tc_fence_after_sync();
@@ -482,7 +506,7 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
             for (int g = 0; g < n; ++g, ++total) {
                 const int half = g & 1;
                 const uint32_t t_g = t_s + 64 * half;
-                ok = warp_wait(&s_scores[x][half], s_phase >> half & 1u, abort_flag);
+                ok = warp_wait(&s_scores[x][half], s_phase >> half & 1u, watch);
                 if (!ok) break;
                 s_phase ^= 1u << half;
                 ptx::tc_fence_after_sync();
@@ -516,7 +540,7 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
                     const bool rises = (seen - top) * c > AF_RISE;       // each row for itself: its result does not depend on its neighbours
                     if (!__any_sync(0xffffffffu, rises)) break;
                     // O is at rest once the last product handed over has been added to it
-                    ok = warp_wait(&s_added[x], total - 1 & 1u, abort_flag);
+                    ok = warp_wait(&s_added[x], total - 1 & 1u, watch);
                     if (!ok) break;
                     ptx::tc_fence_after_sync();
                     const float keep = rises ? exp2_approx((top - seen) * c) : 1.f;
@@ -543,7 +567,7 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
             if (!ok) break;
             if (a.lse && me < t.rows) a.lse[a.row_number(t, item.head) + me] = me < t.len ? fmaf(top, a.scale, logf(sum)) : -INFINITY;
             if (n > 0) {
-                ok = warp_wait(&s_free[x], f_phase, abort_flag);       // the item before has left, and its sums have been read
+                ok = warp_wait(&s_free[x], f_phase, watch);       // the item before has left, and its sums have been read
                 if (!ok) break;
                 f_phase ^= 1u;
                 s_sum[x][row] = sum;

@@ -40,8 +40,8 @@ struct StepReader {
 // A fixed tile, as soon as its place is free.  The whole warp.
 template <int DP>
 __device__ __forceinline__ bool ab_load_fixed(uint8_t* dst, const CUtensorMap* tm, const Item& item, uint64_t* full, uint64_t* empty, uint32_t phase,
-                                              volatile int* abort_flag) {
-    if (!warp_wait(empty, phase ^ 1u, abort_flag)) return false;
+                                              volatile Watch* watch) {
+    if (!warp_wait(empty, phase ^ 1u, watch)) return false;
     if (ptx::elect_one()) {
         ptx::mbar_arrive_expect_tx(full, DP / 64 * AU_BLOCK_BYTES);
         au_load<DP>(dst, tm, item.t, item.head, item.t.at, full);
@@ -67,7 +67,7 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
         s_rows_free, s_tail[2];
     __shared__ float s_less[AU_ROWS], s_delta[AU_ROWS];
     __shared__ uint32_t s_tmem;
-    __shared__ int s_abort;
+    __shared__ Watch s_watch;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint8_t* fixed = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* ring_tiles = fixed + 2 * Plan::TILE_BYTES;
@@ -88,7 +88,7 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
         ptx::mbar_init(&s_rows_free, 8);
         ptx::mbar_init(&s_tail[0], 1);
         ptx::mbar_init(&s_tail[1], 1);
-        s_abort = 0;
+        s_watch = {};
         ptx::fence_barrier_init();
         ptx::fence_proxy_async();
     }
@@ -101,29 +101,29 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
     __syncthreads();
     ptx::tc_fence_after_sync();
     const uint32_t tmem = s_tmem;
-    volatile int* abort_flag = &s_abort;
+    volatile Watch* watch = &s_watch;
     grid_dependency_wait();
     bool ok = true;
-    ItemReader reader = {&s_queue, abort_flag};
+    ItemReader reader = {&s_queue, watch};
     Item item;
 
     if (warp >= AU_TMA_WARP) {
         ptx::registers_down<AU_OTHER_REGS>();
         if (warp == AU_ITEMS_WARP) {
-            ok = au_find_items<AU_ROWS>(s_queue, a.s, order, abort_flag, [&](const Tile& t) { return au_key_tiles(t, a.causal, 0); },
+            ok = au_find_items<AU_ROWS>(s_queue, a.s, order, watch, [&](const Tile& t) { return au_key_tiles(t, a.causal, 0); },
                                         [&](const Item& it) { au_clear(a.dq, it, AU_ROWS, a.d); });
         } else if (warp == AU_TMA_WARP) {
-            TileRing keys = {ring_tiles, s_full, s_empty, &s_tail[0], abort_flag, K_SLOTS, 0, 0, 0, 0, false};
-            TileRing values = {ring_tiles + K_SLOTS * Plan::TILE_BYTES, s_full + K_SLOTS, s_empty + K_SLOTS, &s_tail[1], abort_flag, V_SLOTS, 0, 0, 0, 0, false};
+            TileRing keys = {ring_tiles, s_full, s_empty, &s_tail[0], watch, K_SLOTS, 0, 0, 0, 0, false};
+            TileRing values = {ring_tiles + K_SLOTS * Plan::TILE_BYTES, s_full + K_SLOTS, s_empty + K_SLOTS, &s_tail[1], watch, V_SLOTS, 0, 0, 0, 0, false};
             uint32_t f_phase = 0;
             while (reader.next(item, ok)) {
                 const Tile& t = item.t;
                 const int n = au_key_tiles(t, a.causal, 0), hk = item.head / a.group;
                 const bool clear = t.first + t.len < a.s.seq;
                 for (int j = 0; j < n && ok; ++j) {
-                    ok = (j > 0 || ab_load_fixed<DP>(fixed, &m.q, item, &s_ffull[0], &s_fempty[0], f_phase, abort_flag)) &&
+                    ok = (j > 0 || ab_load_fixed<DP>(fixed, &m.q, item, &s_ffull[0], &s_fempty[0], f_phase, watch)) &&
                          au_produce<DP>(keys, &m.k, t, hk, j * AU_ROWS, clear) &&
-                         (j > 0 || ab_load_fixed<DP>(fixed + Plan::TILE_BYTES, &m.d_o, item, &s_ffull[1], &s_fempty[1], f_phase, abort_flag)) &&
+                         (j > 0 || ab_load_fixed<DP>(fixed + Plan::TILE_BYTES, &m.d_o, item, &s_ffull[1], &s_fempty[1], f_phase, watch)) &&
                          au_produce<DP>(values, &m.v, t, hk, j * AU_ROWS, clear);
                 }
                 if (!ok) break;
@@ -140,7 +140,7 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
             const int steps = (a.d + 15) / 16;
             const uint32_t f_addr = ptx::smem_u32(fixed), ring_addr = ptx::smem_u32(ring_tiles);
             uint32_t q_phase = 0, free_phase = 1, scored = 0, taken = 0;        // the next tile of each kind of product
-            const auto wait = [&](uint64_t& bar, uint32_t parity) { return ptx::mbar_wait(&bar, parity & 1u, abort_flag); };
+            const auto wait = [&](uint64_t& bar, uint32_t parity) { return au_wait(&bar, parity & 1u, watch); };
             StepReader<false> ahead = {reader};
             Step now = {}, one = {};
 #pragma unroll 1
@@ -182,7 +182,7 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
             const int steps = (a.d + 15) / 16;
             const uint32_t f_addr = ptx::smem_u32(fixed) + Plan::TILE_BYTES, ring_addr = ptx::smem_u32(ring_tiles);
             uint32_t g_phase = 0;
-            const auto wait = [&](uint64_t& bar, uint32_t parity) { return ptx::mbar_wait(&bar, parity & 1u, abort_flag); };
+            const auto wait = [&](uint64_t& bar, uint32_t parity) { return au_wait(&bar, parity & 1u, watch); };
             StepReader<false> ahead = {reader};
 #pragma unroll 1
             for (uint32_t step = 0; ok; ++step) {
@@ -252,7 +252,7 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
                     }
                 }
                 if (lane < valid) a.delta[number + lane] = delta;
-                ok = warp_wait(&s_rows_free, rows_phase, abort_flag);
+                ok = warp_wait(&s_rows_free, rows_phase, watch);
                 if (!ok) break;
                 rows_phase ^= 1u;
                 s_less[row] = less;
@@ -263,7 +263,7 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
             if (any) {
                 const Tile& t = before.t;
                 const int me = t.at + row;
-                ok = warp_wait(&s_done, done_phase, abort_flag);
+                ok = warp_wait(&s_done, done_phase, watch);
                 if (!ok) break;
                 done_phase ^= 1u;
                 ptx::tc_fence_after_sync();
@@ -284,7 +284,7 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
             const Tile& t = item.t;
             const int n = au_key_tiles(t, a.causal, 0), me = t.at + row;
             const int last = a.causal ? min(me, t.len - 1) : t.len - 1;
-            ok = warp_wait(&s_rows, phase, abort_flag);
+            ok = warp_wait(&s_rows, phase, watch);
             if (!ok) break;
             phase ^= 1u;
             const float less = s_less[row], delta = s_delta[row];
@@ -292,7 +292,7 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
             if (lane == 0) ptx::mbar_arrive(&s_rows_free);
             for (int j = 0; j < n; ++j, ++step) {
                 const uint32_t t_s = tmem + (step & 1u) * 128 + half * 64 + lanes;
-                ok = warp_wait(&s_scores[step & 1u], (step >> 1) & 1u, abort_flag);
+                ok = warp_wait(&s_scores[step & 1u], (step >> 1) & 1u, watch);
                 if (!ok) break;
                 ptx::tc_fence_after_sync();
                 uint32_t s[2][32];
@@ -313,7 +313,7 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
                     mask_behind(s[0], limit, 0u);
                     mask_behind(s[1], limit - 32, 0u);
                 }
-                ok = warp_wait(&s_grads, step & 1u, abort_flag);
+                ok = warp_wait(&s_grads, step & 1u, watch);
                 if (!ok) break;
                 ptx::tc_fence_after_sync();
 #pragma unroll
@@ -364,7 +364,7 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
         s_tail;      // [0]: S, P, dV, log-sums; [1]: dP, dS, dK, deltas
     __shared__ __align__(16) float s_less[AU_ROWS], s_delta[AU_ROWS];
     __shared__ uint32_t s_tmem;
-    __shared__ int s_abort;
+    __shared__ Watch s_watch;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint8_t* fixed = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* ring_tiles = fixed + 2 * Plan::TILE_BYTES;
@@ -381,7 +381,7 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
             ptx::mbar_init(&s_free[x], 4);
         }
         ptx::mbar_init(&s_tail, 1);
-        s_abort = 0;
+        s_watch = {};
         ptx::fence_barrier_init();
         ptx::fence_proxy_async();
     }
@@ -394,22 +394,22 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
     __syncthreads();
     ptx::tc_fence_after_sync();
     const uint32_t tmem = s_tmem;
-    volatile int* abort_flag = &s_abort;
+    volatile Watch* watch = &s_watch;
     grid_dependency_wait();
     bool ok = true;
-    ItemReader reader = {&s_queue, abort_flag};
+    ItemReader reader = {&s_queue, watch};
     Item item;
     int from, per;
 
     if (warp >= AU_TMA_WARP) {
         ptx::registers_down<AU_OTHER_REGS>();
         if (warp == AU_ITEMS_WARP) {
-            ok = au_find_items<AU_ROWS>(s_queue, a.s, order, abort_flag, [&](const Tile& t) { return ab_query_tiles(t, a.causal, a.group, from, per); }, [&](const Item& it) {
+            ok = au_find_items<AU_ROWS>(s_queue, a.s, order, watch, [&](const Tile& t) { return ab_query_tiles(t, a.causal, a.group, from, per); }, [&](const Item& it) {
                 au_clear(a.dk, it, AU_ROWS, a.d);
                 au_clear(a.dv, it, AU_ROWS, a.d);
             });
         } else if (warp == AU_TMA_WARP) {
-            TileRing ring = {ring_tiles, s_full, s_empty, &s_tail, abort_flag, Plan::SLOTS, 0, 0, 0, 0, false};
+            TileRing ring = {ring_tiles, s_full, s_empty, &s_tail, watch, Plan::SLOTS, 0, 0, 0, 0, false};
             uint32_t f_phase = 0;
             while (reader.next(item, ok)) {
                 const Tile& t = item.t;
@@ -417,9 +417,9 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
                 const bool clear = t.first + t.len < a.s.seq;
                 for (int j = 0; j < n && ok; ++j) {
                     const int g = j / per, at = (from + j - g * per) * AU_ROWS, h = item.head * a.group + g;
-                    ok = (j > 0 || ab_load_fixed<DP>(fixed, &m.k, item, &s_ffull[0], &s_fempty[0], f_phase, abort_flag)) &&
+                    ok = (j > 0 || ab_load_fixed<DP>(fixed, &m.k, item, &s_ffull[0], &s_fempty[0], f_phase, watch)) &&
                          au_produce<DP>(ring, &m.q, t, h, at, clear) &&
-                         (j > 0 || ab_load_fixed<DP>(fixed + Plan::TILE_BYTES, &m.v, item, &s_ffull[1], &s_fempty[1], f_phase, abort_flag)) &&
+                         (j > 0 || ab_load_fixed<DP>(fixed + Plan::TILE_BYTES, &m.v, item, &s_ffull[1], &s_fempty[1], f_phase, watch)) &&
                          au_produce<DP>(ring, &m.d_o, t, h, at, clear);
                 }
                 if (!ok) break;
@@ -436,7 +436,7 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
             const uint32_t f_addr = ptx::smem_u32(fixed), ring_addr = ptx::smem_u32(ring_tiles);
             uint32_t f_phase = 0, free_phase = 3, phase = 0;        // bit `what`
             uint32_t scored = 0, taken = 0;         // ring tiles before the pair that the scores, and the weighted operands, take next
-            const auto wait = [&](uint64_t& bar, uint32_t parity) { return ptx::mbar_wait(&bar, parity & 1u, abort_flag); };
+            const auto wait = [&](uint64_t& bar, uint32_t parity) { return au_wait(&bar, parity & 1u, watch); };
             StepReader<true> ahead = {reader};
             Step now = {};
             for (bool begun = false; ok; begun = true) {
@@ -493,13 +493,13 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
                         less[u] = valid ? -a.lse_in[number + q] * LOG2E : -INFINITY;
                         delta[u] = valid ? -a.delta[number + q] : 0.f;
                     }
-                    ok = warp_wait(&s_weights[0], phase, abort_flag);
+                    ok = warp_wait(&s_weights[0], phase, watch);
                     if (!ok) break;
 #pragma unroll
                     for (int u = 0; u < 4; ++u) s_less[lane + 32 * u] = less[u];
                     __syncwarp();
                     if (lane == 0) ptx::mbar_arrive(&s_stats[0]);
-                    ok = warp_wait(&s_weights[1], phase, abort_flag);
+                    ok = warp_wait(&s_weights[1], phase, watch);
                     if (!ok) break;
 #pragma unroll
                     for (int u = 0; u < 4; ++u) s_delta[lane + 32 * u] = delta[u];
@@ -518,7 +518,7 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
             const Tile& t = item.t;
             const int me = t.at + row;
             for (int what = 0; what < 2 && ok; ++what) {
-                ok = warp_wait(&s_done[what], phase, abort_flag);
+                ok = warp_wait(&s_done[what], phase, watch);
                 if (!ok) break;
                 ptx::tc_fence_after_sync();
                 au_store(tmem + 256 + what * 128 + lanes, (what ? a.dk : a.dv).at<__nv_bfloat16>(t.b, t.first + me, item.head), a.d, what ? a.scale : 1.f, true,
@@ -537,7 +537,7 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
         while (reader.next(item, ok)) {
             const int n = ab_query_tiles(item.t, a.causal, a.group, from, per);
             for (int j = 0; j < n; ++j, phase ^= 1u) {
-                ok = warp_wait(&s_stats[0], phase, abort_flag) && warp_wait(&s_scores[0], phase, abort_flag);
+                ok = warp_wait(&s_stats[0], phase, watch) && warp_wait(&s_scores[0], phase, watch);
                 if (!ok) break;
                 ptx::tc_fence_after_sync();
                 uint32_t s[2][32];
@@ -574,7 +574,7 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
                 ptx::tc_fence_before_sync();
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(&s_weights[0]);
-                ok = warp_wait(&s_stats[1], phase, abort_flag) && warp_wait(&s_scores[1], phase, abort_flag);
+                ok = warp_wait(&s_stats[1], phase, watch) && warp_wait(&s_scores[1], phase, watch);
                 if (!ok) break;
                 ptx::tc_fence_after_sync();
 #pragma unroll

@@ -548,6 +548,29 @@ __global__ void selftest_bounded_wait_kernel(uint32_t polls) {
     const bool done = ptx::mbar_wait(&s_bar, 0, abort_flag, polls);
     if (!done && (threadIdx.x & 31) == 0) raise_status(DEV_TIMEOUT);
 }
+// One warp waits with a limit of 256 polls (about a millisecond) for another that shows progress every quarter of one, 32 times, and
+// only then arrives: eight times the limit.
+__global__ void selftest_progress_wait_kernel(uint32_t polls) {
+    __shared__ uint64_t s_bar;
+    __shared__ Watch s_watch;
+    if (threadIdx.x == 0) {
+        ptx::mbar_init(&s_bar, 1);
+        s_watch = {};
+        ptx::fence_barrier_init();
+    }
+    __syncthreads();
+    volatile Watch* watch = &s_watch;
+    if (threadIdx.x >= 32) {
+        const bool done = warp_wait(&s_bar, 0, watch, polls);
+        if (!done && threadIdx.x == 32) raise_status(DEV_TIMEOUT);
+    } else if (threadIdx.x == 0) {
+        for (uint32_t i = 1; i <= 32; ++i) {
+            for (int n = 0; n < 256; ++n) __nanosleep(1000);
+            watch->items = i;
+        }
+        ptx::mbar_arrive(&s_bar);
+    }
+}
 
 // ---- the operators around the projection ---------------------------------------------------
 namespace {
@@ -1281,6 +1304,11 @@ pamm_status pamm_clip_grad_norm(const pamm_tensor* grads, const pamm_tensor* out
 
 pamm_status pamm_selftest_bounded_wait(void* stream) {
     launch(selftest_bounded_wait_kernel, dim3(1), dim3(64), 0, (cudaStream_t)stream, false, (uint32_t)2048);
+    return launch_status();
+}
+
+pamm_status pamm_selftest_progress_wait(void* stream) {
+    launch(selftest_progress_wait_kernel, dim3(1), dim3(64), 0, (cudaStream_t)stream, false, (uint32_t)256);
     return launch_status();
 }
 

@@ -107,6 +107,7 @@ _SIGNATURES = {
     "pamm_dropout": ([_vp, _i64, _vp, _i64, _i64, _i64, _ci, _f64, _u64, _u64, _vp, _vp, _i64, _vp], _ci),
     "pamm_last_device_status": ([_vp], _ci),
     "pamm_selftest_bounded_wait": ([_vp], _ci),
+    "pamm_selftest_progress_wait": ([_vp], _ci),
     "pamm_probe_read": ([_ci, _vp, _i64, _i64, _i64, _vp, _vp, _vp], _ci),
     "pamm_launch_count": ([], ctypes.c_ulonglong),
     "pamm_set_profile_events": ([_ci, _vp, _vp], _ci),
@@ -577,6 +578,11 @@ def probe_read(kind: int, data: torch.Tensor, order=None, sum32=None, stream=Non
 def selftest_bounded_wait(stream=None) -> None:
     """Launch the kernel whose bounded wait must run out (sets ERR_TIMEOUT in the device status word)."""
     _check(_lib.pamm_selftest_bounded_wait(_stream(stream)), "pamm_selftest_bounded_wait")
+
+
+def selftest_progress_wait(stream=None) -> None:
+    """Launch the kernel that waits for longer than its limit beside another warp's progress (the status stays clear)."""
+    _check(_lib.pamm_selftest_progress_wait(_stream(stream)), "pamm_selftest_progress_wait")
 
 
 def last_device_status(stream=None, synchronize: bool = True) -> int:
