@@ -138,7 +138,11 @@ __device__ __forceinline__ bool au_find_items(ItemQueue& q, const Sequences& s, 
             ptx::take_next_block(&q.response, &q.answered);
         }
         __syncwarp();
-        if (!warp_wait(&q.answered, phase, watch)) return false;
+        if (!warp_wait(&q.answered, phase, watch)) {       // the answer lands before the block's memory is given back
+            int never = 0;
+            ptx::mbar_wait(&q.answered, phase, &never, 1u << 14);
+            return false;
+        }
         phase ^= 1u;
         w = ptx::taken_block(&q.response);
         __syncwarp();
@@ -208,6 +212,12 @@ __device__ __forceinline__ void au_drain(const TileRing& r) {
         const uint32_t it = r.used - d;
         ptx::mbar_wait(&r.full[it % r.slots], (it / r.slots) & 1u, &never, 1u << 14);
     }
+}
+// The same for the products of the thread that issued them: they end before the memory of their operands and sums is given back.
+__device__ __forceinline__ void au_settle(uint64_t* last) {
+    int never = 0;
+    ptx::umma_commit(last);
+    ptx::mbar_wait(last, 0, &never, 1u << 14);
 }
 
 // The products.  One thread.  A product is issued only shortly before it runs, so what this thread computes between two of them counts.
@@ -332,7 +342,7 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
     using Plan = AttentionPlan<DP>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(16) ItemQueue s_queue;
-    __shared__ uint64_t s_full[Plan::SLOTS], s_empty[Plan::SLOTS], s_qfull[2], s_qempty[2], s_scores[2][2], s_probs[2][2], s_added[2], s_done[2], s_sums[2], s_free[2], s_tail;
+    __shared__ uint64_t s_full[Plan::SLOTS], s_empty[Plan::SLOTS], s_qfull[2], s_qempty[2], s_scores[2][2], s_probs[2][2], s_added[2], s_done[2], s_sums[2], s_free[2], s_tail, s_last[2];
     __shared__ float s_sum[2][AU_ROWS];
     __shared__ uint32_t s_tmem;
     __shared__ Watch s_watch;
@@ -353,6 +363,7 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
             ptx::mbar_init(&s_done[x], 1);
             ptx::mbar_init(&s_sums[x], 4);
             ptx::mbar_init(&s_free[x], 4);
+            ptx::mbar_init(&s_last[x], 1);
         }
         ptx::mbar_init(&s_tail, 1);
         s_watch = {};
@@ -465,6 +476,7 @@ attention_forward_kernel(const __grid_constant__ AttentionArgs a, const __grid_c
                 if (!ok) break;
                 base += 2 * n;
             }
+            if (!ok) au_settle(&s_last[x]);
         }
     } else if (warp >= AU_FINISH_WARP) {
         ptx::registers_down<AU_OTHER_REGS>();

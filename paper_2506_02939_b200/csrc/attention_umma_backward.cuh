@@ -64,7 +64,7 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(16) ItemQueue s_queue;
     __shared__ uint64_t s_full[Plan::SLOTS], s_empty[Plan::SLOTS], s_ffull[2], s_fempty[2], s_scores[2], s_grads, s_read, s_ds[2], s_done, s_free, s_rows,
-        s_rows_free, s_tail[2];
+        s_rows_free, s_tail[2], s_last[2];
     __shared__ float s_less[AU_ROWS], s_delta[AU_ROWS];
     __shared__ uint32_t s_tmem;
     __shared__ Watch s_watch;
@@ -88,6 +88,8 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
         ptx::mbar_init(&s_rows_free, 8);
         ptx::mbar_init(&s_tail[0], 1);
         ptx::mbar_init(&s_tail[1], 1);
+        ptx::mbar_init(&s_last[0], 1);
+        ptx::mbar_init(&s_last[1], 1);
         s_watch = {};
         ptx::fence_barrier_init();
         ptx::fence_proxy_async();
@@ -176,6 +178,7 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
                 now = one;
                 one = two;
             }
+            if (!ok) au_settle(&s_last[0]);
         } else if (warp == AU_MMA_WARP + 1 && ptx::elect_one()) {
             // dP, as soon as the last one has been read
             const uint32_t idesc_s = ptx::umma_idesc_bf16(AU_ROWS, AU_ROWS);
@@ -200,6 +203,7 @@ attention_queries_backward_kernel(const __grid_constant__ AttentionArgs a, const
                 ptx::umma_commit(&s_empty[slot]);
                 if (now.last) ptx::umma_commit(&s_fempty[1]);
             }
+            if (!ok) au_settle(&s_last[1]);
         }
     } else if (warp >= AU_FINISH_WARP) {
         // An item's deltas and log-sums before its first step, while the item before is computed; then the gradients of that one.
@@ -361,7 +365,7 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(16) ItemQueue s_queue;
     __shared__ uint64_t s_full[Plan::SLOTS], s_empty[Plan::SLOTS], s_ffull[2], s_fempty[2], s_scores[2], s_weights[2], s_done[2], s_free[2], s_stats[2],
-        s_tail;      // [0]: S, P, dV, log-sums; [1]: dP, dS, dK, deltas
+        s_tail, s_last;      // [0]: S, P, dV, log-sums; [1]: dP, dS, dK, deltas
     __shared__ __align__(16) float s_less[AU_ROWS], s_delta[AU_ROWS];
     __shared__ uint32_t s_tmem;
     __shared__ Watch s_watch;
@@ -381,6 +385,7 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
             ptx::mbar_init(&s_free[x], 4);
         }
         ptx::mbar_init(&s_tail, 1);
+        ptx::mbar_init(&s_last, 1);
         s_watch = {};
         ptx::fence_barrier_init();
         ptx::fence_proxy_async();
@@ -476,6 +481,7 @@ attention_keys_backward_kernel(const __grid_constant__ AttentionArgs a, const __
                 }
                 now = one;
             }
+            if (!ok) au_settle(&s_last);
           }
         } else {
             uint32_t phase = 1;      // the first tile waits for nothing
