@@ -254,11 +254,15 @@ class DropoutFunction(torch.autograd.Function):
         return dX, dY.to(ctx.residual) if ctx.needs_input_grad[1] else None, None, None, None, None
 
 
-def dropout(X, p: float, seed: int, offset: int = 0, counter=None, residual=None):
-    """``residual`` + X / (1 - p) where the generator keeps it, as ``pamm.dropout``; ``residual`` has X's shape.  A ``counter`` must not
-    change between the forward and the backward pass."""
+def _same_shape(X, residual):
     if residual is not None and residual.shape != X.shape:
         raise ValueError("the residual has X's shape")
+
+
+def dropout(X, p: float, seed: int, offset: int = 0, counter=None, residual=None):
+    """``residual`` + X / (1 - p) where the generator keeps it, as ``pamm.dropout``; ``residual`` has X's shape and, as ``Norm``'s,
+    is taken in X's type.  A ``counter`` must not change between the forward and the backward pass."""
+    _same_shape(X, residual)
     return DropoutFunction.apply(X, residual, counter, float(p), int(seed), int(offset))
 
 
@@ -280,7 +284,8 @@ class Dropout(torch.nn.Module):
 
     def forward(self, X, residual=None):
         if not self.training or self.p == 0.0:
-            return X if residual is None else X + residual
+            _same_shape(X, residual)
+            return X if residual is None else X + residual.to(X.dtype)
         self.calls += 1
         return dropout(X, self.p, self.seed, self.calls << 32, self.counter, residual)
 

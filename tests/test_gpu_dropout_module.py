@@ -1,0 +1,31 @@
+"""The dropout module's masks and types."""
+import pytest
+import torch
+
+from paper_2506_02939_b200 import build as pamm_build
+
+pamm_build.build()
+from paper_2506_02939_b200.autograd import Dropout  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def normal(shape, dtype, seed):
+    return torch.randn(shape, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda").to(dtype)
+
+
+@pytest.mark.parametrize("types", [(BF16, F32), (F32, BF16)])
+def test_a_residual_of_another_type_in_every_mode(types):
+    x, r = normal((9, 40), types[0], 1).requires_grad_(), normal((9, 40), types[1], 2).requires_grad_()
+    module = Dropout(0.5, seed=3)
+    train = module(x, r)
+    evaluated, none = module.eval()(x, r), Dropout(0.0)(x, r)
+    assert torch.equal(evaluated, x + r.to(types[0])) and torch.equal(none, evaluated)
+    for y in (train, evaluated, none):
+        assert y.dtype == types[0]
+        x.grad = r.grad = None
+        y.backward(torch.ones_like(y))
+        assert x.grad.dtype == types[0] and r.grad.dtype == types[1] and (r.grad == 1).all()
+    same = Dropout(0.5, seed=3)(x, r.to(types[0]))
+    assert torch.equal(train, same)
