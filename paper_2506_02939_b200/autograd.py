@@ -267,27 +267,33 @@ def dropout(X, p: float, seed: int, offset: int = 0, counter=None, residual=None
 
 
 class Dropout(torch.nn.Module):
-    """Dropout with an optional residual addition, ``dropout(X)`` or ``dropout(X, residual)``: a fresh mask every call, the same ones for
-    the same ``seed``.  In evaluation mode X (+ residual) passes.  Two modules with one seed have the same masks: give each its own.
+    """Dropout with an optional residual addition, ``dropout(X)`` or ``dropout(X, residual)``: a fresh mask every call.  In evaluation mode
+    X (+ residual) passes.
+
+    Every call draws its key from torch's host generator: modules are independent of each other, ``torch.manual_seed`` repeats them, and
+    what restores that generator's state to run a forward pass again (activation checkpointing) gets the same mask again.
+    With a ``seed`` the masks follow from it and from ``calls``, the number of the call, alone.  Two modules with one seed have the same
+    masks then: give each its own.  Code that runs a forward pass a second time for its backward pass would draw another mask there.
 
     ``counter``: a one-element int64 tensor on the device that numbers the calls in a captured graph (counted up by the program
-    between replays); without it a graph replays the mask that it was captured with.
+    between replays); without it a graph replays the mask that it was captured with."""
 
-    ``calls`` numbers the calls outside a graph.  Code that runs a forward pass a second time for its backward pass (activation
-    checkpointing) would draw another mask there: give ``dropout`` a seed and an offset of your own instead."""
-
-    def __init__(self, p: float = 0.1, seed: int = 0, counter=None):
+    def __init__(self, p: float = 0.1, seed: int | None = None, counter=None):
         super().__init__()
         if not 0.0 <= p <= 1.0:
             raise ValueError(f"p is a probability, got {p}")
-        self.p, self.seed, self.counter, self.calls = float(p), int(seed), counter, 0
+        self.p, self.seed, self.counter, self.calls = float(p), None if seed is None else int(seed), counter, 0
 
     def forward(self, X, residual=None):
         if not self.training or self.p == 0.0:
             _same_shape(X, residual)
             return X if residual is None else X + residual.to(X.dtype)
-        self.calls += 1
-        return dropout(X, self.p, self.seed, self.calls << 32, self.counter, residual)
+        if self.seed is None:
+            key, offset = int(torch.empty((), dtype=torch.int64, device="cpu").random_()), 0
+        else:
+            self.calls += 1
+            key, offset = self.seed, self.calls << 32
+        return dropout(X, self.p, key, offset, self.counter, residual)
 
 
 def clip_grad_norm_(parameters, max_norm: float):

@@ -1,6 +1,7 @@
 """The dropout module's masks and types."""
 import pytest
 import torch
+import torch.utils.checkpoint
 
 from paper_2506_02939_b200 import build as pamm_build
 
@@ -29,3 +30,24 @@ def test_a_residual_of_another_type_in_every_mode(types):
         assert x.grad.dtype == types[0] and r.grad.dtype == types[1] and (r.grad == 1).all()
     same = Dropout(0.5, seed=3)(x, r.to(types[0]))
     assert torch.equal(train, same)
+
+
+@pytest.mark.parametrize("reentrant", [False, True])
+def test_two_layers_under_checkpointing(reentrant):
+    """The masks of two modules differ, and the gradient has the ones that the loss had."""
+    x = normal((64, 128), F32, 4).requires_grad_()
+    a, b = Dropout(0.5), Dropout(0.5)
+    seen = []
+
+    def layers(t):
+        one = a(t)
+        two = b(torch.ones_like(t))
+        seen.append((one.detach() != 0, two.detach() != 0))
+        return one * two
+
+    y = torch.utils.checkpoint.checkpoint(layers, x, use_reentrant=reentrant)
+    torch.rand(3)
+    y.sum().backward()
+    (m, n), again = seen
+    assert torch.equal(m, again[0]) and torch.equal(n, again[1]) and not torch.equal(m, n)
+    assert torch.equal(x.grad, torch.where(m & n, 4.0, 0.0))
