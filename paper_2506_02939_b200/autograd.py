@@ -273,7 +273,8 @@ class Dropout(torch.nn.Module):
     Every call draws its key from torch's host generator: modules are independent of each other, ``torch.manual_seed`` repeats them, and
     what restores that generator's state to run a forward pass again (activation checkpointing) gets the same mask again.
     With a ``seed`` the masks follow from it and from ``calls``, the number of the call, alone.  Two modules with one seed have the same
-    masks then: give each its own.  Code that runs a forward pass a second time for its backward pass would draw another mask there.
+    masks then: give each its own.  A call from a backward pass, where activation checkpointing runs a forward pass again, is refused,
+    because its number would not be the first call's.
 
     ``counter``: a one-element int64 tensor on the device that numbers the calls in a captured graph (counted up by the program
     between replays); without it a graph replays the mask that it was captured with."""
@@ -290,6 +291,9 @@ class Dropout(torch.nn.Module):
             return X if residual is None else X + residual.to(X.dtype)
         if self.seed is None:
             key, offset = int(torch.empty((), dtype=torch.int64, device="cpu").random_()), 0
+        elif torch._C._current_graph_task_id() != -1:
+            raise RuntimeError("a Dropout with a seed numbers its calls and would draw another mask for the same activations in a backward pass "
+                               "(activation checkpointing): give it no seed, or call dropout() with an offset")
         else:
             self.calls += 1
             key, offset = self.seed, self.calls << 32

@@ -70,3 +70,16 @@ def test_checkpointing_draws_the_same_masks_again(drawn, reentrant):
     torch.rand(5)                                            # something else draws in between
     y.sum().backward()
     assert len(drawn) == 4 and drawn[2:] == drawn[:2] and drawn[0] != drawn[1]
+
+
+@pytest.mark.parametrize("reentrant", [False, True])
+def test_a_seeded_module_is_refused_in_a_backward_pass(drawn, reentrant):
+    x = torch.ones(3, requires_grad=True)
+    module = Dropout(0.5, seed=4)
+    y = torch.utils.checkpoint.checkpoint(lambda t: module(t).exp(), x, use_reentrant=reentrant)
+    with pytest.raises(RuntimeError, match="seed"):
+        y.sum().backward()
+    assert drawn == [(4, 1 << 32)] and module.calls == 1
+    module(x).sum().backward()                               # outside it works on
+    module.eval()                                            # and in evaluation mode anywhere
+    torch.utils.checkpoint.checkpoint(lambda t: module(t).exp(), x, use_reentrant=reentrant).sum().backward()

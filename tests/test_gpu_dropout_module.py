@@ -51,3 +51,15 @@ def test_two_layers_under_checkpointing(reentrant):
     (m, n), again = seen
     assert torch.equal(m, again[0]) and torch.equal(n, again[1]) and not torch.equal(m, n)
     assert torch.equal(x.grad, torch.where(m & n, 4.0, 0.0))
+
+
+@pytest.mark.parametrize("reentrant", [False, True])
+def test_a_seeded_module_is_refused_in_a_backward_pass(reentrant):
+    x = normal((8, 16), F32, 5).requires_grad_()
+    module = Dropout(0.5, seed=4)
+    y = torch.utils.checkpoint.checkpoint(lambda t: module(t).exp(), x, use_reentrant=reentrant)
+    with pytest.raises(RuntimeError, match="seed"):
+        y.sum().backward()
+    again = Dropout(0.5, seed=4)
+    again(x)
+    assert torch.equal(module(x), again(x))
