@@ -272,7 +272,7 @@ class Dropout(torch.nn.Module):
 
     Every call draws its key from torch's host generator: modules are independent of each other, ``torch.manual_seed`` repeats them, and
     what restores that generator's state to run a forward pass again (activation checkpointing) gets the same mask again.
-    With a ``seed`` the masks follow from it and from ``calls``, the number of the call, alone.  Two modules with one seed have the same
+    With a ``seed`` the masks follow from it and from ``calls``, the number of the call, alone; the state dict has that number.  Two modules with one seed have the same
     masks then: give each its own.  A call from a backward pass, where activation checkpointing runs a forward pass again, is refused,
     because its number would not be the first call's.
 
@@ -298,6 +298,16 @@ class Dropout(torch.nn.Module):
             self.calls += 1
             key, offset = self.seed, self.calls << 32
         return dropout(X, self.p, key, offset, self.counter, residual)
+
+    def get_extra_state(self):
+        return torch.tensor(self.calls, dtype=torch.int64, device="cpu")
+
+    def set_extra_state(self, state):
+        self.calls = int(state)
+
+    def _load_from_state_dict(self, state_dict, prefix, *args):
+        state_dict.setdefault(prefix + "_extra_state", self.get_extra_state())       # one from before there was a number
+        super()._load_from_state_dict(state_dict, prefix, *args)
 
 
 def clip_grad_norm_(parameters, max_norm: float):

@@ -83,3 +83,19 @@ def test_a_seeded_module_is_refused_in_a_backward_pass(drawn, reentrant):
     module(x).sum().backward()                               # outside it works on
     module.eval()                                            # and in evaluation mode anywhere
     torch.utils.checkpoint.checkpoint(lambda t: module(t).exp(), x, use_reentrant=reentrant).sum().backward()
+
+
+def test_a_resumed_run_goes_on_with_the_masks(drawn, tmp_path):
+    x = torch.ones(3)
+    a = torch.nn.Sequential(Dropout(0.5, seed=4), Dropout(0.5))
+    for _ in range(3):
+        a(x)
+    torch.save(a.state_dict(), tmp_path / "state.pt")
+    b = torch.nn.Sequential(Dropout(0.5, seed=4), Dropout(0.5))
+    b.load_state_dict(torch.load(tmp_path / "state.pt"))
+    a[0](x), b[0](x)
+    assert drawn[-1] == drawn[-2] == (4, 4 << 32)
+    b.load_state_dict({})                                    # one that does not have the number
+    assert b[0].calls == 4
+    with pytest.raises(RuntimeError):
+        b.load_state_dict({"2.weight": x})
