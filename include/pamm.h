@@ -486,7 +486,8 @@ pamm_status pamm_clip_grad_norm(const pamm_tensor* grads, const pamm_tensor* out
  * and infinities too).  Among valid tokens a value that is not finite reaches what the formulas say, and may reach other
  * rows of its sequence as 0 times infinity does.
  *   pamm_heads   element (b, s, h, d) of a tensor lies at data + b batch + s token + h head + d, distances in elements, of any
- *                sign and order; 0 repeats (not in outputs).  Q, O: `heads` heads; K, V: kv_heads, a divisor.
+ *                sign and order; 0 repeats (not in outputs).  Q, O: `heads` heads; K, V: kv_heads, a divisor (none without a
+ *                query head).
  *   lse          batch x heads x seq fp32, contiguous; NULL in the forward call: not wanted
  *   scale        positive and finite
  *   lengths      NULL, or `batch` entries: the first lengths[b] tokens of sequence b are valid

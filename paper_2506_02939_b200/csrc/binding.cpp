@@ -403,7 +403,7 @@ struct AttentionCall {
         heads = Q.size(dims - 2);
         d = Q.size(dims - 1);
         kv_heads = K.size(dims - 2);
-        if (heads > 0 && (kv_heads < 1 || heads % kv_heads))
+        if (heads > 0 ? kv_heads < 1 || heads % kv_heads : kv_heads > 0)
             fail(PyExc_ValueError, "%lld query heads cannot share %lld key heads evenly", (long long)heads, (long long)kv_heads);
         holds(Q, "Q", heads);
         holds(K, "K", kv_heads);

@@ -965,7 +965,7 @@ pamm_status check_attention(const AttentionShape& g, pamm_dtype dt, float scale,
     if (g.batch < 0 || g.seq < 0 || g.heads < 0 || g.kv_heads < 0 || g.d < 1 || !(scale > 0.f) || !std::isfinite(scale)) return PAMM_ERR_INVALID_ARG;
     if (lengths && starts) return PAMM_ERR_INVALID_ARG;
     if (starts && (g.batch != 1 || g.sequences < 0)) return PAMM_ERR_INVALID_ARG;
-    if (g.heads > 0 && (g.kv_heads == 0 || g.heads % g.kv_heads)) return PAMM_ERR_INVALID_ARG;
+    if (g.heads > 0 ? g.kv_heads == 0 || g.heads % g.kv_heads : g.kv_heads > 0) return PAMM_ERR_INVALID_ARG;
     const size_t entry = index_type == PAMM_POS_I64 ? 8 : 4;
     if ((lengths && !aligned(lengths, entry)) || (starts && !aligned(starts, entry))) return PAMM_ERR_INVALID_ARG;
     if (g.d > ATT_MAX_DIM || g.batch > MAX_ROWS || g.seq > MAX_ROWS || g.heads > MAX_ROWS || (starts && g.sequences > MAX_ROWS - 2))
