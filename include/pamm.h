@@ -496,8 +496,9 @@ pamm_status pamm_clip_grad_norm(const pamm_tensor* grads, const pamm_tensor* out
  *                starts[sequences] on are in no sequence: not valid
  *   index_type   of lengths or starts (device arrays; one of them at most)
  * An entry that is negative, larger than seq or falls raises PAMM_ERR_BAD_INDEX in the device status and is taken as the nearest
- * possible one.  No output overlaps an input or another output (one that begins where another tensor does is refused).  Limits: head_dim <= 256, batch x seq x heads < 2^40,
- * seq < 2^31 - 1024, fewer than 2^31 - 1024 tiles of 32 rows over all heads and sequences.
+ * possible one.  No output (the log-sums of the forward call and the workspace are some too) overlaps an input or another output;
+ * one that begins where another tensor does is refused.  Limits: head_dim <= 256, batch x seq x heads < 2^40, seq < 2^31 - 1024,
+ * fewer than 2^31 - 1024 tiles of 32 rows over all heads and sequences.
  * bf16 heads of up to 128, in multiples of 8, with 16-byte aligned rows are computed on the tensor cores, with probabilities (and, in
  * the backward pass, score gradients) rounded to bf16 as operands of their products; everything else is fp32.
  */

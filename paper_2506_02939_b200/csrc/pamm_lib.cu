@@ -1095,7 +1095,7 @@ pamm_status pamm_attention_forward(const pamm_heads* Q, const pamm_heads* K, con
     const size_t es = esize(dt);
     AttentionArgs a = {};
     if (!heads_view(Q, g, heads, es, false, a.q) || !heads_view(K, g, kv_heads, es, false, a.k) || !heads_view(V, g, kv_heads, es, false, a.v) ||
-        !heads_view(O, g, heads, es, true, a.o) || !aligned(lse, 4) || !begin_apart({Q->data, K->data, V->data, lse}, {O->data}))
+        !heads_view(O, g, heads, es, true, a.o) || !aligned(lse, 4) || !begin_apart({Q->data, K->data, V->data}, {O->data, lse}))
         return PAMM_ERR_INVALID_ARG;
     a.lse = lse;
     a.s = sequences_of(g, lengths, starts, index_type);
@@ -1121,7 +1121,7 @@ pamm_status pamm_attention_backward(const pamm_heads* dO, const pamm_heads* Q, c
         !heads_view(dK, g, kv_heads, es, true, a.dk) || !heads_view(dV, g, kv_heads, es, true, a.dv) || !lse || !aligned(lse, 4))
         return PAMM_ERR_INVALID_ARG;
     if (!workspace || !aligned(workspace, 16) || ws_bytes < attention_backward_ws_bytes(batch * seq, heads)) return PAMM_ERR_WORKSPACE;
-    if (!begin_apart({dO->data, Q->data, K->data, V->data, O->data, lse, workspace}, {dQ->data, dK->data, dV->data})) return PAMM_ERR_INVALID_ARG;
+    if (!begin_apart({dO->data, Q->data, K->data, V->data, O->data, lse}, {dQ->data, dK->data, dV->data, workspace})) return PAMM_ERR_INVALID_ARG;
     a.lse_in = lse;
     a.delta = static_cast<float*>(workspace);
     a.s = sequences_of(g, lengths, starts, index_type);
