@@ -495,8 +495,9 @@ pamm_status pamm_clip_grad_norm(const pamm_tensor* grads, const pamm_tensor* out
  *                has the tokens starts[i] .. starts[i+1] - 1, all of them valid; tokens before starts[0] and from
  *                starts[sequences] on are in no sequence: not valid
  *   index_type   of lengths or starts (device arrays; one of them at most)
- * An entry that is negative, larger than seq or falls raises PAMM_ERR_BAD_INDEX in the device status and is taken as the nearest
- * possible one.  No output (the log-sums of the forward call and the workspace are some too) overlaps an input or another output;
+ * An entry that is negative or larger than seq raises PAMM_ERR_BAD_INDEX in the device status and is taken as the nearest possible
+ * one.  Starts that fall raise it too; which sequence a token is then in, and what the outputs hold, is not specified, but nothing
+ * outside of the tensors is read or written.  No output (the log-sums of the forward call and the workspace are some too) overlaps an input or another output;
  * one that begins where another tensor does is refused.  Limits: head_dim <= 256, batch x seq x heads < 2^40, seq < 2^31 - 1024,
  * fewer than 2^31 - 1024 tiles of 32 rows over all heads and sequences.
  * bf16 heads of up to 128, in multiples of 8, with 16-byte aligned rows are computed on the tensor cores, with probabilities (and, in

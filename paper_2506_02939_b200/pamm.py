@@ -526,7 +526,8 @@ def attention_forward(Q, K, V, causal: bool = False, lengths=None, starts=None, 
     ``Z.split((heads, kv_heads, kv_heads), -2)`` of the fused row.  ``lengths`` (batch,): the valid tokens of each padded sequence;
     ``starts`` (sequences + 1,): where sequences packed along the one token axis begin, and the last one's end; both on the
     device, int32 or int64.  ``scale`` is 1 / sqrt(head_dim) by default.  Returns O, contiguous by token unless given, and the rows' log-sums
-    (batch, heads, tokens) or (heads, tokens), fp32; rows of tokens that are not valid are 0 and -infinity."""
+    (batch, heads, tokens) or (heads, tokens), fp32; rows of tokens that are not valid are 0 and -infinity.  Entries out of range or starts
+    that fall show in ``last_device_status``; where starts fall the outputs are not specified."""
     return _binding_on(stream, _binding.attention_forward, Q, K, V, causal, lengths, starts, scale, O, lse)
 
 

@@ -78,3 +78,30 @@ def test_a_million_empty_sequences_between_two():
     for a, b in zip((O, lse, *grads), (o, l, *pamm.attention_backward(q, q, k, v, o, l, lengths=few))):
         assert torch.equal(a[[0, -1]], b)
         assert (a[1:-1] == (-math.inf if a is lse else 0.0)).all()
+
+
+def test_falling_starts_are_reported_and_stay_in_bounds():
+    tokens, heads, d, guard = 150, 3, 64, 4096
+    Q, K, V = torch.randn((tokens, heads + 2, d), generator=torch.Generator(device="cuda").manual_seed(5), device="cuda").to(BF16).split((heads, 1, 1), -2)
+
+    def guarded(shape, dtype=BF16):
+        n = math.prod(shape)
+        whole = torch.full((n + 2 * guard,), 3.0, dtype=dtype, device="cuda")
+        return whole, whole[guard:guard + n].view(shape)
+
+    rows = {"O": (tokens, heads, d), "dQ": (tokens, heads, d), "dK": (tokens, 1, d), "dV": (tokens, 1, d)}
+    for dtype in (BF16, torch.float32):
+        q, k, v = (t.to(dtype) for t in (Q, K, V))
+        for starts in ([0, 100, 50, 150], [150, 0], [0, 150, 0, 150, 0, 150], [120, 30, 31, 20, 150], list(range(150, -1, -1))):
+            out = {n: guarded(s, dtype) for n, s in rows.items()}
+            out["lse"] = guarded((heads, tokens), torch.float32)
+            s = torch.tensor(starts, device="cuda")
+            O, lse = pamm.attention_forward(q, k, v, starts=s, O=out["O"][1], lse=out["lse"][1])
+            assert pamm.last_device_status() == pamm.ERR_BAD_INDEX, starts
+            pamm.attention_backward(q, q, k, v, O, lse, starts=s, **{n: out[n][1] for n in ("dQ", "dK", "dV")})
+            assert pamm.last_device_status() == pamm.ERR_BAD_INDEX, starts
+            for whole, _ in out.values():
+                assert (whole[:guard] == 3.0).all() and (whole[-guard:] == 3.0).all()
+        sound = torch.tensor([0, 50, 150], device="cuda")
+        a, b = pamm.attention_forward(q, k, v, starts=sound)[0], pamm.attention_forward(q[50:], k[50:], v[50:])[0]
+        assert pamm.last_device_status() == pamm.OK and torch.equal(a[50:], b)
