@@ -30,7 +30,7 @@ struct HeadsView {
 struct Sequences {
     const void *lengths, *starts;
     int64_t seq;
-    int batch, count, items;        // items: tiles of all sequences, one head's; an upper bound where packed
+    int batch, count;
     bool i64;
 };
 // A tile of one sequence: tokens first .. first + rows - 1 of batch entry b are written, the first `len` of them are valid.

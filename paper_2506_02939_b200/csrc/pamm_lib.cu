@@ -976,33 +976,34 @@ pamm_status check_attention(const AttentionShape& g, pamm_dtype dt, float scale,
     const int64_t tiles = starts ? g.seq / AG_ROWS + g.sequences + 2 : g.batch * ((g.seq + AG_ROWS - 1) / AG_ROWS);
     return tiles > MAX_ROWS / g.heads ? PAMM_ERR_UNSUPPORTED : PAMM_OK;
 }
+// Tiles of all sequences, one head's; an upper bound where packed.
 inline int tiles_of(const Sequences& s, int64_t size) {
     return (int)(s.starts ? s.seq / size + s.count + 2 : s.batch * ((s.seq + size - 1) / size));
 }
 Sequences sequences_of(const AttentionShape& g, const void* lengths, const void* starts, pamm_position_type index_type) {
-    return {lengths, starts, g.seq, (int)g.batch, starts ? (int)g.sequences : 0, 0, index_type == PAMM_POS_I64};
+    return {lengths, starts, g.seq, (int)g.batch, starts ? (int)g.sequences : 0, index_type == PAMM_POS_I64};
 }
 
 template <typename T, int DP>
-pamm_status launch_attention_forward_generic(AttentionArgs a, cudaStream_t st) {
+pamm_status launch_attention_forward_generic(const AttentionArgs& a, cudaStream_t st) {
     const size_t smem = ag_smem<DP, false>;
     if (!ensure_dynamic_smem((const void*)attention_forward_generic_kernel<T, DP>, smem)) return PAMM_ERR_CUDA;
-    a.s.items = tiles_of(a.s, AG_ROWS);
-    launch(attention_forward_generic_kernel<T, DP>, dim3((unsigned)a.s.items * a.heads), dim3(AG_THREADS), smem, st, true, a,
+    const int items = tiles_of(a.s, AG_ROWS);
+    launch(attention_forward_generic_kernel<T, DP>, dim3((unsigned)items * a.heads), dim3(AG_THREADS), smem, st, true, a,
            attention_order(a.s, a.heads, AG_ROWS, sm_count(), a.causal));
     return launch_result("attention_forward_generic_kernel launch");
 }
 template <typename T, int DP>
-pamm_status launch_attention_backward_generic(AttentionArgs a, cudaStream_t st) {
+pamm_status launch_attention_backward_generic(const AttentionArgs& a, cudaStream_t st) {
     const size_t smem = ag_smem<DP, true>;
     if (!ensure_dynamic_smem((const void*)attention_backward_generic_kernel<T, DP, false>, smem) ||
         !ensure_dynamic_smem((const void*)attention_backward_generic_kernel<T, DP, true>, smem))
         return PAMM_ERR_CUDA;
-    a.s.items = tiles_of(a.s, AG_ROWS);
+    const int items = tiles_of(a.s, AG_ROWS);
     const int kv = a.heads / a.group, sms = sm_count();
-    launch(attention_backward_generic_kernel<T, DP, false>, dim3((unsigned)a.s.items * a.heads), dim3(AG_THREADS), smem, st, true, a,
+    launch(attention_backward_generic_kernel<T, DP, false>, dim3((unsigned)items * a.heads), dim3(AG_THREADS), smem, st, true, a,
            attention_order(a.s, a.heads, AG_ROWS, sms, a.causal));
-    launch(attention_backward_generic_kernel<T, DP, true>, dim3((unsigned)a.s.items * kv), dim3(AG_THREADS), smem, st, true, a,
+    launch(attention_backward_generic_kernel<T, DP, true>, dim3((unsigned)items * kv), dim3(AG_THREADS), smem, st, true, a,
            attention_order(a.s, kv, AG_ROWS, sms, false));
     return launch_result("attention_backward_generic_kernel launch");
 }
@@ -1014,26 +1015,26 @@ pamm_status run_attention_generic(const AttentionArgs& a, bool back, cudaStream_
 }
 
 template <int DP>
-pamm_status launch_attention_forward(AttentionArgs a, const AttentionMaps& m, cudaStream_t st) {
+pamm_status launch_attention_forward(const AttentionArgs& a, const AttentionMaps& m, cudaStream_t st) {
     using Plan = AttentionPlan<DP>;
     if (!ensure_dynamic_smem((const void*)attention_forward_kernel<DP>, Plan::SMEM)) return PAMM_ERR_CUDA;
-    a.s.items = tiles_of(a.s, AF_QUERIES);
-    launch(attention_forward_kernel<DP>, dim3((unsigned)(a.s.items * a.heads)), dim3(AU_THREADS), Plan::SMEM, st, true, a, m,
+    const int items = tiles_of(a.s, AF_QUERIES);
+    launch(attention_forward_kernel<DP>, dim3((unsigned)(items * a.heads)), dim3(AU_THREADS), Plan::SMEM, st, true, a, m,
            attention_order(a.s, a.heads, AF_QUERIES, sm_count(), a.causal));
     return launch_result("attention_forward_kernel launch");
 }
 
 template <int DP>
-pamm_status launch_attention_backward(AttentionArgs a, const AttentionMaps& m, cudaStream_t st) {
+pamm_status launch_attention_backward(const AttentionArgs& a, const AttentionMaps& m, cudaStream_t st) {
     using Plan = AttentionPlan<DP>;
     if (!ensure_dynamic_smem((const void*)attention_queries_backward_kernel<DP>, Plan::SMEM) ||
         !ensure_dynamic_smem((const void*)attention_keys_backward_kernel<DP>, Plan::SMEM))
         return PAMM_ERR_CUDA;
-    a.s.items = tiles_of(a.s, AU_ROWS);
+    const int items = tiles_of(a.s, AU_ROWS);
     const int kv = a.heads / a.group;
-    launch(attention_queries_backward_kernel<DP>, dim3((unsigned)(a.s.items * a.heads)), dim3(AU_THREADS), Plan::SMEM, st, true, a, m,
+    launch(attention_queries_backward_kernel<DP>, dim3((unsigned)(items * a.heads)), dim3(AU_THREADS), Plan::SMEM, st, true, a, m,
            attention_order(a.s, a.heads, AU_ROWS, sm_count(), a.causal));
-    launch(attention_keys_backward_kernel<DP>, dim3((unsigned)(a.s.items * kv)), dim3(AU_THREADS), Plan::SMEM, st, true, a, m,
+    launch(attention_keys_backward_kernel<DP>, dim3((unsigned)(items * kv)), dim3(AU_THREADS), Plan::SMEM, st, true, a, m,
            attention_order(a.s, kv, AU_ROWS, sm_count(), false));
     return launch_result("attention_keys_backward_kernel launch");
 }
