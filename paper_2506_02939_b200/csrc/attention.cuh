@@ -142,8 +142,9 @@ struct AttentionArgs {
 // Products in fp32 by fused multiply-adds: tiles of 32 x 64 scores, 16 a thread in 4 rows, whose operands come out of shared
 // memory as vectors along the head (rows 4 words past a multiple of 32 apart: no bank conflicts).  They serve fp32, heads
 // that are not multiples of 8 or wider than 128, and rows off the 16-byte grid.  Bound by multiply-adds and reads of shared memory, and
-// by their latency where an SM's last blocks are alone.  8 x 256 tokens of 8 heads of 64, causal: 29 us forward, 83 backward; 31 and 87
-// with one multiply-add an instruction; 33 and 113 in blocks of 64 rows and 256 threads, 2 an SM and unevenly loaded.
+// by their latency where an SM's last blocks are alone.  8 x 256 tokens of 8 heads of 64, causal, in a CUDA graph: 29 us forward, 80 backward
+// (through the Python entry 35 and 92); 31 and 87 with one multiply-add an instruction; 33 and 113 in blocks of 64 rows and 256 threads,
+// 2 an SM and unevenly loaded.  The sizes of blocks and tiles were measured on that batch alone.
 constexpr int AG_ROWS = 32, AG_TILE = 64, AG_THREADS = 4 * AG_ROWS, AG_P_LD = AG_TILE + 4;       // owned rows, streamed rows
 
 // Whether the two streamed tiles have a place each, so that the one is on its way while the other is worked on.
